@@ -39,6 +39,11 @@ admmq_status admmq_test_w_update_series(admmq_ctx* ctx, const float* d_W0, int d
                                         const float* d_zero, const float* d_V, double rho, int terms,
                                         float* d_Z_out);
 
+/* The bound of every device-side wait of the tensor-core projection (admmq_linear_forward for more than 16 rows,
+ * admmq_linear_grad_input), and whether its producer withholds every load: as admmq_test_set_wait, but for the whole
+ * process, since those calls have no context.  hold_loads = 0 and 2e9 cycles restore normal operation. */
+admmq_status admmq_test_linear_set_wait(long long wait_limit_cycles, int hold_loads);
+
 #ifdef __cplusplus
 }
 #endif

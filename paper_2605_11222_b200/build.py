@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadmmq.so")
 SOURCES = ["api.cu", "elem.cu", "gemm_simt.cu", "gemm_tc.cu", "tridiag.cu", "tridiag_blocked.cu", "local_search.cu", "pair_swap.cu",
-           "objective_static.cu"]
+           "objective_static.cu", "adapt_api.cu", "linear_small.cu", "linear_tc.cu", "adapter_grad.cu", "checkpoint8.cu",
+           "qk_rope.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
@@ -27,7 +28,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    headers.append(os.path.join(os.path.dirname(HERE), "include", "admmq.h"))
+    include = os.path.join(os.path.dirname(HERE), "include")
+    headers += [os.path.join(include, f) for f in os.listdir(include) if f.endswith(".h")]
 
     def compile_one(name):
         src = os.path.join(CSRC, name)

@@ -1,0 +1,269 @@
+// Gradients of the adapters:  G_a[r][c] = sum over the rows t of adapter a of f[t][r] v[t][c],
+// once with (f, v) = (u, x) for down and once with (h, dy) for up, both in one launch.
+//
+// Bound: memory, the one pass over x (8 bits a value when it comes from a checkpoint) and dy; the factors f are rank
+// values a row.  A CTA owns 128 columns (one checkpoint block) of one adapter and a share of its rows.  Rows arrive 64 at
+// a time through registers (the next 64 are on their way while these are multiplied) and become bf16 tiles
+// [row][column], which ldmatrix.trans turns into operands of mma.sync: the contraction runs over the rows, so both
+// operands are read across their storage order.  (The tensor work, 2 rank flop a value read, is far below what
+// mma.sync delivers: tcgen05 would wait for the same loads.)
+// The shares of one (adapter, columns) tile form a cluster; their fp32 sums meet over distributed shared memory and
+// are added in rank order, so nothing goes through global memory and the result does not depend on timing.
+//
+// Rounding.  x^ = scale code: the code (at most 127) is exact in bf16 and the scale is multiplied into f in fp32, so
+// f scale is rounded once, as f is on the bf16 path: 2^-9 relative a term, the size of the output's own rounding.
+#include <cooperative_groups.h>
+
+#include "adapt.h"
+
+namespace cg = cooperative_groups;
+
+namespace admmq {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int COLS = 128, ROWS = 64;
+constexpr int V_STRIDE = COLS + 8;                 // bf16; 272 bytes: eight rows of 16 bytes fall in eight bank groups
+
+struct Side {
+  const float* f;            // [T][rank]
+  const bf16* v;             // [T][ldv] or NULL: codes
+  long long ldv;
+  const int8_t* codes;       // [T][width]
+  const float* scale;        // [T][nb]
+  bf16* grad;                // [n][rank][width]
+  int width, nb;
+};
+struct GradParams {
+  Side side[2];              // down, up
+  int tiles0;                // column tiles of side 0
+  const int* order;
+  const int* offsets;
+  long long T;
+  int rank;
+};
+
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], const void* p) {
+  const uint32_t a = (uint32_t)__cvta_generic_to_shared(p);
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a));
+}
+
+// MT tiles of 16 ranks.
+template <int MT>
+__global__ void __launch_bounds__(THREADS) adapter_grad_kernel(const __grid_constant__ GradParams P) {
+  constexpr int RP = 16 * MT;
+  constexpr int F_STRIDE = RP + 8;
+  constexpr int TILE_BYTES = ROWS * (V_STRIDE + F_STRIDE) * 2;
+  constexpr int SUM_BYTES = RP * COLS * 4;
+  constexpr int BYTES = TILE_BYTES > SUM_BYTES ? TILE_BYTES : SUM_BYTES;
+  extern __shared__ __align__(16) uint8_t smem[];
+  bf16* vt = reinterpret_cast<bf16*>(smem);                       // [ROWS][V_STRIDE]
+  bf16* ft = vt + ROWS * V_STRIDE;                                // [ROWS][F_STRIDE]
+  float* sums = reinterpret_cast<float*>(smem);                   // [RP][COLS], after the last tile
+  int* ids = reinterpret_cast<int*>(smem + BYTES);                // [2][ROWS] row numbers, -1: none
+
+  cg::cluster_group cluster = cg::this_cluster();
+  const int share = blockIdx.x, shares = gridDim.x;
+  const bool up = (int)blockIdx.y >= P.tiles0;
+  const Side& S = P.side[up ? 1 : 0];
+  const int blk = (int)blockIdx.y - (up ? P.tiles0 : 0);
+  const int c0 = blk * COLS;
+  const int a = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool eight = S.v == nullptr;
+
+  // this share's part of the adapter's rows, in whole tiles
+  long long lo = min((long long)max(P.offsets[a], 0), P.T), hi = min((long long)max(P.offsets[a + 1], 0), P.T);
+  if (hi < lo) hi = lo;
+  const long long tiles = (hi - lo + ROWS - 1) / ROWS;
+  const long long tile0 = tiles * share / shares, tile1 = tiles * (share + 1) / shares;
+
+  // loads: 16 threads a row of 8 columns each, 16 rows a pass
+  const int vc = (tid & 15) * 8, vr = tid >> 4;
+  const bool vin = c0 + vc < S.width;
+  uint4 vreg[ROWS / 16];
+  constexpr int FQ = ROWS * RP / 4 / THREADS;                     // float4 of f a thread: MT
+  float4 freg[FQ];
+
+  auto row_id = [&](long long tile) -> int {                      // threads 0..63
+    const long long k = lo + tile * ROWS + tid;
+    if (tile >= tile1 || k >= hi) return -1;
+    const int t = P.order[k];
+    return (long long)t < P.T && t >= 0 ? t : -1;
+  };
+  auto load = [&](const int* id) {
+#pragma unroll
+    for (int q = 0; q < ROWS / 16; ++q) {
+      const int t = id[vr + 16 * q];
+      vreg[q] = make_uint4(0, 0, 0, 0);
+      if (t >= 0 && vin) {
+        if (eight) {
+          const uint2 c = __ldg(reinterpret_cast<const uint2*>(S.codes + (long long)t * S.width + c0 + vc));
+          vreg[q].x = c.x;
+          vreg[q].y = c.y;
+        } else {
+          vreg[q] = ldg_stream(S.v + (long long)t * S.ldv + c0 + vc);
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) {
+      const int i = tid + THREADS * q, row = i / (RP / 4), r4 = (i % (RP / 4)) * 4;
+      const int t = id[row];
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (t >= 0 && r4 < P.rank) {                                // rank is a multiple of 8
+        f = __ldg(reinterpret_cast<const float4*>(S.f + (long long)t * P.rank + r4));
+        if (eight) {
+          const float s = __ldg(S.scale + (long long)t * S.nb + blk);
+          f.x *= s;
+          f.y *= s;
+          f.z *= s;
+          f.w *= s;
+        }
+      }
+      freg[q] = f;
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int q = 0; q < ROWS / 16; ++q) {
+      uint4 o = vreg[q];
+      if (eight) {
+        const uint32_t c[2] = {vreg[q].x, vreg[q].y};
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t two = c[e >> 1] >> (16 * (e & 1));
+          w[e] = float2_to_bf16x2((float)(int8_t)two, (float)(int8_t)(two >> 8));
+        }
+        o = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      *reinterpret_cast<uint4*>(vt + (vr + 16 * q) * V_STRIDE + vc) = o;
+    }
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) {
+      const int i = tid + THREADS * q, row = i / (RP / 4), r4 = (i % (RP / 4)) * 4;
+      *reinterpret_cast<uint2*>(ft + row * F_STRIDE + r4) =
+          make_uint2(float2_to_bf16x2(freg[q].x, freg[q].y), float2_to_bf16x2(freg[q].z, freg[q].w));
+    }
+  };
+
+  float acc[MT][2][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[m][n][e] = 0.0f;
+
+  if (tile0 < tile1) {
+    if (tid < ROWS) ids[tid] = row_id(tile0);
+    __syncthreads();
+    load(ids);
+    int next_id = tid < ROWS ? row_id(tile0 + 1) : -1;
+    for (long long tile = tile0; tile < tile1; ++tile) {
+      const int par = (int)(tile - tile0) & 1;
+      put();
+      if (tid < ROWS) ids[(par ^ 1) * ROWS + tid] = next_id;
+      __syncthreads();
+      if (tile + 1 < tile1) {
+        load(ids + (par ^ 1) * ROWS);
+        next_id = tid < ROWS ? row_id(tile + 2) : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < ROWS; k += 16) {
+        uint32_t b[4];                                            // two tiles of 8 columns
+        ldmatrix_x4_trans(b, vt + (k + (lane & 15)) * V_STRIDE + warp * 16 + (lane >> 4) * 8);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          uint32_t f[4];
+          ldmatrix_x4_trans(f, ft + (k + (lane & 7) + (lane >> 4) * 8) * F_STRIDE + m * 16 + ((lane >> 3) & 1) * 8);
+          mma_bf16(acc[m][0], f, b[0], b[1]);
+          mma_bf16(acc[m][1], f, b[2], b[3]);
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  const int g = lane >> 2, q2 = (lane & 3) * 2;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int col = warp * 16 + n * 8 + q2;
+      *reinterpret_cast<float2*>(sums + (m * 16 + g) * COLS + col) = make_float2(acc[m][n][0], acc[m][n][1]);
+      *reinterpret_cast<float2*>(sums + (m * 16 + g + 8) * COLS + col) = make_float2(acc[m][n][2], acc[m][n][3]);
+    }
+  cluster.sync();
+  // rank `share` of the cluster adds up every shares-th pair of ranks: 16 threads a row of 8 columns each
+  for (int r = share * 16 + vr; r < P.rank; r += shares * 16) {
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = 0.0f;
+    for (int k = 0; k < shares; ++k) {
+      const float* o = cluster.map_shared_rank(sums, k) + r * COLS + vc;
+      const float4 x = *reinterpret_cast<const float4*>(o), y = *reinterpret_cast<const float4*>(o + 4);
+      s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+      s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+    }
+    if (vin) {
+      uint4 o;
+      o.x = float2_to_bf16x2(s[0], s[1]);
+      o.y = float2_to_bf16x2(s[2], s[3]);
+      o.z = float2_to_bf16x2(s[4], s[5]);
+      o.w = float2_to_bf16x2(s[6], s[7]);
+      *reinterpret_cast<uint4*>(S.grad + ((long long)a * P.rank + r) * S.width + c0 + vc) = o;
+    }
+  }
+  cluster.sync();                                                 // no CTA leaves while its sums are read
+}
+
+template <int MT>
+cudaError_t launch_mt(const GradParams& P, int shares, int tiles, int n, cudaStream_t stream) {
+  constexpr int RP = 16 * MT;
+  constexpr int TILE_BYTES = ROWS * (V_STRIDE + RP + 8) * 2, SUM_BYTES = RP * COLS * 4;
+  constexpr int BYTES = (TILE_BYTES > SUM_BYTES ? TILE_BYTES : SUM_BYTES) + 2 * ROWS * 4;
+  const cudaError_t e = ensure_dynamic_smem((const void*)adapter_grad_kernel<MT>, BYTES);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(shares, tiles, n);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = shares;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, adapter_grad_kernel<MT>, P);
+}
+
+}  // namespace
+
+cudaError_t launch_adapter_grad(const admmq_adapter_grad_args& a, cudaStream_t stream) {
+  GradParams P = {};
+  P.side[0] = {a.d_u, (const bf16*)a.d_x, a.ldx, (const int8_t*)a.d_x_codes, a.d_x_scale, (bf16*)a.d_grad_down, a.d_in,
+               (a.d_in + ADMMQ_CHECKPOINT_BLOCK - 1) / ADMMQ_CHECKPOINT_BLOCK};
+  P.side[1] = {a.d_h, (const bf16*)a.d_dy, a.lddy, nullptr, nullptr, (bf16*)a.d_grad_up, a.d_out, 0};
+  P.tiles0 = (a.d_in + COLS - 1) / COLS;
+  const int tiles = P.tiles0 + (a.d_out + COLS - 1) / COLS;
+  P.order = a.d_order;
+  P.offsets = a.d_offsets;
+  P.T = a.n_rows;
+  P.rank = a.rank;
+  // Shares of an adapter's rows: as many as leave each 128 rows if the rows are spread evenly over the adapters,
+  // at most the portable cluster size.
+  int shares = 1;
+  while (shares < 8 && a.n_rows / a.n_adapters >= 256LL * shares) shares *= 2;
+  if (a.rank <= 16) return launch_mt<1>(P, shares, tiles, a.n_adapters, stream);
+  if (a.rank <= 32) return launch_mt<2>(P, shares, tiles, a.n_adapters, stream);
+  if (a.rank <= 64) return launch_mt<4>(P, shares, tiles, a.n_adapters, stream);
+  return launch_mt<8>(P, shares, tiles, a.n_adapters, stream);
+}
+
+}  // namespace admmq

@@ -1,0 +1,569 @@
+"""GPU tests of the operators on quantized layers (adapt.py) against plain 64-bit formulas.
+
+Tolerances, element by element, from the arithmetic (EPS = 2^-8 is half a bf16 ulp, relative: 8 significant bits):
+ - an output rounded to bf16: EPS |result|;
+ - operands rounded to bf16 inside a sum (weights expanded for the tensor cores, h and u of an expansion, factors of the
+   adapters' gradients): independent errors of at most EPS |term| each, standard deviation at most EPS / sqrt(3) |term|,
+   so six standard deviations are 6 EPS / sqrt(3) sqrt(sum term^2);
+ - fp32 sums on the tensor cores, which may truncate: a step loses at most 2^-23 of the running sum, over at most 32 steps
+   between folds (small kernel) or with errors that add up at random otherwise: 2^-18 sum |term|.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -8
+SIX = 6.0 / math.sqrt(3.0)
+ACC = 2.0 ** -18
+DEV = "cuda:0"
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+def _layer(g, n, p, bits, group, sym=False):
+    gs = group or n
+    w = (_randn(g, p, n) * 0.02).view(p, n // gs, gs)
+    lo, hi = w.amin(-1), w.amax(-1)
+    if sym:
+        hi = torch.maximum(hi, -lo)
+        lo = -hi
+    top = 2 ** bits - 1
+    scale = (hi - lo) / top
+    codes = torch.round((w - lo[..., None]) / scale[..., None]).clamp_(0, top).to(torch.uint8).view(p, n)
+    return codes, scale.contiguous(), lo.contiguous()
+
+
+def _weight64(codes, scale, zero):
+    p, n = codes.shape
+    gs = n // scale.shape[1]
+    e = lambda t: t.double().repeat_interleave(gs, 1)  # noqa: E731
+    return e(zero) + e(scale) * codes.double()
+
+
+def _bank(g, na, r, n, p):
+    from paper_2605_11222_b200 import adapt
+    down = ((torch.rand(na, r, n, generator=g, device=DEV) * 2 - 1) / math.sqrt(n)).bfloat16()
+    up = (_randn(g, na, r, p) * 0.02).bfloat16()
+    return adapt.AdapterBank(down, up, torch.linspace(0.5, 2.0, na, device=DEV))
+
+
+def _rows64(plan):
+    a = plan.row_adapter.long()
+    return a, (a >= 0).double()
+
+
+def _shrink64(x, mat, bank, plan):
+    """(values, sum of |term|)."""
+    a, on = _rows64(plan)
+    s = bank.scale.double()[a.clamp(min=0)] * on
+    m = mat.double()[a.clamp(min=0)]
+    x = x.double()
+    return torch.einsum("ti,tri->tr", x, m) * s[:, None], torch.einsum("ti,tri->tr", x.abs(), m.abs()) * s[:, None]
+
+
+def _expand64(u, mat, plan):
+    """(values, sum of term^2)."""
+    a, on = _rows64(plan)
+    m = mat.double()[a.clamp(min=0)] * on[:, None, None]
+    return torch.einsum("tr,tri->ti", u.double(), m), torch.einsum("tr,tri->ti", u.double() ** 2, m ** 2)
+
+
+def _within(got, want, tol):
+    err = (got.double() - want).abs()
+    worst = (err / tol.clamp(min=1e-300)).max().item() if err.numel() else 0.0
+    assert worst <= 1.0, f"error is {worst:.3g} of the tolerance"
+
+
+
+def _plan(kind, T, na, seed=0):
+    from paper_2605_11222_b200 import adapt
+    g = torch.Generator().manual_seed(seed)
+    if kind == "one":
+        lengths, ids = [T], [na - 1]
+    elif kind == "none":
+        lengths, ids = [T], [-1]
+    elif kind == "each":                         # a row a request, an adapter of its own as far as they go
+        lengths, ids = [1] * T, [(5 * i) % (na + 1) - 1 for i in range(T)]
+    else:                                        # ragged, some empty, some without an adapter
+        cuts = torch.randint(0, T + 1, (5,), generator=g).sort().values.tolist()
+        cuts = [0] + cuts[:3] + [cuts[2]] + cuts[3:] + [T]
+        lengths = [b - a for a, b in zip(cuts, cuts[1:])]
+        ids = torch.randint(-1, na, (len(lengths),), generator=g).tolist()
+    return adapt.RequestPlan(lengths, ids, na)
+
+
+# (rows, d_in, d_out, bits, group, symmetric, adapters, rank, plan)
+LINEAR = [
+    (1, 64, 8, 4, 64, False, 1, 8, "one"),
+    (1, 4096, 1024, 4, 128, False, 3, 16, "one"),
+    (2, 72, 40, 2, 0, True, 2, 8, "each"),
+    (7, 512, 264, 3, 128, False, 4, 24, "each"),
+    (8, 1000, 136, 4, 0, False, 5, 32, "mixed"),
+    (9, 4096, 1024, 2, 0, True, 16, 8, "each"),
+    (16, 576, 1000, 4, 64, False, 3, 128, "mixed"),
+    (17, 576, 1000, 4, 64, False, 3, 128, "mixed"),
+    (33, 8, 8, 4, 0, False, 2, 8, "mixed"),
+    (64, 256, 384, 3, 128, True, 6, 16, "each"),
+    (65, 1024, 128, 4, 256, False, 2, 48, "mixed"),
+    (128, 200, 136, 2, 0, False, 40, 8, "each"),
+    (129, 4096, 520, 4, 128, False, 4, 64, "mixed"),
+    (300, 1344, 1096, 3, 64, False, 70, 8, "each"),
+    (520, 768, 2056, 4, 128, True, 3, 72, "none"),
+    (1030, 2048, 392, 4, 0, False, 3, 16, "mixed"),
+]
+
+
+@pytest.mark.parametrize("T,n,p,bits,group,sym,na,r,kind", LINEAR)
+def test_forward_matches_the_formula(T, n, p, bits, group, sym, na, r, kind):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + n)
+    codes, scale, zero = _layer(g, n, p, bits, group, sym)
+    layer = adapt.QuantLinear(codes, scale, zero, bits, group)
+    bank, plan = _bank(g, na, r, n, p), _plan(kind, T, na, T)
+    x = _randn(g, T, n)
+    x[:, :: 97] *= 30.0                          # outlier channels
+    x = x.bfloat16()
+    y, h = layer.forward(x, bank, plan)
+    adapt.check_device_status(DEV)
+    W = _weight64(codes, scale, zero)
+    want_h, abs_h = _shrink64(x, bank.down, bank, plan)
+    _within(h, want_h, ACC * abs_h + 1e-30)
+    base = x.double() @ W.T
+    delta, sq_delta = _expand64(want_h, bank.up, plan)
+    want = base + delta
+    sq = x.double() ** 2 @ (W ** 2).T + sq_delta
+    top = scale.double().amax(1) * 143 + zero.double().abs().amax(1)      # 128 + k steps of the grid, and its origin
+    acc = ACC * (x.double().abs().sum(1)[:, None] * top[None] + sq_delta.sqrt() * math.sqrt(r))
+    rounding = torch.zeros_like(want) if T <= 16 else SIX * EPS * sq.sqrt()
+    _within(y, want, EPS * want.abs() + acc + rounding + 1e-30)
+    # without adapters
+    y0, h0 = layer.forward(x)
+    assert h0 is None
+    _within(y0, base, EPS * base.abs() + acc + rounding + 1e-30)
+
+
+@pytest.mark.parametrize("T,n,p,bits,group,sym,na,r,kind", LINEAR)
+def test_grad_input_matches_the_formula(T, n, p, bits, group, sym, na, r, kind):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + p)
+    codes, scale, zero = _layer(g, n, p, bits, group, sym)
+    layer = adapt.QuantLinear(codes, scale, zero, bits, group)
+    bank, plan = _bank(g, na, r, n, p), _plan(kind, T, na, T)
+    dy = (_randn(g, T, p) * 1e-3).bfloat16()
+    dx, u = layer.grad_input(dy, bank, plan)
+    adapt.check_device_status(DEV)
+    W = _weight64(codes, scale, zero)
+    want_u, abs_u = _shrink64(dy, bank.up, bank, plan)
+    _within(u, want_u, ACC * abs_u + 1e-30)
+    base = dy.double() @ W
+    delta, sq_delta = _expand64(want_u, bank.down, plan)
+    want = base + delta
+    sq = dy.double() ** 2 @ W ** 2 + sq_delta
+    acc = ACC * (dy.double().abs() @ W.abs() + sq_delta.sqrt() * math.sqrt(r))
+    _within(dx, want, EPS * want.abs() + SIX * EPS * sq.sqrt() + acc + 1e-30)
+    dx0, _ = layer.grad_input(dy)
+    _within(dx0, base, EPS * base.abs() + SIX * EPS * sq.sqrt() + acc + 1e-30)
+
+
+# (rows, d_in, d_out, adapters, rank, plan, checkpoint)
+GRADS = [
+    (0, 64, 64, 2, 8, "none", True), (1, 136, 8, 1, 8, "one", True), (5, 128, 264, 3, 16, "mixed", False),
+    (63, 1000, 128, 2, 24, "mixed", True), (64, 256, 384, 4, 32, "each", True), (65, 256, 384, 70, 8, "each", False),
+    (333, 4096, 1024, 3, 64, "mixed", True), (1500, 392, 520, 1, 128, "one", True), (4100, 264, 200, 2, 16, "mixed", False),
+    (200, 72, 136, 2, 48, "none", True),
+]
+
+
+@pytest.mark.parametrize("T,n,p,na,r,kind,eight", GRADS)
+def test_adapter_grads_match_the_formula(T, n, p, na, r, kind, eight):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T * 3 + n)
+    bank, plan = _bank(g, na, r, n, p), _plan(kind, T, na, T)
+    x = _randn(g, T, n).bfloat16()
+    dy = (_randn(g, T, p) * 1e-3).bfloat16()
+    h, u = _randn(g, T, r), _randn(g, T, r) * 1e-3
+    v = x
+    x64 = x.double()
+    if eight:
+        v = adapt.Checkpoint.save(x)
+        x64 = v.codes.double() * v.scale.double().repeat_interleave(128, 1)[:, :n]
+    d_down, d_up = adapt.adapter_grads(bank, plan, v, h, dy, u)
+    for a in range(na):
+        t = (plan.row_adapter == a).nonzero()[:, 0]
+        for got, f, w in ((d_down[a], u, x64), (d_up[a], h, dy.double())):
+            want = f[t].double().T @ w[t]
+            sq, ab = (f[t].double() ** 2).T @ w[t] ** 2, f[t].double().abs().T @ w[t].abs()
+            _within(got, want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * ab + 1e-30)
+
+
+def test_adapter_grads_are_the_same_bits_every_time():
+    from paper_2605_11222_b200 import adapt
+    g = _gen(9)
+    bank, plan = _bank(g, 2, 16, 512, 256), _plan("mixed", 3000, 2, 4)
+    x, dy = _randn(g, 3000, 512).bfloat16(), _randn(g, 3000, 256).bfloat16()
+    h, u = _randn(g, 3000, 16), _randn(g, 3000, 16)
+    first = adapt.adapter_grads(bank, plan, x, h, dy, u)
+    for _ in range(3):
+        again = adapt.adapter_grads(bank, plan, x, h, dy, u)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("T", [11, 150])
+def test_gradients_agree_with_differences(T):
+    """The output is linear in x and in each adapter matrix, so a difference over any step is the derivative; what is left
+    is the rounding of the outputs to bf16, EPS |y| each with independent signs."""
+    from paper_2605_11222_b200 import adapt
+    n, p, na, r = 512, 384, 2, 16
+    g = _gen(T)
+    codes, scale, zero = _layer(g, n, p, 4, 128)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 128), _bank(g, na, r, n, p), _plan("mixed", T, na, 3)
+    x, dy = _randn(g, T, n).bfloat16(), _randn(g, T, p).bfloat16()
+    y, h = layer.forward(x, bank, plan)
+    dx, u = layer.grad_input(dy, bank, plan)
+    d_down, d_up = adapt.adapter_grads(bank, plan, x, h, dy, u)
+
+    def loss(x, down, up):
+        out, _ = layer.forward(x, adapt.AdapterBank(down, up, bank.scale), plan)
+        return out.double()
+
+    for name, grad, value in (("x", dx, x), ("down", d_down, bank.down), ("up", d_up, bank.up)):
+        step = _randn(g, *value.shape).bfloat16() if name == "x" else (value * 4).bfloat16()
+        at = {"x": x, "down": bank.down, "up": bank.up}
+        hi, lo = dict(at), dict(at)
+        hi[name], lo[name] = (value + step).bfloat16(), (value - step).bfloat16()
+        moved = hi[name].double() - lo[name].double()              # what the step is after rounding
+        yh, yl = loss(**hi), loss(**lo)
+        got = ((yh - yl) * dy.double()).sum()
+        want = (grad.double() * moved).sum()
+        # roundings: both outputs (and their weights), and the gradient's own entries
+        noise = 2 * SIX * EPS * (((yh.abs() + yl.abs() + 1) * dy.double()) ** 2).sum().sqrt() \
+            + 2 * SIX * EPS * ((grad.double() * moved) ** 2).sum().sqrt()
+        assert abs(got - want) <= noise, (name, float(got), float(want), float(noise))
+
+
+def test_strided_rows_outputs_and_another_stream():
+    from paper_2605_11222_b200 import adapt
+    g = _gen(5)
+    n, p, T = 256, 136, 37
+    codes, scale, zero = _layer(g, n, p, 3, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 3, 64), _bank(g, 2, 8, n, p), _plan("mixed", T, 2, 1)
+    big = _randn(g, T, n + 24).bfloat16()
+    x = big[:, 16: 16 + n]
+    out = torch.full((T, p + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    y, h = layer.forward(x, bank, plan)
+    layer.forward(x, bank, plan, out=out[:, :p])
+    assert torch.equal(out[:, :p], y) and bool((out[:, p:] == 7).all())
+    dx = torch.full((T, n + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    ref, _ = layer.grad_input(y, bank, plan)
+    layer.grad_input(out[:, :p], bank, plan, out=dx[:, :n])
+    assert torch.equal(dx[:, :n], ref) and bool((dx[:, n:] == 7).all())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        y2, h2 = layer.forward(x, bank, plan)
+    s.synchronize()
+    assert torch.equal(y, y2) and torch.equal(h, h2)
+
+
+@pytest.mark.parametrize("T", [5, 40])
+def test_forward_in_a_cuda_graph(T):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(6)
+    n, p = 512, 256
+    codes, scale, zero = _layer(g, n, p, 4, 128)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 128), _bank(g, 3, 16, n, p), _plan("each", T, 3)
+    x = _randn(g, T, n).bfloat16()
+    y, h = torch.empty(T, p, dtype=torch.bfloat16, device=DEV), torch.empty(T, 16, device=DEV)
+    layer.forward(x, bank, plan, out=y, h=h)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, bank, plan, out=y, h=h)
+    x.copy_(_randn(g, T, n))
+    graph.replay()
+    want, _ = layer.forward(x, bank, plan)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("T", [6, 50])
+def test_a_bad_row_stays_in_its_row(T):
+    """A NaN or infinity in one row's input does not reach another row, whatever adapters they have."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(8)
+    n, p = 256, 128
+    codes, scale, zero = _layer(g, n, p, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, 3, 8, n, p), _plan("each", T, 3)
+    x = _randn(g, T, n).bfloat16()
+    want, _ = layer.forward(x, bank, plan)
+    bad = x.clone()
+    bad[1, 3], bad[4, 9] = float("nan"), float("inf")
+    got, _ = layer.forward(bad, bank, plan)
+    keep = [t for t in range(T) if t not in (1, 4)]
+    assert torch.equal(got[keep], want[keep])
+    assert not torch.isfinite(got[1].float()).any() and not torch.isfinite(got[4].float()).any()
+
+
+def test_a_bank_with_a_non_finite_entry_is_refused():
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(10)
+    bank = _bank(g, 2, 8, 64, 64)
+    for t, bad in ((bank.down, float("inf")), (bank.up, float("nan"))):
+        keep = t[1, 7, 63].clone()
+        t[1, 7, 63] = bad
+        with pytest.raises(adapt.AdmmqError) as e:
+            bank.check()
+        assert e.value.status == B.ERR_NONFINITE
+        t[1, 7, 63] = keep
+        bank.check()
+
+
+def test_codes_beyond_the_bits_are_refused():
+    from paper_2605_11222_b200 import adapt, binding as B
+    codes, scale, zero = _layer(_gen(1), 64, 8, 3, 0)
+    codes[5, 60] = 8
+    with pytest.raises(adapt.AdmmqError) as e:
+        adapt.QuantLinear(codes, scale, zero, 3)
+    assert e.value.status == B.ERR_INVALID_ARG
+    adapt.QuantLinear(codes, scale, zero, 4)
+
+
+def test_refusals():
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(2)
+    codes, scale, zero = _layer(g, 128, 64, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, 2, 8, 128, 64), _plan("mixed", 9, 2)
+    x = _randn(g, 9, 128).bfloat16()
+
+    def refused(status, f, *a, **k):
+        with pytest.raises(adapt.AdmmqError) as e:
+            f(*a, **k)
+        assert e.value.status == status
+
+    refused(B.ERR_UNSUPPORTED, adapt.QuantLinear, codes, scale, zero, 5, 64)
+    refused(B.ERR_SHAPE, adapt.QuantLinear, codes, scale, zero, 1, 64)
+    refused(B.ERR_SHAPE, adapt.QuantLinear, codes, scale, zero, 4, 32)          # 4 groups: wrong count of scales
+    c2, s2, z2 = _layer(g, 128, 64, 4, 32)
+    refused(B.ERR_SHAPE, adapt.QuantLinear, c2, s2, z2, 4, 32)                   # a group of 32
+    refused(B.ERR_INVALID_ARG, adapt.QuantLinear, codes.int(), scale, zero, 4, 64)
+    refused(B.ERR_INVALID_ARG, layer.forward, x.float(), bank, plan)
+    refused(B.ERR_SHAPE, layer.forward, x[:, :120], bank, plan)
+    refused(B.ERR_SHAPE, layer.forward, x[:8], bank, plan)                       # another number of rows
+    refused(B.ERR_SHAPE, layer.forward, x, bank)                                 # a bank without a plan
+    odd = torch.empty(9, 132, dtype=torch.bfloat16, device=DEV)
+    refused(B.ERR_SHAPE, layer.forward, odd[:, :128])                            # rows of 264 bytes
+    refused(B.ERR_INVALID_ARG, layer.forward, torch.empty(9 * 136, dtype=torch.bfloat16, device=DEV)[1:1 + 8 * 136 + 128]
+            .as_strided((9, 128), (136, 1)))                                     # not on a 16-byte boundary
+    refused(B.ERR_SHAPE, adapt.RequestPlan, [1, -1], [0, 0], 2)
+    refused(B.ERR_INVALID_ARG, adapt.RequestPlan, [1], [2], 2)
+    h = torch.zeros(9, 8, device=DEV)
+    y = torch.zeros(9, 64, dtype=torch.bfloat16, device=DEV)
+    refused(B.ERR_SHAPE, adapt.adapter_grads, bank, plan, x, h[:8], y, h)
+    refused(B.ERR_SHAPE, adapt.Checkpoint.save, torch.zeros(3, 12, device=DEV))
+    refused(B.ERR_INVALID_ARG, adapt.Checkpoint.save, torch.zeros(3, 16, device=DEV).half())
+    adapt.check_device_status(DEV)
+    e = layer.forward(x[:0])[0]
+    assert e.shape == (0, 64)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    """The producer withholds its loads, so the first wait of every CTA expires with nothing in flight."""
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(3)
+    codes, scale, zero = _layer(g, 512, 256, 4, 128)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 128), _bank(g, 2, 8, 512, 256), _plan("mixed", 70, 2)
+    x = _randn(g, 70, 512).bfloat16()
+    want, _ = layer.forward(x, bank, plan)
+    lib = adapt._library()
+    assert lib.admmq_test_linear_set_wait(10, 0) == B.ERR_INVALID_ARG
+    assert lib.admmq_test_linear_set_wait(200000, 1) == B.OK
+    try:
+        layer.forward(x, bank, plan)
+        with pytest.raises(adapt.AdmmqError) as e:
+            adapt.check_device_status(DEV)
+        assert e.value.status == B.ERR_TIMEOUT
+    finally:
+        assert lib.admmq_test_linear_set_wait(2_000_000_000, 0) == B.OK
+    got, _ = layer.forward(x, bank, plan)
+    adapt.check_device_status(DEV)
+    assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------ checkpoints
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,n", [(0, 64), (1, 8), (3, 128), (5, 136), (77, 4096), (200, 1000), (2, 12288)])
+def test_checkpoint_codes_scales_and_values(T, n, dtype):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + n)
+    big = _randn(g, T, n + 8) * 3
+    if T > 1:
+        big[0] = 0.0                              # a row of zeros
+        big[1, ::3] *= 1e4
+    x = big.to(dtype)[:, 8:]
+    c = adapt.Checkpoint.save(x)
+    nb = -(-n // 128)
+    f = torch.zeros(T, nb * 128, device=DEV)
+    f[:, :n] = x.float()
+    f = f.view(T, nb, 128)
+    scale = f.abs().amax(-1) / torch.full((), 127.0, device=DEV)
+    codes = torch.where(scale[..., None] > 0, torch.round(f / scale[..., None]), torch.zeros_like(f))
+    assert torch.equal(c.scale, scale)
+    assert torch.equal(c.codes.float(), codes.view(T, nb * 128)[:, :n])
+    want = (c.codes.float() * scale.repeat_interleave(128, 1)[:, :n]).to(dtype)
+    assert torch.equal(c.restore(dtype), want)
+    wide = torch.full((T, n + 8), 5.0, dtype=dtype, device=DEV)
+    c.restore(dtype, out=wide[:, :n])
+    assert torch.equal(wide[:, :n], want) and bool((wide[:, n:] == 5).all())
+    # within half a step of what was kept
+    assert bool(((c.restore(torch.float32) - x.float()).abs()
+                 <= 0.5001 * scale.repeat_interleave(128, 1)[:, :n]).all())
+
+
+def test_checkpoint_of_extreme_values():
+    from paper_2605_11222_b200 import adapt
+    x = torch.zeros(4, 256)
+    x[0, 0], x[0, 1] = 3e38, -1.0
+    x[1, 0], x[1, 1] = 1e-44, -1e-45              # subnormal: the scale is one of a few bits, or zero
+    x[2, 5], x[2, 130] = float("nan"), 2.0
+    x[3, 5], x[3, 130] = float("-inf"), 2.0
+    r = adapt.Checkpoint.save(x.to(DEV)).restore(torch.float32).cpu()
+    assert abs(r[0, 0] / 3e38 - 1) < 1e-6 and r[0, 1] == 0
+    assert torch.isfinite(r[1]).all() and (r[1].abs() <= 1e-43).all()
+    for t in (2, 3):
+        assert torch.isnan(r[t, :128]).all()      # the block, and only it
+        assert r[t, 130] == 2 and (r[t, 131:] == 0).all()
+
+
+# ------------------------------------------------------------------ norm and rotation
+def _qk64(x, w, cos, sin, rot, eps):
+    n = x / (x.square().mean(-1, keepdim=True) + eps).sqrt()
+    z = n * w
+    a, b, rest = z[..., : rot // 2], z[..., rot // 2: rot], z[..., rot:]
+    y = torch.cat([a * cos - b * sin, b * cos + a * sin, rest], -1)
+    mag = torch.cat([a.abs() + b.abs(), a.abs() + b.abs(), rest.abs()], -1)
+    return y, mag
+
+
+QK = [(0, 4, 2, 64, 64), (1, 32, 8, 128, 128), (2, 1, 1, 16, 16), (3, 5, 0, 96, 32), (17, 12, 3, 64, 32), (33, 7, 7, 256, 256),
+      (259, 3, 1, 80, 80), (1000, 6, 2, 128, 96), (5000, 4, 2, 48, 48), (9, 40, 33, 32, 16)]
+
+
+def _qk_inputs(T, hq, hk, d, rot, dtype, g):
+    big = (_randn(g, T, (hq + 2 * hk) * d + 16) * 2).to(dtype)
+    q = big[:, : hq * d].view(T, hq, d) if T else torch.empty(0, hq, d, dtype=dtype, device=DEV)
+    k = big[:, hq * d: (hq + hk) * d].view(T, hk, d) if T else torch.empty(0, hk, d, dtype=dtype, device=DEV)
+    wq, wk = [(1 + 0.3 * _randn(g, d)).to(dtype) for _ in range(2)]
+    ang = torch.arange(700, device=DEV)[:, None] * 1e4 ** (-torch.arange(0, rot, 2, device=DEV, dtype=torch.float64) / rot)
+    pos = torch.randint(0, 700, (T,), generator=g, device=DEV, dtype=torch.int32)
+    return q, k, wq, wk, ang.cos().float(), ang.sin().float(), pos
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,hq,hk,d,rot", QK)
+def test_qk_norm_rope(T, hq, hk, d, rot, dtype):
+    """fp32: the mean of squares over at most 256 values, its root, two products and the rotation, each a few half ulps:
+    32 of them in all, of the magnitudes that enter the rotation; bf16 adds the output's rounding."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + d)
+    q, k, wq, wk, cos, sin, pos = _qk_inputs(T, hq, hk, d, rot, dtype, g)
+    yq, yk = adapt.qk_norm_rope(q, k, wq, wk, cos, sin, pos, 1e-6)
+    adapt.check_device_status(DEV)
+    c, s = cos.double()[pos.long()][:, None], sin.double()[pos.long()][:, None]
+    half = EPS if dtype == torch.bfloat16 else 0.0
+    for got, x, w in ((yq, q, wq), (yk, k, wk)):
+        want, mag = _qk64(x.double(), w.double(), c, s, rot, 1e-6)
+        _within(got, want, half * want.abs() + 32 * 2.0 ** -24 * mag + 1e-30)
+    # in place
+    q2, k2 = q.clone(), k.clone()
+    adapt.qk_norm_rope(q2, k2, wq, wk, cos, sin, pos, 1e-6, out_q=q2, out_k=k2)
+    assert torch.equal(q2, yq) and torch.equal(k2, yk)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,hq,hk,d,rot", QK)
+def test_qk_norm_rope_backward(T, hq, hk, d, rot, dtype):
+    """As forward, with r |dn| and r |n| mean |dn n| as the magnitudes that enter the last difference; weights: the
+    sum's terms each with the same error, and the fp32 sum's own (64 half ulps of the sum of magnitudes)."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + d + 1)
+    q, k, wq, wk, cos, sin, pos = _qk_inputs(T, hq, hk, d, rot, dtype, g)
+    dyq, dyk = _randn(g, T, hq, d).to(dtype), _randn(g, T, hk, d).to(dtype)
+    got = adapt.qk_norm_rope_backward(q, k, wq, wk, cos, sin, pos, dyq, dyk, 1e-6)
+    adapt.check_device_status(DEV)
+    c, s = cos.double()[pos.long()][:, None], sin.double()[pos.long()][:, None]
+    half = EPS if dtype == torch.bfloat16 else 0.0
+    h = rot // 2
+    for gx, gw, x, w, dy in ((got[0], got[2], q, wq, dyq), (got[1], got[3], k, wk, dyk)):
+        x, w, dy = x.double(), w.double(), dy.double()
+        r = 1 / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()
+        n = x * r
+        a, b = dy[..., :h], dy[..., h:rot]
+        gr = torch.cat([a * c + b * s, b * c - a * s, dy[..., rot:]], -1)
+        ga = torch.cat([a.abs() + b.abs(), a.abs() + b.abs(), dy[..., rot:].abs()], -1)
+        dn = gr * w
+        want = r * (dn - n * (dn * n).mean(-1, keepdim=True))
+        mag = r * (ga * w.abs() + n.abs() * (ga * w.abs() * n.abs()).mean(-1, keepdim=True))
+        _within(gx, want, half * want.abs() + 64 * 2.0 ** -24 * mag + 1e-30)
+        ww = (gr * n).sum((0, 1))
+        _within(gw, ww, half * ww.abs() + 64 * 2.0 ** -24 * (ga * n.abs()).sum((0, 1)) + 1e-30)
+
+
+def test_qk_gradient_agrees_with_differences():
+    """Central differences of the fp32 forward call: error of order step^2 third derivatives plus the forward's
+    rounding over the step; both are below 1e-3 of the gradient's scale at the step used."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(4)
+    T, hq, hk, d, rot = 6, 3, 2, 64, 32
+    q, k, wq, wk, cos, sin, pos = [t.contiguous() for t in _qk_inputs(T, hq, hk, d, rot, torch.float32, g)]
+    cq, ck = _randn(g, T, hq, d), _randn(g, T, hk, d)
+    grads = adapt.qk_norm_rope_backward(q, k, wq, wk, cos, sin, pos, cq, ck, 1e-6)
+
+    def loss(v):
+        a, b = adapt.qk_norm_rope(*v, cos, sin, pos, 1e-6)
+        return float((a.double() * cq.double()).sum() + (b.double() * ck.double()).sum())
+
+    for i in range(4):
+        v = [q, k, wq, wk]
+        step = _randn(g, *v[i].shape)
+        e = 2e-3
+        hi, lo = list(v), list(v)
+        hi[i], lo[i] = v[i] + e * step, v[i] - e * step
+        got = (loss(hi) - loss(lo)) / (2 * e)
+        want = float((grads[i].double() * step.double()).sum())
+        size = float((grads[i].double() * step.double()).square().sum().sqrt()) + 1.0
+        assert abs(got - want) <= 1e-2 * size, (i, got, want)
+
+
+def test_qk_refusals_and_positions_out_of_range():
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(7)
+    q, k, wq, wk, cos, sin, pos = _qk_inputs(4, 2, 1, 64, 64, torch.float32, g)
+
+    def refused(status, *a, **kw):
+        with pytest.raises(adapt.AdmmqError) as e:
+            adapt.qk_norm_rope(*a, **kw)
+        assert e.value.status == status
+
+    refused(B.ERR_INVALID_ARG, q.half(), k.half(), wq, wk, cos, sin, pos)
+    refused(B.ERR_INVALID_ARG, q, k, wq.bfloat16(), wk, cos, sin, pos)
+    refused(B.ERR_SHAPE, q, k, wq, wk, cos[:, :12].contiguous(), sin[:, :12].contiguous(), pos)
+    refused(B.ERR_INVALID_ARG, q, k, wq, wk, cos, sin, pos.long())
+    refused(B.ERR_SHAPE, q[..., :40], k[..., :40], wq[:40], wk[:40], cos[:, :16].contiguous(), sin[:, :16].contiguous(), pos)
+    refused(B.ERR_INVALID_ARG, q, k, wq, wk, cos, sin, pos, -1.0)
+    pos[2] = 700
+    adapt.qk_norm_rope(q, k, wq, wk, cos, sin, pos)
+    with pytest.raises(adapt.AdmmqError) as e:
+        adapt.check_device_status(DEV)
+    assert e.value.status == B.ERR_SHAPE
+    adapt.check_device_status(DEV)

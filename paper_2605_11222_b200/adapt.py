@@ -15,8 +15,8 @@ a status word, which `check_device_status` reads (it synchronises) and clears.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import struct
 from typing import Optional, Sequence, Union
 
 import numpy as np
@@ -38,26 +38,12 @@ class Adapters(C.Structure):
                 ("d_up", C.c_void_p), ("d_scale", C.c_void_p)]
 
 
-class AdapterGradArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_size_t), ("d_in", C.c_int), ("d_out", C.c_int), ("n_adapters", C.c_int),
-                ("rank", C.c_int), ("n_rows", C.c_longlong), ("d_order", C.c_void_p), ("d_offsets", C.c_void_p),
-                ("d_h", C.c_void_p), ("d_u", C.c_void_p), ("d_x", C.c_void_p), ("ldx", C.c_longlong),
-                ("d_x_codes", C.c_void_p), ("d_x_scale", C.c_void_p), ("d_dy", C.c_void_p), ("lddy", C.c_longlong),
-                ("d_grad_down", C.c_void_p), ("d_grad_up", C.c_void_p)]
-
-
-class QkArgs(C.Structure):
-    _fields_ = [("struct_size", C.c_size_t), ("dtype", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int),
-                ("head_dim", C.c_int), ("rot_dim", C.c_int), ("n_rows", C.c_longlong), ("eps", C.c_double),
-                ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("q_row", C.c_longlong), ("q_head", C.c_longlong),
-                ("k_row", C.c_longlong), ("k_head", C.c_longlong), ("d_wq", C.c_void_p), ("d_wk", C.c_void_p),
-                ("d_cos", C.c_void_p), ("d_sin", C.c_void_p), ("n_positions", C.c_longlong), ("d_pos", C.c_void_p),
-                ("d_out_q", C.c_void_p), ("d_out_k", C.c_void_p), ("out_q_row", C.c_longlong),
-                ("out_q_head", C.c_longlong), ("out_k_row", C.c_longlong), ("out_k_head", C.c_longlong),
-                ("d_dy_q", C.c_void_p), ("d_dy_k", C.c_void_p), ("dy_q_row", C.c_longlong),
-                ("dy_q_head", C.c_longlong), ("dy_k_row", C.c_longlong), ("dy_k_head", C.c_longlong),
-                ("d_grad_wq", C.c_void_p), ("d_grad_wk", C.c_void_p), ("d_workspace", C.c_void_p),
-                ("workspace_bytes", C.c_size_t), ("d_status", C.c_void_p)]
+# The two larger argument structs are packed by format in one step, in native layout: filling a ctypes structure field by
+# field takes longer than the launch that it describes.
+_GRAD_ARGS = struct.Struct("@N4iq5Pq3Pq2P")       # admmq_adapter_grad_args
+_GRAD_ARGS_BYTES = _GRAD_ARGS.size
+_QK_ARGS = struct.Struct("@N5iqd2P4q4PqP2P4q2P4q3PNP")   # admmq_qk_args
+_QK_ARGS_BYTES = _QK_ARGS.size
 
 
 _lib = None
@@ -92,57 +78,67 @@ def _need(ok: bool, what: str, status: int = B.ERR_INVALID_ARG):
         raise AdmmqError(status, what)
 
 
-def _check(st: int, where: str):
-    if st != B.OK:
+def _call(fn, where: str, index: int, *args):
+    """fn(*args, stream) with device `index` current, as the library asks, on that device's current stream."""
+    if _current_device() == index:
+        st = fn(*args, _current_stream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, _current_stream(index))
+    if st != 0:
         raise AdmmqError(st, where)
 
 
-def _on(device: torch.device):
-    """The device made current for a call, as the library asks (a no-op when it is)."""
-    if device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
-
-
-def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+# The device and the stream as plain integers: these are on the path of every decoded token.
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 _status_words: dict = {}
 
 
-def _status(device: torch.device) -> int:
-    """Pointer of the device's status word, made (zeroed) at its first use."""
-    w = _status_words.get(device)
+def _status(index: int) -> int:
+    """Pointer of a device's status word, made (zeroed) at its first use."""
+    w = _status_words.get(index)
     if w is None:
-        w = torch.zeros(4, dtype=torch.int32, device=device)
-        torch.cuda.synchronize(device)
-        w = _status_words[device] = (w, w.data_ptr())
-    return w[1]
+        word = torch.zeros(4, dtype=torch.int32, device=f"cuda:{index}")
+        torch.cuda.synchronize(index)
+        w = _status_words[index] = (word.data_ptr(), word)
+    return w[0]
 
 
 def check_device_status(device: Union[str, torch.device] = "cuda:0", where: str = "device status"):
     """Waits for the device, raises AdmmqError for the first error that a call of this module met on it, and clears it."""
     device = torch.device(device)
-    _status(device)
-    word = _status_words[device][0]
-    torch.cuda.synchronize(device)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    _status(index)
+    word = _status_words[index][1]
+    torch.cuda.synchronize(index)
     st = int(word[0].item())
     if st != B.OK:
         word.zero_()
-        torch.cuda.synchronize(device)
+        torch.cuda.synchronize(index)
         raise AdmmqError(st, where)
 
 
-def _rows(t: torch.Tensor, width: int, device: torch.device, name: str):
-    _need(t.dim() == 2 and t.dtype == torch.bfloat16 and t.device == device,
-          f"{name}: a [rows, {width}] bf16 tensor on {device}")
-    _need(t.shape[1] == width and (t.shape[0] == 0 or t.stride(1) == 1), f"{name}: rows of {width} adjacent values",
-          B.ERR_SHAPE)
+def _fail(status: int, what: str):
+    raise AdmmqError(status, what)
+
+
+def _rows(t: torch.Tensor, width: int, index: int, name: str) -> int:
+    """Checks a [rows, width] bf16 tensor on device `index`, returns its row stride.  (The stride of a single row does
+    not matter, and torch may give it any value.)"""
+    if t.dim() != 2 or t.dtype is not torch.bfloat16 or t.get_device() != index:
+        _fail(B.ERR_INVALID_ARG, f"{name}: a [rows, {width}] bf16 tensor on cuda:{index}")
+    rows, w = t.shape
+    ld, inner = t.stride()
+    if w != width or (rows > 0 and inner != 1):
+        _fail(B.ERR_SHAPE, f"{name}: rows of {width} adjacent values")
+    return ld if rows > 1 else w
 
 
 def _ld(t: torch.Tensor) -> int:
-    """Row stride in elements; that of a single row does not matter, and torch may give it any value."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -161,6 +157,7 @@ class AdapterBank:
               and up.device == scale.device == down.device, "AdapterBank: bf16 down and up, fp32 scale, one device")
         _need(down.is_contiguous() and up.is_contiguous() and scale.is_contiguous(), "AdapterBank: contiguous tensors")
         self.down, self.up, self.scale, self.device = down, up, scale, down.device
+        self.index = down.get_device()
         self.n_adapters, self.rank, self.d_in = down.shape
         self.d_out = up.shape[2]
         self._c = Adapters(C.sizeof(Adapters), self.n_adapters, self.rank, down.data_ptr(), up.data_ptr(),
@@ -170,9 +167,8 @@ class AdapterBank:
             self.check()
 
     def check(self):
-        with _on(self.device):
-            _check(_library().admmq_adapters_check(self._ref, self.d_in, self.d_out, _status(self.device),
-                                                   _stream(self.device)), "admmq_adapters_check")
+        _call(_library().admmq_adapters_check, "admmq_adapters_check", self.index, self._ref, self.d_in, self.d_out,
+              _status(self.index))
         check_device_status(self.device, "admmq_adapters_check")
 
 
@@ -192,6 +188,7 @@ class RequestPlan:
         if device.type == "cuda" and device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
         self.n_rows, self.n_adapters, self.device = int(lengths.sum()), n_adapters, device
+        self.index = device.index
         _need(self.n_rows < 2 ** 30, "RequestPlan: too many rows", B.ERR_SHAPE)
         rows = np.repeat(adapters, lengths)
         order = np.argsort(rows, kind="stable")
@@ -231,30 +228,34 @@ class Checkpoint:
 
     @classmethod
     def save(cls, x: torch.Tensor) -> "Checkpoint":
-        _need(x.dim() == 2 and x.is_cuda and x.dtype in (torch.float32, torch.bfloat16),
-              "Checkpoint.save: [rows, width] fp32 or bf16 on a GPU")
+        bf16 = x.dtype is torch.bfloat16
+        if x.dim() != 2 or not x.is_cuda or not (bf16 or x.dtype is torch.float32):
+            _fail(B.ERR_INVALID_ARG, "Checkpoint.save: [rows, width] fp32 or bf16 on a GPU")
         t, n = x.shape
-        _need(t == 0 or x.stride(1) == 1, "Checkpoint.save: adjacent values", B.ERR_SHAPE)
-        codes = torch.empty(t, n, dtype=torch.int8, device=x.device)
-        scale = torch.empty(t, -(-n // BLOCK), dtype=torch.float32, device=x.device)
-        with _on(x.device):
-            _check(_library().admmq_checkpoint_save(x.data_ptr(), B.BF16 if x.dtype == torch.bfloat16 else B.F32, t, n,
-                                                    _ld(x), codes.data_ptr(), scale.data_ptr(), _stream(x.device)),
-                   "admmq_checkpoint_save")
-        return cls(codes, scale)
+        ld, inner = x.stride()
+        if t > 0 and inner != 1:
+            _fail(B.ERR_SHAPE, "Checkpoint.save: adjacent values")
+        self = cls.__new__(cls)
+        self.codes = codes = x.new_empty((t, n), dtype=torch.int8)
+        self.scale = scale = x.new_empty((t, -(-n // BLOCK)), dtype=torch.float32)
+        _call((_lib or _library()).admmq_checkpoint_save, "admmq_checkpoint_save", x.get_device(), x.data_ptr(),
+              1 if bf16 else 0, t, n, ld if t > 1 else n, codes.data_ptr(), scale.data_ptr())
+        return self
 
     def restore(self, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        _need(dtype in (torch.float32, torch.bfloat16), "Checkpoint.restore: fp32 or bf16")
-        t, n = self.codes.shape
+        codes = self.codes
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            _fail(B.ERR_INVALID_ARG, "Checkpoint.restore: fp32 or bf16")
+        t, n = codes.shape
+        ld = n
         if out is None:
-            out = torch.empty(t, n, dtype=dtype, device=self.device)
+            out = codes.new_empty((t, n), dtype=dtype)
         else:
             _need(out.dtype == dtype and out.device == self.device and tuple(out.shape) == (t, n)
                   and (t == 0 or out.stride(1) == 1), "Checkpoint.restore: out [rows, width]", B.ERR_SHAPE)
-        with _on(self.device):
-            _check(_library().admmq_checkpoint_restore(self.codes.data_ptr(), self.scale.data_ptr(), t, n,
-                                                       out.data_ptr(), B.BF16 if dtype == torch.bfloat16 else B.F32,
-                                                       _ld(out), _stream(self.device)), "admmq_checkpoint_restore")
+            ld = _ld(out)
+        _call((_lib or _library()).admmq_checkpoint_restore, "admmq_checkpoint_restore", codes.get_device(),
+              codes.data_ptr(), self.scale.data_ptr(), t, n, out.data_ptr(), 1 if dtype is torch.bfloat16 else 0, ld)
         return out
 
 
@@ -267,7 +268,7 @@ class QuantLinear:
         _need(codes.dim() == 2 and codes.dtype == torch.uint8 and codes.is_cuda and codes.is_contiguous(),
               "QuantLinear: contiguous uint8 codes [d_out, d_in]")
         self.d_out, self.d_in = codes.shape
-        self.bits, self.group_size, self.device = bits, group_size, codes.device
+        self.bits, self.group_size, self.device, self.index = bits, group_size, codes.device, codes.get_device()
         groups = 1 if group_size in (0, self.d_in) else self.d_in // max(1, group_size)
         for t in (scale, zero):
             _need(t.dtype == torch.float32 and t.device == codes.device and t.is_contiguous(),
@@ -278,51 +279,52 @@ class QuantLinear:
         _need(nb > 0 and ng > 0, "QuantLinear: d_in and d_out multiples of 8, the group a multiple of 64", B.ERR_SHAPE)
         self.packed = torch.empty(nb, dtype=torch.uint8, device=self.device)
         self.grid = torch.empty(ng, dtype=torch.uint8, device=self.device)
-        with _on(self.device):
-            _check(lib.admmq_pack_layer(codes.data_ptr(), scale.data_ptr(), zero.data_ptr(), self.d_in, self.d_out,
-                                        bits, group_size, self.packed.data_ptr(), self.grid.data_ptr(),
-                                        _status(self.device), _stream(self.device)), "admmq_pack_layer")
+        _call(lib.admmq_pack_layer, "admmq_pack_layer", self.index, codes.data_ptr(), scale.data_ptr(), zero.data_ptr(),
+              self.d_in, self.d_out, bits, group_size, self.packed.data_ptr(), self.grid.data_ptr(),
+              _status(self.index))
         check_device_status(self.device, "admmq_pack_layer")
         self._c = PackedLayer(C.sizeof(PackedLayer), self.d_in, self.d_out, group_size, self.packed.data_ptr(),
                               self.grid.data_ptr())
         self._ref = C.addressof(self._c)
 
     def _run(self, fn, name, x, k, m, bank, plan, out, factor):
-        dev = self.device
-        _rows(x, k, dev, name)
+        index = self.index
+        ldx = _rows(x, k, index, name)
         t = x.shape[0]
         if out is None:
-            out = torch.empty(t, m, dtype=torch.bfloat16, device=dev)
+            out, ldo = x.new_empty((t, m)), m
         else:
-            _rows(out, m, dev, name + " out")
+            ldo = _rows(out, m, index, name + " out")
             _need(out.shape[0] == t, name + ": out has other rows", B.ERR_SHAPE)
-        ref = row_ptr = f_ptr = None
-        if bank is not None:
-            _need(plan is not None and plan.n_rows == t, name + ": a plan of these rows goes with a bank", B.ERR_SHAPE)
-            _need(bank.d_in == self.d_in and bank.d_out == self.d_out and plan.n_adapters == bank.n_adapters,
-                  name + ": bank, plan and layer differ", B.ERR_SHAPE)
-            _need(bank.device == dev and plan.device == dev, name + ": bank and plan on the layer's device")
-            if factor is None:
-                factor = torch.empty(t, bank.rank, dtype=torch.float32, device=dev)
-            else:
-                _need(factor.dtype == torch.float32 and factor.is_contiguous() and factor.device == dev
-                      and tuple(factor.shape) == (t, bank.rank), name + ": factor [rows, rank] fp32", B.ERR_SHAPE)
-            ref, row_ptr, f_ptr = bank._ref, plan._ptr[0], factor.data_ptr()
-        with _on(dev):
-            _check(fn(self._ref, ref, t, row_ptr, x.data_ptr(), _ld(x), out.data_ptr(), _ld(out), f_ptr, _status(dev),
-                      _stream(dev)), name)
+        if bank is None:
+            _call(fn, name, index, self._ref, None, t, None, x.data_ptr(), ldx, out.data_ptr(), ldo, None,
+                  _status(index))
+            return out, None
+        if plan is None or plan.n_rows != t:
+            _fail(B.ERR_SHAPE, name + ": a plan of these rows goes with a bank")
+        if bank.d_in != self.d_in or bank.d_out != self.d_out or plan.n_adapters != bank.n_adapters:
+            _fail(B.ERR_SHAPE, name + ": bank, plan and layer differ")
+        if bank.index != index or plan.index != index:
+            _fail(B.ERR_INVALID_ARG, name + ": bank and plan on the layer's device")
+        if factor is None:
+            factor = x.new_empty((t, bank.rank), dtype=torch.float32)
+        else:
+            _need(factor.dtype == torch.float32 and factor.is_contiguous() and factor.get_device() == index
+                  and tuple(factor.shape) == (t, bank.rank), name + ": factor [rows, rank] fp32", B.ERR_SHAPE)
+        _call(fn, name, index, self._ref, bank._ref, t, plan._ptr[0], x.data_ptr(), ldx, out.data_ptr(), ldo,
+              factor.data_ptr(), _status(index))
         return out, factor
 
     def forward(self, x: torch.Tensor, bank: Optional[AdapterBank] = None, plan: Optional[RequestPlan] = None,
                 out: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
         """(y, h):  y_t = W x_t + up_a^T h_t,  h_t = scale_a down_a x_t (None without a bank).  x [rows, d_in] bf16."""
-        return self._run(_library().admmq_linear_forward, "admmq_linear_forward", x, self.d_in, self.d_out, bank, plan,
+        return self._run((_lib or _library()).admmq_linear_forward, "admmq_linear_forward", x, self.d_in, self.d_out, bank, plan,
                          out, h)
 
     def grad_input(self, dy: torch.Tensor, bank: Optional[AdapterBank] = None, plan: Optional[RequestPlan] = None,
                    out: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None):
         """(dx, u):  dx_t = W^T dy_t + down_a^T u_t,  u_t = scale_a up_a dy_t (None without a bank)."""
-        return self._run(_library().admmq_linear_grad_input, "admmq_linear_grad_input", dy, self.d_out, self.d_in, bank,
+        return self._run((_lib or _library()).admmq_linear_grad_input, "admmq_linear_grad_input", dy, self.d_out, self.d_in, bank,
                          plan, out, u)
 
 
@@ -331,82 +333,102 @@ def adapter_grads(bank: AdapterBank, plan: RequestPlan, x: Union[Checkpoint, tor
                   grad_up: Optional[torch.Tensor] = None):
     """(d_down, d_up), bf16 in the bank's layout: sums over an adapter's rows of u_t x_t^T and h_t dy_t^T.  x: the
     layer's input in bf16, or its Checkpoint.  An adapter without rows gets zeros."""
-    dev, name = bank.device, "admmq_adapter_grad"
+    index, name = bank.index, "admmq_adapter_grad"
     t, r = plan.n_rows, bank.rank
-    _need(plan.n_adapters == bank.n_adapters, name + ": bank and plan differ", B.ERR_SHAPE)
-    _need(plan.device == dev and x.device == dev, name + ": one device")
+    if plan.n_adapters != bank.n_adapters:
+        _fail(B.ERR_SHAPE, name + ": bank and plan differ")
     for f in (h, u):
-        _need(f.dtype == torch.float32 and f.is_contiguous() and f.device == dev, name + ": contiguous fp32 h and u")
-        _need(tuple(f.shape) == (t, r), name + ": h and u [rows, rank]", B.ERR_SHAPE)
-    _rows(dy, bank.d_out, dev, name + " dy")
-    _need(dy.shape[0] == t and tuple(x.shape) == (t, bank.d_in), name + ": x and dy of the plan's rows", B.ERR_SHAPE)
-    kept = isinstance(x, Checkpoint)
-    if not kept:
-        _rows(x, bank.d_in, dev, name + " x")
+        if f.dtype is not torch.float32 or not f.is_contiguous() or f.get_device() != index:
+            _fail(B.ERR_INVALID_ARG, name + ": contiguous fp32 h and u")
+        if f.shape != (t, r):
+            _fail(B.ERR_SHAPE, name + ": h and u [rows, rank]")
+    lddy = _rows(dy, bank.d_out, index, name + " dy")
+    if dy.shape[0] != t or x.shape != (t, bank.d_in):
+        _fail(B.ERR_SHAPE, name + ": x and dy of the plan's rows")
+    if isinstance(x, Checkpoint):
+        if plan.index != index or x.codes.get_device() != index:
+            _fail(B.ERR_INVALID_ARG, name + ": one device")
+        xp, ldx, codes, scale = 0, 0, x.codes.data_ptr(), x.scale.data_ptr()
+    else:
+        if plan.index != index:
+            _fail(B.ERR_INVALID_ARG, name + ": one device")
+        ldx = _rows(x, bank.d_in, index, name + " x")
+        xp, codes, scale = x.data_ptr(), 0, 0
     out = []
     for g, like in ((grad_down, bank.down), (grad_up, bank.up)):
         if g is None:
             g = torch.empty_like(like)
         else:
-            _need(g.dtype == torch.bfloat16 and g.is_contiguous() and g.device == dev and g.shape == like.shape,
+            _need(g.dtype == torch.bfloat16 and g.is_contiguous() and g.device == like.device and g.shape == like.shape,
                   name + ": gradients of the bank's layout", B.ERR_SHAPE)
         out.append(g)
-    args = AdapterGradArgs(C.sizeof(AdapterGradArgs), bank.d_in, bank.d_out, bank.n_adapters, r, t, plan._ptr[1],
-                           plan._ptr[2], h.data_ptr(), u.data_ptr(), None if kept else x.data_ptr(),
-                           0 if kept else _ld(x), x.codes.data_ptr() if kept else None,
-                           x.scale.data_ptr() if kept else None, dy.data_ptr(), _ld(dy), out[0].data_ptr(),
+    args = _GRAD_ARGS.pack(_GRAD_ARGS_BYTES, bank.d_in, bank.d_out, bank.n_adapters, r, t, plan._ptr[1], plan._ptr[2],
+                           h.data_ptr(), u.data_ptr(), xp, ldx, codes, scale, dy.data_ptr(), lddy, out[0].data_ptr(),
                            out[1].data_ptr())
-    with _on(dev):
-        _check(_library().admmq_adapter_grad(C.addressof(args), _stream(dev)), name)
+    _call((_lib or _library()).admmq_adapter_grad, name, index, args)
     return out[0], out[1]
 
 
-def _qk(name, q, k, wq, wk, cos, sin, positions, eps, dq, dk, out_q, out_k):
-    dev, dt = q.device, q.dtype
-    _need(q.is_cuda and dt in (torch.float32, torch.bfloat16), name + ": fp32 or bf16 on a GPU")
-    _need(q.dim() == 3 and k.dim() == 3 and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2],
-          name + ": q [rows, heads, dim], k [rows, heads, dim]", B.ERR_SHAPE)
+def _heads(x, t, h, d, dt, index, name):
+    """Checks a [t, h, d] tensor, returns its row and head strides."""
+    if x.dtype is not dt or x.get_device() != index:
+        _fail(B.ERR_INVALID_ARG, name + ": one type, one device")
+    if x.dim() != 3 or x.shape != (t, h, d):
+        _fail(B.ERR_SHAPE, name + ": [rows, heads, dim]")
+    row, head, inner = x.stride()
+    if inner != 1 and x.numel() > 0:
+        _fail(B.ERR_SHAPE, name + ": adjacent values of a head")
+    return (row if t > 1 else 0), (head if h > 1 else 0)
+
+
+def _qk(fn, name, q, k, wq, wk, cos, sin, positions, eps, dq, dk, out_q, out_k):
+    dt, index = q.dtype, q.get_device()
+    bf16 = dt is torch.bfloat16
+    if not q.is_cuda or not (bf16 or dt is torch.float32):
+        _fail(B.ERR_INVALID_ARG, name + ": fp32 or bf16 on a GPU")
+    if q.dim() != 3 or k.dim() != 3:
+        _fail(B.ERR_SHAPE, name + ": q and k [rows, heads, dim]")
     t, hq, d = q.shape
     hk = k.shape[1]
-    for x, h in ((q, hq), (k, hk), (dq, hq), (dk, hk), (out_q, hq), (out_k, hk)):
-        if x is None:
-            continue
-        _need(x.dtype == dt and x.device == dev, name + ": one type, one device")
-        _need(tuple(x.shape) == (t, h, d) and (x.numel() == 0 or x.stride(2) == 1),
-              name + ": [rows, heads, dim] with adjacent values", B.ERR_SHAPE)
+    sq, sk = _heads(q, t, hq, d, dt, index, name), _heads(k, t, hk, d, dt, index, name)
     for w in (wq, wk):
-        _need(w.dtype == dt and w.device == dev and w.is_contiguous(), name + ": weights of q's type")
-        _need(tuple(w.shape) == (d,), name + ": weights [dim]", B.ERR_SHAPE)
-    _need(cos.dtype == sin.dtype == torch.float32 and cos.device == sin.device == dev and cos.is_contiguous()
-          and sin.is_contiguous(), name + ": contiguous fp32 cos and sin")
-    _need(cos.dim() == 2 and cos.shape == sin.shape, name + ": cos and sin [positions, rot / 2]", B.ERR_SHAPE)
-    _need(positions.dtype == torch.int32 and positions.device == dev and positions.is_contiguous(),
-          name + ": int32 positions")
-    _need(tuple(positions.shape) == (t,), name + ": a position a row", B.ERR_SHAPE)
+        if w.dtype is not dt or w.get_device() != index or not w.is_contiguous():
+            _fail(B.ERR_INVALID_ARG, name + ": weights of q's type")
+        if w.shape != (d,):
+            _fail(B.ERR_SHAPE, name + ": weights [dim]")
+    for c in (cos, sin):
+        if c.dtype is not torch.float32 or c.get_device() != index or not c.is_contiguous():
+            _fail(B.ERR_INVALID_ARG, name + ": contiguous fp32 cos and sin")
+    if cos.dim() != 2 or cos.shape != sin.shape:
+        _fail(B.ERR_SHAPE, name + ": cos and sin [positions, rot / 2]")
+    if positions.dtype is not torch.int32 or positions.get_device() != index or not positions.is_contiguous():
+        _fail(B.ERR_INVALID_ARG, name + ": contiguous int32 positions")
+    if positions.shape != (t,):
+        _fail(B.ERR_SHAPE, name + ": a position a row")
+    dense_q, dense_k = (hq * d, d), (hk * d, d)
     if out_q is None:
-        out_q = torch.empty(t, hq, d, dtype=dt, device=dev)
+        out_q, oq = q.new_empty((t, hq, d)), dense_q
+    else:
+        oq = _heads(out_q, t, hq, d, dt, index, name)
     if out_k is None:
-        out_k = torch.empty(t, hk, d, dtype=dt, device=dev)
-    args = QkArgs(C.sizeof(QkArgs), B.BF16 if dt == torch.bfloat16 else B.F32, hq, hk, d, 2 * cos.shape[1], t, eps,
-                  q.data_ptr(), k.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), wq.data_ptr(),
-                  wk.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0], positions.data_ptr(),
-                  out_q.data_ptr(), out_k.data_ptr(), out_q.stride(0), out_q.stride(1), out_k.stride(0),
-                  out_k.stride(1))
-    args.d_status = _status(dev)
-    if dq is None:
-        with _on(dev):
-            _check(_library().admmq_qk_norm_rope(C.addressof(args), _stream(dev)), name)
-        return out_q, out_k
-    gw = torch.empty(2, d, dtype=dt, device=dev)
-    args.d_dy_q, args.d_dy_k = dq.data_ptr(), dk.data_ptr()
-    args.dy_q_row, args.dy_q_head, args.dy_k_row, args.dy_k_head = dq.stride(0), dq.stride(1), dk.stride(0), dk.stride(1)
-    args.d_grad_wq, args.d_grad_wk = gw[0].data_ptr(), gw[1].data_ptr()
-    args.workspace_bytes = _library().admmq_qk_workspace_bytes(d)
-    work = torch.empty(max(16, args.workspace_bytes), dtype=torch.uint8, device=dev)
-    args.d_workspace = work.data_ptr()
-    with _on(dev):
-        _check(_library().admmq_qk_norm_rope_backward(C.addressof(args), _stream(dev)), name)
-    return out_q, out_k, gw[0], gw[1]
+        out_k, ok = k.new_empty((t, hk, d)), dense_k
+    else:
+        ok = _heads(out_k, t, hk, d, dt, index, name)
+    gw = None
+    back = (0,) * 10
+    if dq is not None:
+        gq, gk = _heads(dq, t, hq, d, dt, index, name), _heads(dk, t, hk, d, dt, index, name)
+        gw = q.new_empty((2, d))
+        nbytes = _lib.admmq_qk_workspace_bytes(d)
+        work = torch.empty(max(16, nbytes), dtype=torch.uint8, device=q.device)
+        at = gw.data_ptr()
+        back = (dq.data_ptr(), dk.data_ptr(), *gq, *gk, at, at + d * gw.element_size(), work.data_ptr(), nbytes)
+    args = _QK_ARGS.pack(_QK_ARGS_BYTES, 1 if bf16 else 0, hq, hk, d, 2 * cos.shape[1], t, eps, q.data_ptr(),
+                         k.data_ptr(), *sq, *sk, wq.data_ptr(), wk.data_ptr(), cos.data_ptr(), sin.data_ptr(),
+                         cos.shape[0], positions.data_ptr(), out_q.data_ptr(), out_k.data_ptr(), *oq, *ok, *back,
+                         _status(index))
+    _call(fn, name, index, args)
+    return (out_q, out_k) if gw is None else (out_q, out_k, gw[0], gw[1])
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: torch.Tensor, wk: torch.Tensor, cos: torch.Tensor,
@@ -415,7 +437,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: torch.Tensor, wk: torch.T
     """(q', k'): every head normed by its root mean square, weighted, and its first rot values rotated by the row's
     position (pairs i, i + rot / 2).  q [rows, heads, dim] and k [rows, kv heads, dim] may be views into one buffer;
     cos, sin [positions, rot / 2] fp32; positions [rows] int32.  out_q, out_k may be q and k themselves."""
-    return _qk("admmq_qk_norm_rope", q, k, wq, wk, cos, sin, positions, eps, None, None, out_q, out_k)
+    return _qk((_lib or _library()).admmq_qk_norm_rope, "admmq_qk_norm_rope", q, k, wq, wk, cos, sin, positions, eps,
+               None, None, out_q, out_k)
 
 
 def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, wq: torch.Tensor, wk: torch.Tensor, cos: torch.Tensor,
@@ -423,4 +446,5 @@ def qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, wq: torch.Tensor, wk
                           eps: float = 1e-6, out_q: Optional[torch.Tensor] = None,
                           out_k: Optional[torch.Tensor] = None):
     """Gradients (q, k, wq, wk) of qk_norm_rope from those of its results, with its inputs (before the norm)."""
-    return _qk("admmq_qk_norm_rope_backward", q, k, wq, wk, cos, sin, positions, eps, dq, dk, out_q, out_k)
+    return _qk((_lib or _library()).admmq_qk_norm_rope_backward, "admmq_qk_norm_rope_backward", q, k, wq, wk, cos, sin,
+               positions, eps, dq, dk, out_q, out_k)

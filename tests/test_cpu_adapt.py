@@ -1,0 +1,190 @@
+"""CPU checks of the operators on quantized layers: argument validation of the C entry points (fake pointers, never
+dereferenced: every call fails before anything is enqueued), argument structs, and the plan of a batch's requests."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def adapt():
+    from paper_2605_11222_b200 import adapt, build
+    build.build()
+    adapt._library()
+    return adapt
+
+
+FAKE = 0x10000
+
+
+def _layer(adapt, d_in=128, d_out=64, group=64, packed=FAKE, grid=FAKE):
+    return adapt.PackedLayer(C.sizeof(adapt.PackedLayer), d_in, d_out, group, packed, grid)
+
+
+def _bank(adapt, n=2, rank=8, down=FAKE, up=FAKE, scale=FAKE):
+    return adapt.Adapters(C.sizeof(adapt.Adapters), n, rank, down, up, scale)
+
+
+def test_sizes_of_a_packed_layer(adapt):
+    lib = adapt._library()
+    assert lib.admmq_packed_bytes(4096, 1024) == 4096 * 1024 // 2
+    assert lib.admmq_packed_bytes(72, 8) == 2 * 8 * 32                     # 72 channels: two blocks of 64
+    assert lib.admmq_grid_bytes(4096, 1024, 128) == 32 * 1024 * 8
+    assert lib.admmq_grid_bytes(4096, 1024, 0) == lib.admmq_grid_bytes(4096, 1024, 4096) == 1024 * 8
+    for bad in [(60, 64), (64, 60), (0, 64), (64, 0), (14344, 64), (-8, 8)]:
+        assert lib.admmq_packed_bytes(*bad) == 0
+    for bad in [(128, 64, 32), (128, 64, 48), (128, 64, 256), (128, 64, -64), (192, 64, 128)]:
+        assert lib.admmq_grid_bytes(*bad) == 0
+
+
+def test_pack_layer_refuses_bad_arguments(adapt):
+    from paper_2605_11222_b200 import binding as B
+    f = adapt._library().admmq_pack_layer
+    ok = [FAKE, FAKE, FAKE, 128, 64, 4, 64, FAKE, FAKE, FAKE, None]
+
+    def with_(i, v):
+        a = list(ok)
+        a[i] = v
+        return f(*a)
+
+    for i in (0, 1, 2, 7, 8, 9):
+        assert with_(i, None) == B.ERR_INVALID_ARG
+    assert with_(7, FAKE + 8) == B.ERR_INVALID_ARG
+    assert with_(5, 5) == B.ERR_UNSUPPORTED and with_(5, 8) == B.ERR_UNSUPPORTED
+    assert with_(5, 1) == B.ERR_SHAPE and with_(5, 9) == B.ERR_SHAPE
+    assert with_(6, 32) == B.ERR_SHAPE and with_(3, 124) == B.ERR_SHAPE and with_(4, 63) == B.ERR_SHAPE
+
+
+@pytest.mark.parametrize("name", ["admmq_linear_forward", "admmq_linear_grad_input"])
+def test_linear_refuses_bad_arguments(adapt, name):
+    from paper_2605_11222_b200 import binding as B
+    f = getattr(adapt._library(), name)
+    grad = name.endswith("input")
+    ldi, ldo = (64, 128) if grad else (128, 64)
+    layer, bank = _layer(adapt), _bank(adapt)
+    ok = [C.byref(layer), C.byref(bank), 5, FAKE, FAKE, ldi, FAKE, ldo, FAKE, FAKE, None]
+
+    def with_(i, v):
+        a = list(ok)
+        a[i] = v
+        return f(*a)
+
+    assert with_(0, None) == B.ERR_INVALID_ARG
+    for i in (3, 4, 6, 8, 9):
+        assert with_(i, None) == B.ERR_INVALID_ARG
+    for i in (4, 6, 8):
+        assert with_(i, FAKE + 8) == B.ERR_INVALID_ARG
+    for i, ld in ((5, ldi), (7, ldo)):
+        assert with_(i, ld - 8) == B.ERR_SHAPE and with_(i, ld + 4) == B.ERR_SHAPE
+    assert with_(2, -1) == B.ERR_SHAPE and with_(2, 2 ** 31) == B.ERR_SHAPE
+    for bad in (_layer(adapt, 124), _layer(adapt, 128, 60), _layer(adapt, 128, 64, 96)):
+        assert with_(0, C.byref(bad)) == B.ERR_SHAPE
+    for bad in (_layer(adapt, packed=None), _layer(adapt, grid=FAKE + 4)):
+        assert with_(0, C.byref(bad)) == B.ERR_INVALID_ARG
+    layer2 = _layer(adapt)
+    layer2.struct_size -= 4
+    assert with_(0, C.byref(layer2)) == B.ERR_INVALID_ARG
+    for bad in (_bank(adapt, 0), _bank(adapt, 70000), _bank(adapt, 2, 12), _bank(adapt, 2, 136), _bank(adapt, 2, 0)):
+        assert with_(1, C.byref(bad)) == B.ERR_SHAPE
+    for bad in (_bank(adapt, down=None), _bank(adapt, up=FAKE + 2), _bank(adapt, scale=None)):
+        assert with_(1, C.byref(bad)) == B.ERR_INVALID_ARG
+    assert with_(2, 0) == B.OK                                             # no rows: nothing to do
+
+
+def test_argument_structs_have_the_c_sizes(adapt):
+    """A struct of another size is refused before anything else; with the right one the next check speaks."""
+    from paper_2605_11222_b200 import binding as B
+    lib = adapt._library()
+    n = adapt._GRAD_ARGS.size
+    good = adapt._GRAD_ARGS.pack(n, 124, 64, 1, 8, 1, *[FAKE] * 5, 128, *[FAKE] * 3, 64, FAKE, FAKE)
+    assert lib.admmq_adapter_grad(good, None) == B.ERR_SHAPE               # d_in 124
+    bad = adapt._GRAD_ARGS.pack(n + 8, 124, 64, 1, 8, 1, *[FAKE] * 5, 128, *[FAKE] * 3, 64, FAKE, FAKE)
+    assert lib.admmq_adapter_grad(bad, None) == B.ERR_INVALID_ARG
+    n = adapt._QK_ARGS.size
+
+    def qk(size=n, dtype=1, hq=2, hk=1, d=64, rot=64, rows=3, eps=1e-6, q=FAKE, row=128, pos=FAKE, npos=10,
+           status=FAKE, back=(0,) * 10):
+        return adapt._QK_ARGS.pack(size, dtype, hq, hk, d, rot, rows, eps, q, FAKE, row, 64, 64, 64, FAKE, FAKE, FAKE,
+                                   FAKE, npos, pos, FAKE, FAKE, 128, 64, 64, 64, *back, status)
+
+    fwd, bwd = lib.admmq_qk_norm_rope, lib.admmq_qk_norm_rope_backward
+    assert fwd(qk(size=n - 8), None) == B.ERR_INVALID_ARG
+    assert fwd(qk(rows=0), None) == B.OK
+    for kw in (dict(d=40), dict(d=272), dict(rot=24), dict(rot=80), dict(hq=0), dict(hk=-1), dict(row=132), dict(rows=-1),
+               dict(npos=0)):
+        assert fwd(qk(**kw), None) == B.ERR_SHAPE, kw
+    for kw in (dict(dtype=2), dict(eps=-1.0), dict(eps=float("nan")), dict(q=0), dict(q=FAKE + 8), dict(pos=0),
+               dict(status=0)):
+        assert fwd(qk(**kw), None) == B.ERR_INVALID_ARG, kw
+    assert bwd(qk(), None) == B.ERR_INVALID_ARG                            # no dy, no workspace
+    ws = lib.admmq_qk_workspace_bytes(64)
+    assert ws > 0 and lib.admmq_qk_workspace_bytes(40) == 0
+    assert bwd(qk(back=(FAKE, FAKE, 128, 64, 64, 64, FAKE, FAKE, FAKE, ws - 1)), None) == B.ERR_WORKSPACE
+
+
+def test_adapter_grad_refuses_bad_arguments(adapt):
+    from paper_2605_11222_b200 import binding as B
+    f, S = adapt._library().admmq_adapter_grad, adapt._GRAD_ARGS
+
+    def call(d_in=128, d_out=64, n=2, rank=8, rows=5, order=FAKE, offsets=FAKE, h=FAKE, u=FAKE, x=FAKE, ldx=128, codes=0,
+             scale=0, dy=FAKE, lddy=64, gd=FAKE, gu=FAKE):
+        return f(S.pack(S.size, d_in, d_out, n, rank, rows, order, offsets, h, u, x, ldx, codes, scale, dy, lddy, gd, gu),
+                 None)
+
+    assert f(None, None) == B.ERR_INVALID_ARG
+    for kw in (dict(d_out=60), dict(n=0), dict(n=65536), dict(rank=12), dict(rank=136), dict(rows=-1), dict(ldx=120),
+               dict(ldx=132), dict(lddy=56), dict(lddy=68)):
+        assert call(**kw) == B.ERR_SHAPE, kw
+    for kw in (dict(order=0), dict(offsets=0), dict(h=0), dict(u=FAKE + 4), dict(x=0), dict(x=FAKE + 2), dict(dy=0),
+               dict(gd=0), dict(gu=FAKE + 8), dict(x=0, codes=FAKE), dict(x=0, codes=FAKE + 8, scale=FAKE)):
+        assert call(**kw) == B.ERR_INVALID_ARG, kw
+
+
+def test_checkpoint_refuses_bad_arguments(adapt):
+    from paper_2605_11222_b200 import binding as B
+    lib = adapt._library()
+    for f, ok in ((lib.admmq_checkpoint_save, [FAKE, 1, 4, 64, 64, FAKE, FAKE, None]),
+                  (lib.admmq_checkpoint_restore, [FAKE, FAKE, 4, 64, FAKE, 1, 64, None])):
+        save = f is lib.admmq_checkpoint_save
+        dt, ld, ptrs = (1, 4, (0, 5, 6)) if save else (5, 6, (0, 1, 4))
+        width = 3
+
+        def with_(i, v):
+            a = list(ok)
+            a[i] = v
+            return f(*a)
+
+        assert with_(dt, 2) == B.ERR_INVALID_ARG
+        for i in ptrs:
+            assert with_(i, None) == B.ERR_INVALID_ARG
+        assert with_(width, 60) == B.ERR_SHAPE and with_(width, 0) == B.ERR_SHAPE
+        assert with_(ld, 56) == B.ERR_SHAPE and with_(ld, 68) == B.ERR_SHAPE
+        assert with_(2, -1) == B.ERR_SHAPE and with_(2, 0) == B.OK
+
+
+def test_request_plan(adapt):
+    from paper_2605_11222_b200 import binding as B
+    plan = adapt.RequestPlan([2, 0, 3, 1, 2], [1, 0, -1, 3, 1], 4, device="cpu")
+    assert plan.n_rows == 8
+    assert plan.row_adapter.tolist() == [1, 1, -1, -1, -1, 3, 1, 1]
+    off = plan.offsets.tolist()
+    assert off == [0, 0, 4, 4, 5]
+    assert plan.order.tolist()[:5] == [0, 1, 6, 7, 5]                      # rows of adapter 1 in order, then of 3
+    assert all(t.dtype == torch.int32 for t in (plan.row_adapter, plan.order, plan.offsets))
+    empty = adapt.RequestPlan([], [], 2, device="cpu")
+    assert empty.n_rows == 0 and empty.offsets.tolist() == [0, 0, 0]
+    rng = np.random.default_rng(0)
+    lengths, ids = rng.integers(0, 9, 50), rng.integers(-1, 7, 50)
+    plan = adapt.RequestPlan(lengths, ids, 7, device="cpu")
+    rows = np.repeat(ids, lengths)
+    for a in range(7):
+        o = plan.offsets.tolist()
+        assert plan.order.tolist()[o[a]: o[a + 1]] == np.flatnonzero(rows == a).tolist()
+    for bad in (([1, 2], [0]), ([-1], [0])):
+        with pytest.raises(adapt.AdmmqError) as e:
+            adapt.RequestPlan(*bad, 2, device="cpu")
+        assert e.value.status == B.ERR_SHAPE
+    for a in (-2, 2):
+        with pytest.raises(adapt.AdmmqError):
+            adapt.RequestPlan([1], [a], 2, device="cpu")

@@ -3,7 +3,10 @@
 //
 // Bound: memory, 3 bytes a bf16 value (2 read, 1 written) and 4 bytes a block.  Sixteen threads hold one block, 8
 // channels each, so that the maximum is four shuffles away and nothing is read twice; a thread takes UNROLL blocks at
-// once, which keeps 64 (bf16) or 128 (fp32) bytes a thread in flight.
+// once, which keeps 64 (bf16) or 128 (fp32) bytes a thread in flight.  At three bytes a value the instructions count
+// (a first form with eight divisions a thread and scalar arithmetic issued 170 a block and thread and ran at 45 % of the
+// copy rate): maxima and products run on packed pairs, and the scale's division and reciprocal are made by one
+// thread of four for all.
 #include "adapt.h"
 
 namespace admmq {
@@ -15,98 +18,155 @@ constexpr int THREADS = 256;
 constexpr int UNROLL = 4;
 constexpr int PAIRS = THREADS / LANES * UNROLL;   // (row, block) pairs of one CTA
 
-struct Place {
-  long long row;
-  int blk;
+// The (row, block) pairs of a CTA: consecutive ones, nb to a row.
+struct Pairs {
+  long long row0;
+  uint32_t blk0, nb, inv;                   // inv = ceil(2^32 / nb): exact quotients for numbers below 2^32 / nb
+  __device__ __forceinline__ Pairs(long long T, uint32_t nb_, uint32_t inv_) : nb(nb_), inv(inv_) {
+    const long long first = (long long)blockIdx.x * PAIRS;
+    if (T * nb <= 0x7fffffffLL) {
+      const uint32_t r = (uint32_t)first / nb;
+      row0 = r;
+      blk0 = (uint32_t)first - r * nb;
+    } else {
+      row0 = first / nb;
+      blk0 = (uint32_t)(first - row0 * nb);
+    }
+  }
+  __device__ __forceinline__ void at(uint32_t off, long long& row, int& blk) const {
+    const uint32_t n = blk0 + off, r = nb == 1 ? n : __umulhi(n, inv);
+    row = row0 + r;
+    blk = (int)(n - r * nb);
+  }
 };
-// Pair `off` after the CTA's first one; nb blocks a row.
-__device__ __forceinline__ Place place_of(long long row0, unsigned blk0, unsigned off, unsigned nb) {
-  const unsigned s = blk0 + off, r = s / nb;
-  return {row0 + r, (int)(s - r * nb)};
+
+// The largest magnitude's bit pattern of this thread's 8 values.  (The order of the patterns is that of the
+// magnitudes, with infinity and NaN on top: an integer maximum finds the largest value and does not lose a NaN.)
+// bf16: as the upper 16 bits of an fp32 number.
+template <bool BF16>
+__device__ __forceinline__ uint32_t top8(const uint4* r) {
+  if (BF16) {
+    uint32_t t = __vmaxu2(__vmaxu2(r->x & 0x7fff7fffu, r->y & 0x7fff7fffu), __vmaxu2(r->z & 0x7fff7fffu, r->w & 0x7fff7fffu));
+    return max(t & 0xffffu, t >> 16);
+  }
+  uint32_t t = 0;
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    t = max(t, max(max(r[q].x & 0x7fffffffu, r[q].y & 0x7fffffffu), max(r[q].z & 0x7fffffffu, r[q].w & 0x7fffffffu)));
+  return t;
 }
 
 template <bool BF16>
 __global__ void __launch_bounds__(THREADS)
-checkpoint_save_kernel(const void* __restrict__ x, long long T, int width, long long ldx, int nb,
+checkpoint_save_kernel(const void* __restrict__ x, long long T, int width, long long ldx, uint32_t nb, uint32_t nb_inv,
                        int8_t* __restrict__ codes, float* __restrict__ scale) {
-  const long long first = (long long)blockIdx.x * PAIRS;
-  const long long row0 = first / nb;
-  const unsigned blk0 = (unsigned)(first - row0 * nb);
+  constexpr int Q = BF16 ? 1 : 2;           // 16-byte loads of 8 values
+  const Pairs pairs(T, nb, nb_inv);
   const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  uint4 raw[UNROLL][BF16 ? 1 : 2];
-  Place at[UNROLL];
+  uint4 raw[UNROLL][Q];
+  long long row[UNROLL];
+  int blk[UNROLL];
   bool on[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    at[u] = place_of(row0, blk0, (unsigned)(u * (THREADS / LANES) + sub), (unsigned)nb);
-    const int i = at[u].blk * BLOCK + lane * 8;
-    on[u] = at[u].row < T && i < width;       // width is a multiple of 8: all eight channels or none
-    const char* p = (const char*)x + (at[u].row * ldx + i) * (BF16 ? 2 : 4);
+    pairs.at((uint32_t)(u * (THREADS / LANES) + sub), row[u], blk[u]);
+    const int i = blk[u] * BLOCK + lane * 8;
+    on[u] = row[u] < T && i < width;        // width is a multiple of 8: all eight channels or none
+    const char* p = (const char*)x + (row[u] * ldx + i) * (BF16 ? 2 : 4);
 #pragma unroll
-    for (int q = 0; q < (BF16 ? 1 : 2); ++q) raw[u][q] = on[u] ? ldg_stream(p + 16 * q) : make_uint4(0, 0, 0, 0);
+    for (int q = 0; q < Q; ++q) raw[u][q] = on[u] ? ldg_stream(p + 16 * q) : make_uint4(0, 0, 0, 0);
   }
+  // largest magnitude of every block, in all its threads
+  uint32_t top[UNROLL];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) top[u] = top8<BF16>(raw[u]);
+  if (BF16) {                               // two blocks to a register
+#pragma unroll
+    for (int u = 0; u < UNROLL; u += 2) {
+      uint32_t t = top[u] | top[u + 1] << 16;
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) t = __vmaxu2(t, __shfl_xor_sync(0xffffffffu, t, o));
+      top[u] = t << 16;
+      top[u + 1] = t & 0xffff0000u;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
+  }
+  // scale and reciprocal of block u: made by the threads with lane % UNROLL == u
+  uint32_t mine = top[0];
+#pragma unroll
+  for (int u = 1; u < UNROLL; ++u) mine = lane % UNROLL == u ? top[u] : mine;
+  const float my_s = mine < 0x7f800000u ? __fdiv_rn(__uint_as_float(mine), 127.0f) : __int_as_float(0x7fc00000);
+  const float my_y = __frcp_rn(my_s);
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    float v[8];
+    const float s = __shfl_sync(0xffffffffu, my_s, u, LANES), y = __shfl_sync(0xffffffffu, my_y, u, LANES);
+    if (!on[u]) continue;
+    float2 v[4];
     if (BF16) {
-      const uint32_t w[4] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w};
+      v[0] = bf16x2_to_float2(raw[u][0].x);
+      v[1] = bf16x2_to_float2(raw[u][0].y);
+      v[2] = bf16x2_to_float2(raw[u][0].z);
+      v[3] = bf16x2_to_float2(raw[u][0].w);
+    } else {
+      const uint4 a = raw[u][0], b = raw[u][Q - 1];
+      v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+      v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+      v[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+      v[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+    }
+    uint32_t k[8];
+    if (s > 1e-28f) {
+      // code = rint(x / s) with the quotient as a division rounds it, without eight divisions: with y = RN(1 / s),
+      // q0 = RN(x y) and the exact remainder e = x - q0 s, RN(q0 + e y) is the rounded quotient (Markstein 1990,
+      // "Computation of elementary functions on the IBM RISC System/6000 processor").  Adding 1.5 * 2^23 rounds to a
+      // whole number, ties to even, and leaves it in the low bits.
+      const float2 y2 = make_float2(y, y), s2 = make_float2(-s, -s), magic = make_float2(12582912.0f, 12582912.0f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = bf16x2_to_float2(w[e]);
-        v[2 * e] = f.x;
-        v[2 * e + 1] = f.y;
+        const float2 q0 = __fmul2_rn(v[e], y2);
+        const float2 t = __fadd2_rn(__ffma2_rn(__ffma2_rn(q0, s2, v[e]), y2, q0), magic);
+        k[2 * e] = __float_as_uint(t.x);
+        k[2 * e + 1] = __float_as_uint(t.y);
       }
-    } else {
-      const uint4* r = raw[u];
-      const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[BF16 ? 0 : 1].x, r[BF16 ? 0 : 1].y, r[BF16 ? 0 : 1].z,
-                             r[BF16 ? 0 : 1].w};
+    } else if (s > 0.0f) {
+      // a scale so small that a remainder could underflow; one that is subnormal leaves quotients above 127: the clamp
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(w[e]);
+      for (int e = 0; e < 8; ++e)
+        k[e] = (uint32_t)min(127, max(-127, __float2int_rn(__fdiv_rn((e & 1) ? v[e >> 1].y : v[e >> 1].x, s))));
+    } else {                                // zeros, or a scale of NaN
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[e] = 0u;
     }
-    // The order of the magnitudes' bit patterns is that of the magnitudes, with infinity and NaN on top: an integer
-    // maximum finds the largest value and does not lose a NaN.
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const bool finite = top < 0x7f800000u;
-    const float s = finite ? __fdiv_rn(__uint_as_float(top), 127.0f) : __int_as_float(0x7fc00000);
-    if (!on[u]) continue;
-    uint32_t out[2] = {0u, 0u};
-    if (finite && s > 0.0f) {
-      // The quotient as the division rounds it: codes do not depend on how a reciprocal is formed.  (A maximum so
-      // small that the scale is subnormal leaves quotients above 127: the clamp.)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int k = min(127, max(-127, __float2int_rn(__fdiv_rn(v[e], s))));
-        out[e >> 2] |= (uint32_t)(k & 0xff) << (8 * (e & 3));
-      }
-    }
-    *reinterpret_cast<uint2*>(codes + at[u].row * width + at[u].blk * BLOCK + lane * 8) = make_uint2(out[0], out[1]);
-    if (lane == 0) scale[at[u].row * nb + at[u].blk] = s;
+    uint2 out;
+    out.x = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
+    out.y = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
+    *reinterpret_cast<uint2*>(codes + row[u] * width + blk[u] * BLOCK + lane * 8) = out;
+    if (lane == 0) scale[row[u] * nb + blk[u]] = s;
   }
 }
 
 template <bool BF16>
 __global__ void __launch_bounds__(THREADS)
 checkpoint_restore_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scale, long long T, int width,
-                          int nb, void* __restrict__ out, long long ldo) {
-  const long long first = (long long)blockIdx.x * PAIRS;
-  const long long row0 = first / nb;
-  const unsigned blk0 = (unsigned)(first - row0 * nb);
+                          uint32_t nb, uint32_t nb_inv, void* __restrict__ out, long long ldo) {
+  const Pairs pairs(T, nb, nb_inv);
   const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES;
   uint2 raw[UNROLL];
   float s[UNROLL];
-  Place at[UNROLL];
+  long long row[UNROLL];
+  int blk[UNROLL];
   bool on[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    at[u] = place_of(row0, blk0, (unsigned)(u * (THREADS / LANES) + sub), (unsigned)nb);
-    const int i = at[u].blk * BLOCK + lane * 8;
-    on[u] = at[u].row < T && i < width;
-    raw[u] = on[u] ? __ldg(reinterpret_cast<const uint2*>(codes + at[u].row * width + i)) : make_uint2(0, 0);
-    s[u] = on[u] ? __ldg(scale + at[u].row * nb + at[u].blk) : 0.0f;
+    pairs.at((uint32_t)(u * (THREADS / LANES) + sub), row[u], blk[u]);
+    const int i = blk[u] * BLOCK + lane * 8;
+    on[u] = row[u] < T && i < width;
+    raw[u] = on[u] ? __ldg(reinterpret_cast<const uint2*>(codes + row[u] * width + i)) : make_uint2(0, 0);
+    s[u] = on[u] ? __ldg(scale + row[u] * nb + blk[u]) : 0.0f;
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
@@ -117,7 +177,7 @@ checkpoint_restore_kernel(const int8_t* __restrict__ codes, const float* __restr
       const uint32_t w = e < 4 ? raw[u].x : raw[u].y;
       v[e] = s[u] * (float)(int8_t)(w >> (8 * (e & 3)));
     }
-    char* p = (char*)out + (at[u].row * ldo + at[u].blk * BLOCK + lane * 8) * (BF16 ? 2 : 4);
+    char* p = (char*)out + (row[u] * ldo + blk[u] * BLOCK + lane * 8) * (BF16 ? 2 : 4);
     if (BF16) {
       uint4 o;
       o.x = float2_to_bf16x2(v[0], v[1]);
@@ -134,27 +194,37 @@ checkpoint_restore_kernel(const int8_t* __restrict__ codes, const float* __restr
 
 }  // namespace
 
+// CTAs for T rows of nb blocks, and ceil(2^32 / nb); false if the grid cannot hold them.
+static bool plan_pairs(long long T, int nb, unsigned* ctas, uint32_t* inv) {
+  const long long n = (T * nb + PAIRS - 1) / PAIRS;
+  *ctas = (unsigned)n;
+  *inv = (uint32_t)(((1ULL << 32) + nb - 1) / nb);            // (nb = 1 does not use it)
+  return n <= 0x7fffffffLL;
+}
+
 cudaError_t launch_checkpoint_save(const void* x, int is_bf16, long long T, int width, long long ldx, int8_t* codes,
                                    float* scale, cudaStream_t stream) {
   const int nb = (width + BLOCK - 1) / BLOCK;
-  const long long ctas = (T * nb + PAIRS - 1) / PAIRS;
-  if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+  unsigned ctas;
+  uint32_t inv;
+  if (!plan_pairs(T, nb, &ctas, &inv)) return cudaErrorInvalidValue;
   if (is_bf16)
-    checkpoint_save_kernel<true><<<(unsigned)ctas, THREADS, 0, stream>>>(x, T, width, ldx, nb, codes, scale);
+    checkpoint_save_kernel<true><<<ctas, THREADS, 0, stream>>>(x, T, width, ldx, nb, inv, codes, scale);
   else
-    checkpoint_save_kernel<false><<<(unsigned)ctas, THREADS, 0, stream>>>(x, T, width, ldx, nb, codes, scale);
+    checkpoint_save_kernel<false><<<ctas, THREADS, 0, stream>>>(x, T, width, ldx, nb, inv, codes, scale);
   return cudaGetLastError();
 }
 
 cudaError_t launch_checkpoint_restore(const int8_t* codes, const float* scale, long long T, int width, void* out,
                                       int is_bf16, long long ldo, cudaStream_t stream) {
   const int nb = (width + BLOCK - 1) / BLOCK;
-  const long long ctas = (T * nb + PAIRS - 1) / PAIRS;
-  if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+  unsigned ctas;
+  uint32_t inv;
+  if (!plan_pairs(T, nb, &ctas, &inv)) return cudaErrorInvalidValue;
   if (is_bf16)
-    checkpoint_restore_kernel<true><<<(unsigned)ctas, THREADS, 0, stream>>>(codes, scale, T, width, nb, out, ldo);
+    checkpoint_restore_kernel<true><<<ctas, THREADS, 0, stream>>>(codes, scale, T, width, nb, inv, out, ldo);
   else
-    checkpoint_restore_kernel<false><<<(unsigned)ctas, THREADS, 0, stream>>>(codes, scale, T, width, nb, out, ldo);
+    checkpoint_restore_kernel<false><<<ctas, THREADS, 0, stream>>>(codes, scale, T, width, nb, inv, out, ldo);
   return cudaGetLastError();
 }
 

@@ -207,6 +207,35 @@ def test_adapter_grads_match_the_formula(T, n, p, na, r, kind, eight):
             _within(got, want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * ab + 1e-30)
 
 
+# tiles of one CTA with and without a split of K, and tiles of CTA pairs (many rows); K of few and of many steps
+@pytest.mark.parametrize("T,n,p,na,r", [(70, 512, 256, 2, 8), (200, 4096, 512, 3, 24), (600, 512, 256, 2, 8),
+                                        (3000, 1024, 2048, 2, 8), (2600, 192, 4096, 5, 72), (2600, 4096, 64, 40, 16),
+                                        (9000, 256, 1024, 3, 48)])
+def test_projections_are_the_same_bits_every_time(T, n, p, na, r):
+    """The order of every sum is fixed, so a difference between two runs is a race.  Other shapes than the formula tests'
+    (more rows, so that multiprocessors work on several tiles), checked against the formula row by row as well."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T)
+    codes, scale, zero = _layer(g, n, p, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, na, r, n, p), _plan("mixed", T, na, 5)
+    x, dy = _randn(g, T, n).bfloat16(), _randn(g, T, p).bfloat16()
+    W = _weight64(codes, scale, zero)
+    for run, v, w, inn, out in ((layer.forward, x, W.T, bank.down, bank.up), (layer.grad_input, dy, W, bank.up, bank.down)):
+        first = run(v, bank, plan)
+        f64 = torch.zeros(T, r, dtype=torch.float64, device=DEV)
+        want, sq = v.double() @ w, v.double() ** 2 @ w ** 2
+        for a in range(na):
+            t = (plan.row_adapter == a).nonzero()[:, 0]
+            f64[t] = bank.scale[a].double() * (v[t].double() @ inn[a].double().T)
+            want[t] += f64[t] @ out[a].double()
+            sq[t] += f64[t] ** 2 @ out[a].double() ** 2
+        _within(first[0], want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * sq.sqrt() * math.sqrt(w.shape[0]) + 1e-30)
+        for _ in range(40):
+            again = run(v, bank, plan)
+            assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    adapt.check_device_status(DEV)
+
+
 def test_adapter_grads_are_the_same_bits_every_time():
     from paper_2605_11222_b200 import adapt
     g = _gen(9)

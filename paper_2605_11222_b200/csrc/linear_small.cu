@@ -14,7 +14,11 @@
 // shrink: h[t][r] = scale_a sum_i x[t][i] in_a[r][i].  Bound: memory, one pass over the rows and over the adapters in
 // use.  Two forms: a CTA for each row and 8 ranks (a warp a rank) for few rows, and tiles of 16 or 32 rows on mma.sync
 // for more, where the passes over a tile are one per distinct adapter in it.
+#include <cooperative_groups.h>
+
 #include "adapt.h"
+
+namespace cg = cooperative_groups;
 
 namespace admmq {
 namespace {
@@ -216,23 +220,21 @@ __global__ void __launch_bounds__(THREADS) shrink_rows_kernel(const __grid_const
   if (lane == 0) P.h[t * P.rank + r] = v;
 }
 
-// Tiles of 16 MT rows and 8 NT ranks; the warps split the contracted channels, 32 of them a step.
+// Tiles of 16 MT rows and 8 NT ranks.  A cluster shares a tile: its CTAs, and the warps in them, split the contracted
+// channels, 32 of them a step; the CTAs' sums meet over distributed shared memory, in rank order.
 template <int MT, int NT>
-__global__ void __launch_bounds__(THREADS) shrink_tile_kernel(const __grid_constant__ ShrinkParams P) {
+__global__ void __launch_bounds__(THREADS, MT * NT <= 4 ? 2 : 1) shrink_tile_kernel(const __grid_constant__ ShrinkParams P) {
   pdl_launch();
   constexpr int TM = 16 * MT, RN = 8 * NT;
-  extern __shared__ float red[];                   // [WARPS][TM][RN]
+  extern __shared__ float red[];                   // [WARPS][TM][RN], then this CTA's sums [TM][RN]
+  float* part = red + WARPS * TM * RN;
   __shared__ int own[TM];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int share = (int)cluster.block_rank(), shares = (int)cluster.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, q = lane & 3;
-  const long long t0 = (long long)blockIdx.x * TM;
+  const long long t0 = (long long)(blockIdx.x / shares) * TM;
   if (threadIdx.x < TM) own[threadIdx.x] = t0 + threadIdx.x < P.T ? row_adapter_of(P.row_adapter, t0 + threadIdx.x, P.n) : -1;
-  __syncthreads();
-  // rows without an adapter
-  for (int o = threadIdx.x; o < TM * P.rank; o += THREADS) {
-    const int t = o / P.rank;
-    if (own[t] < 0 && t0 + t < P.T) P.h[t0 * P.rank + o] = 0.0f;
-  }
   const bf16* xr[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -241,6 +243,7 @@ __global__ void __launch_bounds__(THREADS) shrink_tile_kernel(const __grid_const
       const long long t = t0 + 16 * m + 8 * hh + g;
       xr[m][hh] = P.x + (t < P.T ? t : P.T - 1) * P.ldx;      // rows past the end: any row, their results are dropped
     }
+  __syncthreads();
   for (int last = -1;;) {
     int a = 0x7fffffff;                            // the next adapter of this tile, in rising order
     for (int t = lane; t < TM; t += 32) a = own[t] > last ? min(a, own[t]) : a;
@@ -256,62 +259,93 @@ __global__ void __launch_bounds__(THREADS) shrink_tile_kernel(const __grid_const
         for (int e = 0; e < 4; ++e) acc[m][nn][e] = 0.0f;
     const bf16* mat = P.mat + (long long)a * P.rank * P.K;
     const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll 2
-    for (int k = warp * 32; k < P.K; k += WARPS * 32) {
-      const int i = k + 8 * q;
-      const bool in = i < P.K;                     // K is a multiple of 8
-      uint4 av[MT][2], bv[NT];
+    constexpr int UNR = 2 * MT + NT <= 4 ? 4 : 2 * MT + NT <= 8 ? 2 : 1;
+    const int stride = WARPS * 32 * shares;
+    for (int k0 = (share * WARPS + warp) * 32; k0 < P.K; k0 += UNR * stride) {
+      uint4 av[UNR][MT][2], bv[UNR][NT];
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int u = 0; u < UNR; ++u) {
+        const int i = k0 + u * stride + 8 * q;
+        const bool in = i < P.K;                   // K is a multiple of 8
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) av[m][hh] = in ? __ldg(reinterpret_cast<const uint4*>(xr[m][hh] + i)) : zero;
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nn = 0; nn < NT; ++nn)
-        bv[nn] = in && 8 * nn + g < P.rank
-                     ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)(8 * nn + g) * P.K + i)) : zero;
+          for (int hh = 0; hh < 2; ++hh)
+            av[u][m][hh] = in ? __ldg(reinterpret_cast<const uint4*>(xr[m][hh] + i)) : zero;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const uint32_t a0[4] = {av[m][0].x, av[m][1].x, av[m][0].y, av[m][1].y};
-        const uint32_t a1[4] = {av[m][0].z, av[m][1].z, av[m][0].w, av[m][1].w};
-#pragma unroll
-        for (int nn = 0; nn < NT; ++nn) {
-          mma_bf16(acc[m][nn], a0, bv[nn].x, bv[nn].y);
-          mma_bf16(acc[m][nn], a1, bv[nn].z, bv[nn].w);
-        }
+        for (int nn = 0; nn < NT; ++nn)
+          bv[u][nn] = in && 8 * nn + g < P.rank
+                          ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)(8 * nn + g) * P.K + i)) : zero;
       }
+#pragma unroll
+      for (int u = 0; u < UNR; ++u)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint4 &lo = av[u][m][0], &hi = av[u][m][1];
+          const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+          for (int nn = 0; nn < NT; ++nn) {
+            mma_bf16(acc[m][nn], a0, bv[u][nn].x, bv[u][nn].y);
+            mma_bf16(acc[m][nn], a1, bv[u][nn].z, bv[u][nn].w);
+          }
+        }
     }
-    __syncthreads();                               // the previous adapter's sums have been read
+    // a row has one adapter: its sums go straight to their place
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nn = 0; nn < NT; ++nn) {
-        float* o = red + ((long long)warp * TM + 16 * m + g) * RN + 8 * nn + 2 * q;
-        o[0] = acc[m][nn][0];
-        o[1] = acc[m][nn][1];
-        o[8 * RN] = acc[m][nn][2];
-        o[8 * RN + 1] = acc[m][nn][3];
-      }
-    __syncthreads();
-    const float s = P.scale[a];
-    for (int o = threadIdx.x; o < TM * RN; o += THREADS) {
-      const int t = o / RN, r = o % RN;
-      if (own[t] != a || r >= P.rank) continue;
-      float v = 0.0f;
+      for (int hh = 0; hh < 2; ++hh)
+        if (own[16 * m + 8 * hh + g] == a) {
+          float* o = red + ((long long)warp * TM + 16 * m + 8 * hh + g) * RN + 2 * q;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) v += red[w * TM * RN + o];
-      P.h[(t0 + t) * P.rank + r] = s * v;
-    }
+          for (int nn = 0; nn < NT; ++nn)
+            *reinterpret_cast<float2*>(o + 8 * nn) = make_float2(acc[m][nn][2 * hh], acc[m][nn][2 * hh + 1]);
+        }
   }
+  __syncthreads();
+  for (int o = threadIdx.x; o < TM * RN; o += THREADS) {
+    if (own[o / RN] < 0) continue;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) v += red[w * TM * RN + o];
+    part[o] = v;
+  }
+  cluster.sync();
+  for (int o = share * THREADS + threadIdx.x; o < TM * RN; o += shares * THREADS) {
+    const int t = o / RN, r = o % RN;
+    if (t0 + t >= P.T || r >= P.rank) continue;
+    float v = 0.0f;
+    if (own[t] >= 0) {
+      for (int k = 0; k < shares; ++k) v += cluster.map_shared_rank(part, k)[o];
+      v *= P.scale[own[t]];
+    }
+    P.h[(t0 + t) * P.rank + r] = v;
+  }
+  cluster.sync();                                  // no CTA leaves while its sums are read
 }
 
 template <int MT, int NT>
-cudaError_t launch_tile(const ShrinkParams& P, cudaStream_t stream) {
-  constexpr int BYTES = WARPS * 16 * MT * 8 * NT * 4;
+cudaError_t launch_tile(const ShrinkParams& P, int sms, cudaStream_t stream) {
+  constexpr int BYTES = (WARPS + 1) * 16 * MT * 8 * NT * 4;
   const cudaError_t e = ensure_dynamic_smem((const void*)shrink_tile_kernel<MT, NT>, BYTES);
   if (e != cudaSuccess) return e;
-  const unsigned ctas = (unsigned)((P.T + 16 * MT - 1) / (16 * MT));
-  shrink_tile_kernel<MT, NT><<<ctas, THREADS, BYTES, stream>>>(P);
-  return cudaGetLastError();
+  const long long tiles = (P.T + 16 * MT - 1) / (16 * MT);
+  // CTAs of a tile: as many as bring two to every multiprocessor and leave each at least two steps of all its warps
+  int shares = 1;
+  while (shares < 8 && tiles * shares < 2 * sms && P.K >= 2 * WARPS * 32 * 2 * shares) shares *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * shares));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = shares;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, shrink_tile_kernel<MT, NT>, P);
 }
 
 template <int MT, int NT>
@@ -339,11 +373,20 @@ cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, cons
     shrink_rows_kernel<<<dim3((unsigned)T, ad.rank / 8), THREADS, 0, stream>>>(P);
     return cudaGetLastError();
   }
-  if (ad.rank <= 8) return launch_tile<2, 1>(P, stream);
-  if (ad.rank <= 16) return launch_tile<2, 2>(P, stream);
-  if (ad.rank <= 32) return launch_tile<2, 4>(P, stream);
-  if (ad.rank <= 64) return launch_tile<2, 8>(P, stream);
-  return launch_tile<1, 16>(P, stream);
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  // Tiles of 32 rows read the adapters half as often; tiles of 16 meet fewer distinct adapters and are more.
+  if (T > 1024) {
+    if (ad.rank <= 8) return launch_tile<2, 1>(P, sms, stream);
+    if (ad.rank <= 16) return launch_tile<2, 2>(P, sms, stream);
+    if (ad.rank <= 32) return launch_tile<2, 4>(P, sms, stream);
+    if (ad.rank <= 64) return launch_tile<2, 8>(P, sms, stream);
+  }
+  if (ad.rank <= 8) return launch_tile<1, 1>(P, sms, stream);
+  if (ad.rank <= 16) return launch_tile<1, 2>(P, sms, stream);
+  if (ad.rank <= 32) return launch_tile<1, 4>(P, sms, stream);
+  if (ad.rank <= 64) return launch_tile<1, 8>(P, sms, stream);
+  return launch_tile<1, 16>(P, sms, stream);
 }
 
 cudaError_t launch_linear_small(const PackedLayer& L, const AdapterView* ad, int T, const int* row_adapter,

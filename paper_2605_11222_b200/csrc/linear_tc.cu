@@ -65,7 +65,7 @@ struct TcParams {
   const float* h;
   bf16* y;
   long long ldy;
-  int tiles_m;
+  int tiles_m, splits;                               // splits: CTAs of a cluster
   int* status;
   long long wait_limit;
   int hold_loads;
@@ -101,9 +101,9 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Waiter wait = {&abort_s, P.status, P.wait_limit};
-  const int split = (int)cluster_ctarank(), splits = gridDim.x;
-  const int tm = blockIdx.y % P.tiles_m;
-  const long long t0 = (long long)(blockIdx.y / P.tiles_m) * NT;
+  const int split = (int)cluster_ctarank(), splits = P.splits;
+  const int tile = (int)blockIdx.x / splits, tm = tile % P.tiles_m;
+  const long long t0 = (long long)(tile / P.tiles_m) * NT;
   const int m0 = tm * BM;
 
   // full: a step's operands are in place; empty: its MMAs have read them; codes landed, read; the list; the end
@@ -447,7 +447,8 @@ cudaError_t launch(TcParams& P, const bf16* x, long long ldx, const AdapterView*
   cudaError_t e = ensure_dynamic_smem((const void*)kernel, C::SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(splits, (unsigned)(P.tiles_m * ((P.T + NT - 1) / NT)));
+  P.splits = splits;
+  cfg.gridDim = dim3((unsigned)(P.tiles_m * ((P.T + NT - 1) / NT) * splits));
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = C::SMEM;
   cfg.stream = stream;
@@ -466,7 +467,7 @@ cudaError_t launch(TcParams& P, const bf16* x, long long ldx, const AdapterView*
 template <bool GRAD>
 cudaError_t dispatch(TcParams& P, const bf16* x, long long ldx, const AdapterView* ad, int nt, int splits,
                      cudaStream_t stream) {
-  if (P.tiles_m * ((P.T + nt - 1) / nt) > 65535) return cudaErrorInvalidValue;
+  if (P.tiles_m * ((P.T + nt - 1) / nt) * splits > 0x7fffffffLL) return cudaErrorInvalidValue;
   if (nt == 64) return launch<GRAD, 64>(P, x, ldx, ad, splits, stream);
   if (nt == 128) return launch<GRAD, 128>(P, x, ldx, ad, splits, stream);
   return launch<GRAD, 256>(P, x, ldx, ad, splits, stream);

@@ -30,7 +30,7 @@ constexpr int HALF = 128;                            // rows and values of a til
 constexpr int X_BYTES = HALF * BK * 2;               // 16 KB a block of rows
 constexpr int W_BYTES = HALF * BK * 2;
 constexpr int MOVE_WARPS = 4;
-constexpr int OUT_COLS = 64, OUT_BYTES = 32 * OUT_COLS * 2;   // staging of one moving warp: 32 rows x 128 bytes
+constexpr int OUT_COLS = 32, OUT_BUF = 32 * OUT_COLS * 2, OUT_BYTES = 2 * OUT_BUF;   // staging of a moving warp: 2 x 32 rows x 64 bytes
 constexpr int NONE = 0xffff;                         // row without an adapter
 
 constexpr int NMB = 2;                               // blocks of 256 rows
@@ -46,7 +46,7 @@ struct Cfg {
 struct PairParams {
   CUtensorMap rows;                                  // [T][K] bf16, box 64 x 128
   CUtensorMap out_side;                              // [n][rank][M] bf16, box 64 x box_rows x 1
-  CUtensorMap out;                                   // [T][M] bf16, box 64 x 32 (stores)
+  CUtensorMap out;                                   // [T][M] bf16, box 32 x 32 (stores)
   PackedLayer L;
   int M, K, num_kb;
   long long T;
@@ -353,11 +353,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
     }
   } else if (warp < ROLE_WARPS) {
     // ===================== finished tiles =====================
-    // A lane holds a row; 64 of its columns at a time go through a swizzled 32 x 128-byte tile in shared memory and out by
-    // a tile store.  (Stored from registers, 16 bytes of 32 rows an instruction, a 512-column tile took 18000 cycles.)
+    // A lane holds a row; 32 of its columns at a time go through one of two swizzled 32 x 64-byte tiles in shared memory
+    // and out by a tile store.  (Stored from registers, 16 bytes of 32 rows an instruction, a 512-column tile took 18000
+    // cycles, through one 32 x 128-byte tile 10700.)
     const int q = warp & 3;
     const uint32_t t_empty_leader = map_to_cta(t_empty, 0);
-    uint8_t* stage = ring_ptr + C::OUT_AT + q * OUT_BYTES + lane * 128;
+    uint8_t* stage = ring_ptr + C::OUT_AT + q * OUT_BYTES + lane * 64;
     const uint32_t stage_s = ring + C::OUT_AT + q * OUT_BYTES;
     uint32_t n = 0;
     bool ok = true;
@@ -373,31 +374,28 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
         const uint32_t taddr = tmem + b * 256u + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
         for (int c = 0; c < 256; c += OUT_COLS) {
+          const uint32_t buf = (c / OUT_COLS & 1) * OUT_BUF;
           uint32_t v[2][16];
+          tc_ld16(taddr + c, v[0]);
+          tc_ld16(taddr + c + 16, v[1]);
+          // the tile before the last has left its staging
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          tc_ld_wait();
+          __syncwarp();
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            tc_ld16(taddr + c + 32 * half, v[0]);
-            tc_ld16(taddr + c + 32 * half + 16, v[1]);
-            tc_ld_wait();
-            if (half == 0) {                         // the tile before has left the staging
-              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              __syncwarp();
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t* w = &v[e >> 1][8 * (e & 1)];
-              uint4 o;
-              o.x = float2_to_bf16x2(__uint_as_float(w[0]), __uint_as_float(w[1]));
-              o.y = float2_to_bf16x2(__uint_as_float(w[2]), __uint_as_float(w[3]));
-              o.z = float2_to_bf16x2(__uint_as_float(w[4]), __uint_as_float(w[5]));
-              o.w = float2_to_bf16x2(__uint_as_float(w[6]), __uint_as_float(w[7]));
-              *reinterpret_cast<uint4*>(stage + (((4 * half + e) ^ (lane & 7)) << 4)) = o;
-            }
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t* w = &v[e >> 1][8 * (e & 1)];
+            uint4 o;
+            o.x = float2_to_bf16x2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            o.y = float2_to_bf16x2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+            o.z = float2_to_bf16x2(__uint_as_float(w[4]), __uint_as_float(w[5]));
+            o.w = float2_to_bf16x2(__uint_as_float(w[6]), __uint_as_float(w[7]));
+            *reinterpret_cast<uint4*>(stage + buf + ((e ^ ((lane >> 1) & 3)) << 4)) = o;
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0 && t < P.T && m0 + c < P.M) {
-            store_2d(&P.out, stage_s, m0 + c, (int)t);
+          if (lane == 0) {
+            if (t < P.T && m0 + c < P.M) store_2d(&P.out, stage_s + buf, m0 + c, (int)t);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         }
@@ -541,7 +539,7 @@ cudaError_t launch(PairParams& P, const bf16* x, long long ldx, const bf16* y, l
   if (!encode_bf16(&P.rows, x, 2, xs, xst, xb)) return cudaErrorInvalidValue;
   const cuuint64_t ys[2] = {(cuuint64_t)P.M, (cuuint64_t)P.T}, yst[1] = {(cuuint64_t)ldy * 2};
   const cuuint32_t yb[2] = {OUT_COLS, 32};
-  if (!encode_bf16(&P.out, y, 2, ys, yst, yb)) return cudaErrorInvalidValue;
+  if (!encode_bf16(&P.out, y, 2, ys, yst, yb, CU_TENSOR_MAP_SWIZZLE_64B)) return cudaErrorInvalidValue;
   P.cap = P.box_rows = 1;
   if (ad) {
     P.cap = ad->rank <= BK / 2 ? BK / ad->rank : 1;

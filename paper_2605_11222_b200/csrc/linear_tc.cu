@@ -417,12 +417,12 @@ EncodeTiledFn encode_fn() {
 }  // namespace
 
 bool encode_bf16(CUtensorMap* map, const bf16* ptr, int dims, const cuuint64_t* size, const cuuint64_t* stride_bytes,
-                 const cuuint32_t* box) {
+                 const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
   const EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   const cuuint32_t one[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)dims, (void*)ptr, size, stride_bytes, box, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

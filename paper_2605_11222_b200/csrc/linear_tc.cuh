@@ -174,9 +174,9 @@ __device__ __forceinline__ void write_weights(uint8_t* tile, int u, const Weight
   for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(dst + (((ch + e) ^ sw) << 4)) = w.w[e];
 }
 
-// Row-major bf16 tensor map with 128B swizzle; sizes innermost first, strides in bytes; out of range reads as zero.
+// Row-major bf16 tensor map; sizes innermost first, strides in bytes; out of range reads as zero.
 bool encode_bf16(CUtensorMap* map, const bf16* ptr, int dims, const cuuint64_t* size, const cuuint64_t* stride_bytes,
-                 const cuuint32_t* box);
+                 const cuuint32_t* box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
 
 // ---- linear_pair.cu ----
 constexpr int PAIR_ROWS = 512, PAIR_VALUES = 256;    // tile of a pair

@@ -75,7 +75,7 @@ admmq_status admmq_adapters_check(const admmq_adapters* bank, int d_in, int d_ou
  * grad_input: u_t = scale_a up_a   dy_t,  dx_t = W^T dy_t + down_a^T u_t      dy [n_rows][lddy], dx [n_rows][lddx] bf16
  * a = d_row_adapter[t]; a value outside [0, n_adapters) means none (h_t = u_t = 0).  bank NULL: no adapters, and
  * d_row_adapter and d_h / d_u are ignored.  d_h, d_u: [n_rows][rank] fp32, outputs (the backward pass reads them).
- * One launch for up to 16 rows without adapters, two with: the second overlaps the first. */
+ * One launch without adapters, two with them, of which the second overlaps the first. */
 admmq_status admmq_linear_forward(const admmq_packed_layer* layer, const admmq_adapters* bank, long long n_rows,
                                   const int* d_row_adapter, const void* d_x, long long ldx, void* d_y, long long ldy,
                                   float* d_h, int* d_status, void* cuda_stream);

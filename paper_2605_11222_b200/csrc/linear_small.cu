@@ -1,15 +1,20 @@
 // The projection for a few rows (decoding), and the contraction of the rows with their adapters.
 //
-// linear_small: y[t][j] = sum_i x[t][i] W[j][i], up to 16 rows.  Bound: memory, half a byte a weight.  With
+// linear_small: y[t][j] = sum_i x[t][i] W[j][i], up to 16 rows.  Bound: memory, half a byte a weight, but at a few
+// megabytes the time is a chain of latencies: the launch, the loads, the products, one exchange, the store.  With
 // W = z0 + Delta k a group of input channels contributes  Delta sum k x + z0 sum x, so the tensor cores multiply the
 // codes themselves: 0x4300 | k is the bf16 number 128 + k, two codes leave a packed word per shift and mask, and
 //   y = sum over groups of  Delta (sum (128 + k) x) + (z0 - 128 Delta) sum x
-// in fp32, without a rounding of any weight.  sum x comes from a second product with a tile of ones.  (The offset
-// 128 costs 7 of the 24 bits of the fp32 sums: 2^-17 relative, under the 2^-9 of the output.)
-// A CTA of 8 warps owns 16 output channels for up to 8 rows, 32 for more (then the rows are read from L2 half as
-// often); the warps split the input channels, a warp's loads of UNROLL blocks of codes leave together, and the sums
-// meet in shared memory.  Channels are taken in an order that lets a thread read 16 of them from consecutive
-// addresses for the codes and for x alike: a product over them does not ask for their order.
+// in fp32, without a rounding of any weight.  (The offset 128 costs 7 of the 24 bits of the fp32 sums: 2^-17 relative,
+// under the 2^-8 of the output.)
+// A CTA owns 16 (or 32) output channels.  Asynchronous copies bring a slice of the rows, the codes and the grid to shared
+// memory, all of a layer of 4096 input channels at once; sixteen warps split the slice and their sums meet at the end.
+// Channels are taken in an order that lets a thread read 16 of them from consecutive addresses for the codes and for x
+// alike: a product over them does not ask for their order.  h comes from a launch of its own, which this one overlaps up
+// to its last step; the adapters' output sides are copied meanwhile.
+// The code is kept short (rolled loops, no divisions): it runs once a launch from cold instruction caches.  With the same
+// work unrolled and its loads in registers a CTA took 14000 cycles; with clusters of eight CTAs that form h themselves
+// and split the input channels it took 12700, and such a launch does not overlap the one before it.
 //
 // shrink: h[t][r] = scale_a sum_i x[t][i] in_a[r][i].  Bound: memory, one pass over the rows and over the adapters in
 // use.  Two forms: a CTA for each row and 8 ranks (a warp a rank) for few rows, and tiles of 16 or 32 rows on mma.sync
@@ -23,7 +28,7 @@ namespace cg = cooperative_groups;
 namespace admmq {
 namespace {
 
-constexpr int THREADS = 256, WARPS = 8;
+constexpr int THREADS = 256, WARPS = 8;          // of the contractions with the adapters
 
 // ------------------------------------------------------------------ few rows: the projection
 struct SmallParams {
@@ -33,141 +38,205 @@ struct SmallParams {
   bf16* y;
   long long ldy;
   int T;
+  int slice;                      // blocks of 64 input channels in shared memory at once
+  uint32_t group_inv;             // ceil(2^32 / blocks of a group); 1: a block is a group, 0: one group
+  int x_stride;                   // elements of a copied row
+  int warps_log;                  // 2^warps_log warps copy a row
+  int at_grid, at_x, at_sx, at_up;   // bytes: after the codes, the grid, the rows, the sums of x
   const bf16* up;                 // adapters' output side [n][rank][d_out], NULL: none
   const int* row_adapter;
   const float* h;                 // [T][rank]
   int n_adapters, rank;
+  bool up_copied;                 // the output sides fit in shared memory
 };
 
-// MT tiles of 16 channels, NT tiles of 8 rows.
-template <int MT, int NT>
-__global__ void __launch_bounds__(THREADS) linear_small_kernel(const __grid_constant__ SmallParams P) {
-  constexpr int UNROLL = 4;
-  __shared__ float red[WARPS][NT * 8][MT * 16 + 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int g = lane >> 2, q = lane & 3;
-  const int j0 = blockIdx.x * 16 * MT;
-  const int p = P.L.d_out, n = P.L.d_in;
-  const int ib0 = P.L.nib * warp / WARPS, ib1 = P.L.nib * (warp + 1) / WARPS;
-
-  int row[MT][2];                                  // output channels of this thread, kept inside the matrix
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
+  const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    row[m][0] = min(j0 + 16 * m + g, p - 1);
-    row[m][1] = min(j0 + 16 * m + g + 8, p - 1);
+  for (int e = 0; e < 4; ++e) {
+    const float2 x = bf16x2_to_float2(av[e]), y = bf16x2_to_float2(bv[e]);
+    s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
   }
-  float y[MT][NT][4], acc[MT][NT][4], sx[NT][4];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      sx[t][e] = 0.0f;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) y[m][t][e] = acc[m][t][e] = 0.0f;
-    }
-  const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  return s;
+}
 
-  for (int ib = ib0; ib < ib1; ib += UNROLL) {
-    uint2 code[UNROLL][MT][2];
+constexpr int MAIN_WARPS = 16, MAIN_THREADS = 32 * MAIN_WARPS;
+constexpr int SLICE_MAX = 64;                        // blocks of 64 input channels in shared memory
+constexpr int X_BYTES_MAX = 132 * 1024;              // bytes of rows in shared memory
+constexpr int UP_MAX = 128;                          // rows * rank up to which the output sides are copied
+
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {      // zeros where there is nothing
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+               "r"(in ? 16 : 0)
+               : "memory");
+}
+
+// MT tiles of 16 channels, NT tiles of 8 rows.  Shared memory: codes [block][channel][32 bytes], grid [block][channel], rows
+// [T][x_stride], sums of x [block][T], output sides [row][rank][channel]; at the end the warps' sums over the codes.
+template <int MT, int NT>
+__global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_small_kernel(const __grid_constant__ SmallParams P) {
+  constexpr int CH = 16 * MT, ROWS = 8 * NT;
+  extern __shared__ __align__(16) uint8_t work[];
+  bf16* x_s = reinterpret_cast<bf16*>(work + P.at_x);
+  float* sx = reinterpret_cast<float*>(work + P.at_sx);
+  bf16* up_s = reinterpret_cast<bf16*>(work + P.at_up);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = lane >> 2, q = lane & 3;
+  const int j0 = (int)blockIdx.x * CH;
+  const int p = P.L.d_out, n = P.L.d_in, T = P.T, rank = P.rank;
+  const int rows_in = min(CH, p - j0);                                 // output channels of the tile
+  // rows to warps, 2^warps_log to a row
+  const int my_row = warp >> P.warps_log, lanes = 32 << P.warps_log, my_lane = tid & (lanes - 1);
+
+  float y[MT][NT][4];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[m][t][e] = 0.0f;
+
+#pragma unroll 1
+  for (int ibA = 0; ibA < P.L.nib; ibA += P.slice) {
+  const int nb = min(P.slice, P.L.nib - ibA);
+  if (ibA > 0) __syncthreads();                                        // the slice before is used up
+  // ---- everything of the slice is asked for at once: rows, codes, grid
+  if (my_row < T)
+#pragma unroll 1
+    for (int c = my_lane * 8; c < nb * CODE_BLOCK; c += lanes * 8) {
+      const int i = ibA * CODE_BLOCK + c;
+      copy16(x_s + my_row * P.x_stride + c, P.x + my_row * P.ldx + (i < n ? i : 0), i < n);
+    }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll 1
+  for (int c = tid; c < nb * CH * 2; c += MAIN_THREADS) {              // 16 bytes: half a channel's block
+    const int b = c / (CH * 2), k = c % (CH * 2);
+    const bool in = (k >> 1) < rows_in;
+    copy16(work + c * 16, P.L.codes + (in ? ((long long)(ibA + b) * p + j0) * BLOCK_WORDS + k * 4 : 0), in);
+  }
+#pragma unroll 1
+  for (int c = tid; c < nb * (CH / 2); c += MAIN_THREADS) {            // 16 bytes: two channels' pairs
+    const int b = c / (CH / 2), k = c % (CH / 2);
+    const bool in = 2 * k < rows_in;                                   // d_out is a multiple of 8
+    const int ib = ibA + b, grp = P.group_inv > 1 ? (int)__umulhi((uint32_t)ib, P.group_inv) : P.group_inv ? ib : 0;
+    copy16(work + P.at_grid + c * 16, P.L.grid + (in ? (long long)grp * p + j0 + 2 * k : 0), in);
+  }
+  if (P.up_copied && ibA == 0) {
+#pragma unroll 1
+    for (int o = warp; o < T * rank; o += MAIN_WARPS) {                // a (row, rank) a warp, 8 channels a lane
+      const int t = o / rank, r = o - t * rank, a = row_adapter_of(P.row_adapter, t, P.n_adapters);
+      if (lane < CH / 8) {
+        const bool in = a >= 0 && lane * 8 < rows_in;
+        copy16(up_s + o * CH + lane * 8, P.up + (in ? ((long long)a * rank + r) * p + j0 + lane * 8 : 0), in);
+      }
+    }
+  }
+  asm volatile("cp.async.commit_group;\ncp.async.wait_group 1;" ::: "memory");
+  __syncthreads();                                 // the rows are in place: their sums over blocks, 8 threads a block
+  if (my_row < T)
+#pragma unroll 2
+    for (int c = my_lane; c < nb * 8; c += lanes) {                    // (nb 8 is a multiple of 8: whole groups of lanes)
+      const uint32_t one = 0x3f803f80u, mask = 0xffu << (lane & 24);
+      float f = dot8(*reinterpret_cast<const uint4*>(x_s + my_row * P.x_stride + c * 8), make_uint4(one, one, one, one), 0.0f);
+#pragma unroll
+      for (int d = 4; d > 0; d >>= 1) f += __shfl_xor_sync(mask, f, d);
+      if ((c & 7) == 0) sx[(c >> 3) * T + my_row] = f;
+    }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+
+  // ---- products, block by block
+#pragma unroll 1
+  for (int b = nb * warp / MAIN_WARPS; b < nb * (warp + 1) / MAIN_WARPS; ++b) {
+    float acc[MT][NT][4], s0[NT], s1[NT];          // s0, s1: sums of x of the rows 8 t + 2 q and the next
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      s0[t] = 8 * t + 2 * q < T ? sx[b * T + 8 * t + 2 * q] : 0.0f;
+      s1[t] = 8 * t + 2 * q + 1 < T ? sx[b * T + 8 * t + 2 * q + 1] : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[m][t][e] = 0.0f;
+    }
+    const uint2* cs = reinterpret_cast<const uint2*>(work) + b * (CH * 4);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {                  // 8 channels of this thread
+      uint4 xv[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        xv[t] = 8 * t + g < T ? *reinterpret_cast<const uint4*>(x_s + (8 * t + g) * P.x_stride + b * CODE_BLOCK + 16 * q + 8 * w)
+                              : make_uint4(0, 0, 0, 0);
+      uint32_t c[MT][2];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-          if (ib + u < ib1)
-            code[u][m][hh] = __ldg(reinterpret_cast<const uint2*>(
-                                       P.L.codes + ((long long)(ib + u) * p + row[m][hh]) * BLOCK_WORDS) + q);
+        for (int hh = 0; hh < 2; ++hh) c[m][hh] = reinterpret_cast<const uint32_t*>(cs + (16 * m + 8 * hh + g) * 4 + q)[w];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      if (ib + u >= ib1) break;
-      const int i = (ib + u) * CODE_BLOCK + 16 * q;
-      uint4 xv[NT][2];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const bf16* px = P.x + (long long)(8 * t + g) * P.ldx + i;
-        const bool in = 8 * t + g < P.T;
-        xv[t][0] = in && i < n ? __ldg(reinterpret_cast<const uint4*>(px)) : make_uint4(0, 0, 0, 0);
-        xv[t][1] = in && i + 8 < n ? __ldg(reinterpret_cast<const uint4*>(px) + 1) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {              // 16 channels: pairs 2 s and 2 s + 1 of the word
-          uint32_t b[NT][2];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            b[t][0] = s == 0 ? xv[t][w].x : xv[t][w].z;
-            b[t][1] = s == 0 ? xv[t][w].y : xv[t][w].w;
-          }
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const uint32_t c0 = w == 0 ? code[u][m][0].x : code[u][m][0].y;
-            const uint32_t c1 = w == 0 ? code[u][m][1].x : code[u][m][1].y;
-            const uint32_t a[4] = {((c0 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                   ((c1 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                   ((c0 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u,
-                                   ((c1 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u};
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma_bf16(acc[m][t], a, b[t][0], b[t][1]);
-          }
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mma_bf16(sx[t], ones, b[t][0], b[t][1]);
-        }
-      // the end of a group (or of this warp's share): fold its sums into y
-      const int grp = (ib + u) * CODE_BLOCK / P.L.gs;
-      if (ib + u + 1 == ib1 || (ib + u + 1) * CODE_BLOCK / P.L.gs != grp) {
+      for (int s = 0; s < 2; ++s) {                // pairs 2 s and 2 s + 1 of the word
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const float2 g0 = __ldg(P.L.grid + (long long)grp * p + row[m][0]);
-          const float2 g1 = __ldg(P.L.grid + (long long)grp * p + row[m][1]);
-          const float z0 = fmaf(-128.0f, g0.x, g0.y), z1 = fmaf(-128.0f, g1.x, g1.y);
+          const uint32_t a[4] = {((c[m][0] >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c[m][1] >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c[m][0] >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c[m][1] >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            y[m][t][0] += fmaf(g0.x, acc[m][t][0], z0 * sx[t][0]);
-            y[m][t][1] += fmaf(g0.x, acc[m][t][1], z0 * sx[t][1]);
-            y[m][t][2] += fmaf(g1.x, acc[m][t][2], z1 * sx[t][2]);
-            y[m][t][3] += fmaf(g1.x, acc[m][t][3], z1 * sx[t][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][t][e] = 0.0f;
-          }
+          for (int t = 0; t < NT; ++t) mma_bf16(acc[m][t], a, s == 0 ? xv[t].x : xv[t].z, s == 0 ? xv[t].y : xv[t].w);
         }
+      }
+    }
+    const float2* gs = reinterpret_cast<const float2*>(work + P.at_grid) + b * CH;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+    for (int m = 0; m < MT; ++m) {
+      const float2 g0 = gs[16 * m + g], g1 = gs[16 * m + 8 + g];
+      const float z0 = fmaf(-128.0f, g0.x, g0.y), z1 = fmaf(-128.0f, g1.x, g1.y);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sx[t][e] = 0.0f;
+      for (int t = 0; t < NT; ++t) {
+        y[m][t][0] += fmaf(g0.x, acc[m][t][0], z0 * s0[t]);
+        y[m][t][1] += fmaf(g0.x, acc[m][t][1], z0 * s1[t]);
+        y[m][t][2] += fmaf(g1.x, acc[m][t][2], z1 * s0[t]);
+        y[m][t][3] += fmaf(g1.x, acc[m][t][3], z1 * s1[t]);
       }
     }
   }
+  }
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(work);     // [warp][ROWS][CH + 1]
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      red[warp][8 * t + 2 * q][16 * m + g] = y[m][t][0];
-      red[warp][8 * t + 2 * q + 1][16 * m + g] = y[m][t][1];
-      red[warp][8 * t + 2 * q][16 * m + g + 8] = y[m][t][2];
-      red[warp][8 * t + 2 * q + 1][16 * m + g + 8] = y[m][t][3];
+      float* o = red + ((warp * ROWS + 8 * t + 2 * q) * (CH + 1) + 16 * m + g);
+      o[0] = y[m][t][0];
+      o[CH + 1] = y[m][t][1];
+      o[8] = y[m][t][2];
+      o[CH + 9] = y[m][t][3];
     }
   __syncthreads();
   if (P.up != nullptr) pdl_wait();                 // h is complete from here on
-  for (int o = threadIdx.x; o < P.T * 16 * MT; o += THREADS) {
-    const int t = o / (16 * MT), m = o % (16 * MT), j = j0 + m;
-    if (j >= p) continue;
+#pragma unroll 1
+  for (int o = tid; o < T * CH; o += MAIN_THREADS) {
+    const int t = o / CH, c = o % CH;
+    if (c >= rows_in) continue;
     float v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) v += red[w][t][m];
+    for (int w = 0; w < MAIN_WARPS; ++w) v += red[(w * ROWS + t) * (CH + 1) + c];
     if (P.up != nullptr) {
       const int a = row_adapter_of(P.row_adapter, t, P.n_adapters);
       if (a >= 0) {
-        const bf16* up = P.up + (long long)a * P.rank * p + j;
-        const float* h = P.h + (long long)t * P.rank;
+        const float* h = P.h + t * rank;
         float d = 0.0f;
+        if (P.up_copied) {
+#pragma unroll 4
+          for (int r = 0; r < rank; ++r) d = fmaf(h[r], __bfloat162float(up_s[(t * rank + r) * CH + c]), d);
+        } else {
+          const bf16* up = P.up + (long long)a * rank * p + j0 + c;
 #pragma unroll 8
-        for (int r = 0; r < P.rank; ++r) d = fmaf(h[r], __bfloat162float(up[(long long)r * p]), d);
+          for (int r = 0; r < rank; ++r) d = fmaf(h[r], __bfloat162float(up[(long long)r * p]), d);
+        }
         v += d;
       }
     }
-    P.y[(long long)t * P.ldy + j] = __float2bfloat16_rn(v);
+    P.y[t * P.ldy + j0 + c] = __float2bfloat16_rn(v);
   }
 }
 
@@ -182,16 +251,6 @@ struct ShrinkParams {
   const int* row_adapter;
   float* h;                       // [T][rank]
 };
-
-__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float s) {
-  const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 x = bf16x2_to_float2(av[e]), y = bf16x2_to_float2(bv[e]);
-    s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
-  }
-  return s;
-}
 
 // One row and 8 ranks a CTA, a warp a rank.
 __global__ void __launch_bounds__(THREADS) shrink_rows_kernel(const __grid_constant__ ShrinkParams P) {
@@ -349,10 +408,27 @@ cudaError_t launch_tile(const ShrinkParams& P, int sms, cudaStream_t stream) {
 }
 
 template <int MT, int NT>
-cudaError_t launch_small(const SmallParams& P, cudaStream_t stream) {
+cudaError_t launch_small(SmallParams& P, cudaStream_t stream) {
+  constexpr int CH = 16 * MT, RED = MAIN_WARPS * 8 * NT * (CH + 1) * 4;
+  P.slice = P.L.nib < SLICE_MAX ? P.L.nib : SLICE_MAX;
+  while (P.T * P.slice * CODE_BLOCK * 2 > X_BYTES_MAX) P.slice = (P.slice + 1) / 2;
+  const int group = P.L.gs == P.L.d_in ? 0 : P.L.gs / CODE_BLOCK;
+  P.group_inv = group <= 1 ? (uint32_t)group : (uint32_t)(((1ULL << 32) + group - 1) / group);
+  P.x_stride = P.slice * CODE_BLOCK + 8;
+  while (P.T << (P.warps_log + 1) <= MAIN_WARPS) ++P.warps_log;
+  P.at_grid = P.slice * CH * 32;
+  P.at_x = P.at_grid + P.slice * CH * 8;
+  P.at_sx = P.at_x + P.T * P.x_stride * 2;
+  const int after = (P.at_sx + P.T * P.slice * 4 + 15) / 16 * 16;
+  P.at_up = after > RED ? after : RED;
+  P.up_copied = P.up != nullptr && P.T * P.rank <= UP_MAX;
+  const int bytes = P.at_up + (P.up_copied ? P.T * P.rank * CH * 2 : 0);
+  const cudaError_t e = ensure_dynamic_smem((const void*)linear_small_kernel<MT, NT>, bytes);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((P.L.d_out + 16 * MT - 1) / (16 * MT));
-  cfg.blockDim = dim3(THREADS);
+  cfg.gridDim = dim3((P.L.d_out + CH - 1) / CH);
+  cfg.blockDim = dim3(MAIN_THREADS);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -392,9 +468,23 @@ cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, cons
 cudaError_t launch_linear_small(const PackedLayer& L, const AdapterView* ad, int T, const int* row_adapter,
                                 const bf16* x, long long ldx, bf16* y, long long ldy, const float* h,
                                 cudaStream_t stream) {
-  const SmallParams P = {L, x, ldx, y, ldy, T, ad ? ad->out : nullptr, row_adapter, h, ad ? ad->n : 0, ad ? ad->rank : 0};
+  SmallParams P = {};
+  P.L = L;
+  P.x = x;
+  P.ldx = ldx;
+  P.y = y;
+  P.ldy = ldy;
+  P.T = T;
+  if (ad) {
+    P.up = ad->out;
+    P.row_adapter = row_adapter;
+    P.h = h;
+    P.n_adapters = ad->n;
+    P.rank = ad->rank;
+  }
   if (T <= 8) return launch_small<1, 1>(P, stream);
-  return launch_small<2, 2>(P, stream);
+  // more rows: tiles of 32 channels read them half as often, where the layer has enough channels for that
+  return L.d_out >= 8192 ? launch_small<2, 2>(P, stream) : launch_small<1, 2>(P, stream);
 }
 
 }  // namespace admmq

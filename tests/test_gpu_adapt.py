@@ -118,6 +118,11 @@ LINEAR = [
     (65, 1024, 128, 4, 256, False, 2, 48, "mixed"),
     (128, 200, 136, 2, 0, False, 40, 8, "each"),
     (129, 4096, 520, 4, 128, False, 4, 64, "mixed"),
+    (4, 4096, 40, 3, 128, False, 3, 8, "each"),         # one launch, input channels split
+    (1, 14336, 24, 4, 64, False, 2, 32, "one"),
+    (5, 2048, 8200, 4, 64, False, 3, 56, "each"),       # two launches
+    (16, 14336, 16, 4, 256, False, 3, 16, "each"),
+    (16, 1032, 8192, 2, 0, True, 6, 16, "each"),
     (300, 1344, 1096, 3, 64, False, 70, 8, "each"),
     (520, 768, 2056, 4, 128, True, 3, 72, "none"),
     (1030, 2048, 392, 4, 0, False, 3, 16, "mixed"),

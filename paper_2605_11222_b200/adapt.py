@@ -9,6 +9,9 @@
     d_down, d_up = adapter_grads(bank, plan, kept, h, dy, u)
     q, k = qk_norm_rope(q, k, wq, wk, cos, sin, positions, eps)
 
+The common forms of the calls (new outputs, no conversion) go through the extension _adapt.so; the others, and every
+call that fails, take the path written here, which names what is wrong.
+
 torch is used for device memory and streams only; every step runs in the library's kernels, on the current stream of
 the tensors' device.  Argument errors raise AdmmqError before anything is enqueued; errors met on the device are kept in
 a status word, which `check_device_status` reads (it synchronises) and clears.
@@ -16,6 +19,7 @@ a status word, which `check_device_status` reads (it synchronises) and clears.
 from __future__ import annotations
 
 import ctypes as C
+import os
 import struct
 from typing import Optional, Sequence, Union
 
@@ -47,12 +51,17 @@ _QK_ARGS_BYTES = _QK_ARGS.size
 
 
 _lib = None
+_fast = None                      # _adapt.so: the common forms of the calls in one step each
 
 
 def _library():
-    global _lib
+    global _lib, _fast
     if _lib is None:
         lib = B.load_library()
+        if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_adapt.so")):
+            raise FileNotFoundError("_adapt.so not found: build it with `python -m paper_2605_11222_b200.build`")
+        from . import _adapt
+        _fast = _adapt
         vp, ci, cll = C.c_void_p, C.c_int, C.c_longlong
         lib.admmq_packed_bytes.restype = lib.admmq_grid_bytes.restype = C.c_size_t
         lib.admmq_qk_workspace_bytes.restype = C.c_size_t
@@ -160,6 +169,7 @@ class AdapterBank:
         self.index = down.get_device()
         self.n_adapters, self.rank, self.d_in = down.shape
         self.d_out = up.shape[2]
+        self._fits = (self.d_in, self.d_out, self.index, self.n_adapters)
         self._c = Adapters(C.sizeof(Adapters), self.n_adapters, self.rank, down.data_ptr(), up.data_ptr(),
                            scale.data_ptr())
         self._ref = C.addressof(self._c)
@@ -228,6 +238,13 @@ class Checkpoint:
 
     @classmethod
     def save(cls, x: torch.Tensor) -> "Checkpoint":
+        if _lib is None:
+            _library()
+        r = _fast.checkpoint_save(x)
+        if r.__class__ is tuple:
+            self = cls.__new__(cls)
+            self.codes, self.scale = r
+            return self
         bf16 = x.dtype is torch.bfloat16
         if x.dim() != 2 or not x.is_cuda or not (bf16 or x.dtype is torch.float32):
             _fail(B.ERR_INVALID_ARG, "Checkpoint.save: [rows, width] fp32 or bf16 on a GPU")
@@ -244,6 +261,12 @@ class Checkpoint:
 
     def restore(self, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         codes = self.codes
+        if out is None and (dtype is torch.bfloat16 or dtype is torch.float32):
+            if _lib is None:
+                _library()
+            r = _fast.checkpoint_restore(codes, self.scale, dtype is torch.bfloat16)
+            if r.__class__ is not int:
+                return r
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             _fail(B.ERR_INVALID_ARG, "Checkpoint.restore: fp32 or bf16")
         t, n = codes.shape
@@ -285,7 +308,16 @@ class QuantLinear:
         check_device_status(self.device, "admmq_pack_layer")
         self._c = PackedLayer(C.sizeof(PackedLayer), self.d_in, self.d_out, group_size, self.packed.data_ptr(),
                               self.grid.data_ptr())
-        self._ref = C.addressof(self._c)
+        self._ref, self._status = C.addressof(self._c), _status(self.index)
+
+    def _quick(self, grad, x, bank, plan):
+        """The call with new outputs; an int (a status) if the longer path has to say what is wrong."""
+        if bank is None:
+            return _fast.linear(grad, self._ref, self.d_in, self.d_out, self.index, self._status, x)
+        if plan is None or bank._fits != (self.d_in, self.d_out, self.index, plan.n_adapters) or plan.index != self.index:
+            return B.ERR_SHAPE
+        return _fast.linear(grad, self._ref, self.d_in, self.d_out, self.index, self._status, x, bank._ref, bank.rank,
+                            plan.n_rows, plan._ptr[0])
 
     def _run(self, fn, name, x, k, m, bank, plan, out, factor):
         index = self.index
@@ -318,12 +350,20 @@ class QuantLinear:
     def forward(self, x: torch.Tensor, bank: Optional[AdapterBank] = None, plan: Optional[RequestPlan] = None,
                 out: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
         """(y, h):  y_t = W x_t + up_a^T h_t,  h_t = scale_a down_a x_t (None without a bank).  x [rows, d_in] bf16."""
+        if out is None and h is None:
+            r = self._quick(False, x, bank, plan)
+            if r.__class__ is tuple:
+                return r
         return self._run((_lib or _library()).admmq_linear_forward, "admmq_linear_forward", x, self.d_in, self.d_out, bank, plan,
                          out, h)
 
     def grad_input(self, dy: torch.Tensor, bank: Optional[AdapterBank] = None, plan: Optional[RequestPlan] = None,
                    out: Optional[torch.Tensor] = None, u: Optional[torch.Tensor] = None):
         """(dx, u):  dx_t = W^T dy_t + down_a^T u_t,  u_t = scale_a up_a dy_t (None without a bank)."""
+        if out is None and u is None:
+            r = self._quick(True, dy, bank, plan)
+            if r.__class__ is tuple:
+                return r
         return self._run((_lib or _library()).admmq_linear_grad_input, "admmq_linear_grad_input", dy, self.d_out, self.d_in, bank,
                          plan, out, u)
 
@@ -333,6 +373,14 @@ def adapter_grads(bank: AdapterBank, plan: RequestPlan, x: Union[Checkpoint, tor
                   grad_up: Optional[torch.Tensor] = None):
     """(d_down, d_up), bf16 in the bank's layout: sums over an adapter's rows of u_t x_t^T and h_t dy_t^T.  x: the
     layer's input in bf16, or its Checkpoint.  An adapter without rows gets zeros."""
+    if grad_down is None and grad_up is None and plan.n_adapters == bank.n_adapters and plan.index == bank.index:
+        if _lib is None:
+            _library()
+        kept = x.__class__ is Checkpoint
+        r = _fast.adapter_grad(bank.index, plan.n_rows, plan._ptr[1], plan._ptr[2], None if kept else x,
+                               x.codes if kept else None, x.scale if kept else None, h, dy, u, bank.down, bank.up)
+        if r.__class__ is tuple:
+            return r
     index, name = bank.index, "admmq_adapter_grad"
     t, r = plan.n_rows, bank.rank
     if plan.n_adapters != bank.n_adapters:
@@ -382,6 +430,12 @@ def _heads(x, t, h, d, dt, index, name):
 
 
 def _qk(fn, name, q, k, wq, wk, cos, sin, positions, eps, dq, dk, out_q, out_k):
+    if out_q is None and out_k is None and q.is_cuda:
+        word = _status(q.get_device())
+        r = _fast.qk(word, q, k, wq, wk, cos, sin, positions, eps) if dq is None else \
+            _fast.qk(word, q, k, wq, wk, cos, sin, positions, eps, dq, dk)
+        if r.__class__ is tuple:
+            return r
     dt, index = q.dtype, q.get_device()
     bf16 = dt is torch.bfloat16
     if not q.is_cuda or not (bf16 or dt is torch.float32):

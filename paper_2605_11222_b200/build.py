@@ -1,4 +1,5 @@
-"""Builds libadmmq.so (sm_100a) next to this file:  python -m paper_2605_11222_b200.build"""
+"""Builds libadmmq.so (sm_100a) and _adapt.so, its calls from Python, next to this file:
+python -m paper_2605_11222_b200.build"""
 from __future__ import annotations
 
 import concurrent.futures
@@ -10,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadmmq.so")
+BIND = os.path.join(HERE, "_adapt.so")
 SOURCES = ["api.cu", "elem.cu", "gemm_simt.cu", "gemm_tc.cu", "tridiag.cu", "tridiag_blocked.cu", "local_search.cu", "pair_swap.cu",
            "objective_static.cu", "adapt_api.cu", "linear_small.cu", "linear_tc.cu", "linear_pair.cu", "adapter_grad.cu", "checkpoint8.cu",
            "qk_rope.cu"]
@@ -49,7 +51,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
                            capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    _build_bind(force, [h for h in headers if h.startswith(include)])
     return LIB
+
+
+def _build_bind(force: bool, headers) -> None:
+    """The Python calls of the operators (CPython and torch C++, no device code)."""
+    src = os.path.join(CSRC, "adapt_bind.cpp")
+    if not force and not _newer([src] + headers, BIND):
+        return
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           os.environ.get("CUDA_INCLUDE", "/usr/local/cuda/include"), sysconfig.get_paths()["include"]]
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                        f"-D_GLIBCXX_USE_CXX11_ABI={abi}", *[f"-I{i}" for i in inc], src, "-o", BIND, f"-L{lib}", f"-L{HERE}",
+                        "-l:libadmmq.so", "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10",
+                        "-Wl,-rpath,$ORIGIN"], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"building {BIND} failed:\n{r.stdout}\n{r.stderr}")
 
 
 if __name__ == "__main__":

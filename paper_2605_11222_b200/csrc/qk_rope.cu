@@ -9,8 +9,11 @@
 // pairs, so the rotation needs no exchange, every access is 16 bytes wide, and the sums are log2(L) shuffles away.
 // A CTA works on queries or on keys; one of its warps takes one row (token) at a time and 32 / L of its heads at once,
 // so that the weight stays in registers throughout and the rotation's cos and sin for a row.  Few rows are cut into
-// slices of heads instead.  The backward kernel's grid is the resident one: a thread sums the weight's gradient over
-// all its rows in 16 registers, the CTA's sums go to a workspace, and a second launch adds them in a fixed order.
+// slices of heads instead.  Forward a thread loads two heads (bf16) at once: 63 us for 16384 rows of 40 heads of 128, 83 % of
+// the copy rate.  Backward the grid is the resident one: a thread sums the weight's gradient over all its rows in 16
+// registers, the CTA's sums go to a workspace, and a second launch adds them in a fixed order.  That leaves few warps, so
+// what a thread needs next, up to DEPTH heads ahead and across rows, is on its way into slots of shared memory of its
+// own (asynchronous copies: no registers, no barrier); with loads into registers 8192 rows took 58 us.
 #include "adapt.h"
 
 namespace admmq {
@@ -50,6 +53,21 @@ __device__ __forceinline__ Raw8<BF16> load8(const void* base, long long at) {
   const char* p = (const char*)base + at * (BF16 ? 2 : 4);
 #pragma unroll
   for (int q = 0; q < (BF16 ? 1 : 2); ++q) r.v[q] = *reinterpret_cast<const uint4*>(p + 16 * q);
+  return r;
+}
+// 8 values into this thread's slots: 16-byte pieces, THREADS slots apart.
+template <bool BF16>
+__device__ __forceinline__ void copy8(uint32_t slot, const void* base, long long at) {
+  const char* p = (const char*)base + at * (BF16 ? 2 : 4);
+#pragma unroll
+  for (int q = 0; q < (BF16 ? 1 : 2); ++q)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot + q * THREADS * 16), "l"(p + 16 * q) : "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> slot8(const uint4* slot) {
+  Raw8<BF16> r;
+#pragma unroll
+  for (int q = 0; q < (BF16 ? 1 : 2); ++q) r.v[q] = slot[q * THREADS];
   return r;
 }
 template <bool BF16>
@@ -92,8 +110,8 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 // L threads a head (a power of two; threads past d / 16 hold nothing), UNR heads of a thread in flight.
-template <bool BF16, bool BWD, int L, int UNR>
-__global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_constant__ QkParams P) {
+template <bool BF16, int L, int UNR>
+__global__ void __launch_bounds__(THREADS, 3) qk_forward_kernel(const __grid_constant__ QkParams P) {
   constexpr int G = 32 / L;                       // heads a warp holds at once
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int l = lane % L, grp = lane / L;
@@ -118,12 +136,6 @@ __global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_c
 #pragma unroll
     for (int e = 0; e < 8; ++e) w0[e] = w1[e] = 0.0f;
   }
-  float gw[BWD ? 16 : 1];                         // sums for the weight's gradient
-  if (BWD) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) gw[BWD ? e : 0] = 0.0f;
-  }
-
   const long long items = P.T * slices;
   for (long long it = (long long)block * WARPS + warp; it < items; it += (long long)blocks * WARPS) {
     const long long t = slices == 1 ? it : it / slices;
@@ -149,7 +161,7 @@ __global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_c
     }
     // heads of this thread: slice G + grp + k step; the loop count is the warp's, so that the shuffles agree
     for (int h0 = slice * G; h0 < A.heads; h0 += UNR * step) {
-      Raw8<BF16> r0[UNR], r1[UNR], y0[BWD ? UNR : 1], y1[BWD ? UNR : 1];
+      Raw8<BF16> r0[UNR], r1[UNR];
       bool on[UNR];
 #pragma unroll
       for (int u = 0; u < UNR; ++u) {
@@ -159,14 +171,8 @@ __global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_c
           const long long at = t * A.x_row + (long long)h * A.x_head;
           r0[u] = load8<BF16>(A.x, at + o0);
           r1[u] = load8<BF16>(A.x, at + o1);
-          if (BWD) {
-            const long long ad = t * A.dy_row + (long long)h * A.dy_head;
-            y0[BWD ? u : 0] = load8<BF16>(A.dy, ad + o0);
-            y1[BWD ? u : 0] = load8<BF16>(A.dy, ad + o1);
-          }
         } else {
           r0[u] = r1[u] = Raw8<BF16>{};
-          if (BWD) y0[BWD ? u : 0] = y1[BWD ? u : 0] = Raw8<BF16>{};
         }
       }
 #pragma unroll
@@ -179,38 +185,11 @@ __global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_c
         for (int e = 0; e < 8; ++e) ss = fmaf(x0[e], x0[e], fmaf(x1[e], x1[e], ss));
         const float r = rsqrtf(fmaf(sum_lanes<L>(ss), P.inv_d, P.eps));
         float out0[8], out1[8];
-        if (!BWD) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z0 = x0[e] * r * w0[e], z1 = x1[e] * r * w1[e];
-            out0[e] = rotated ? z0 * c[e] - z1 * s[e] : z0;
-            out1[e] = rotated ? z1 * c[e] + z0 * s[e] : z1;
-          }
-        } else {
-          float d0[8], d1[8];
-          unpack8<BF16>(y0[BWD ? u : 0], d0);
-          unpack8<BF16>(y1[BWD ? u : 0], d1);
-          float dot = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float g0 = rotated ? d0[e] * c[e] + d1[e] * s[e] : d0[e];
-            const float g1 = rotated ? d1[e] * c[e] - d0[e] * s[e] : d1[e];
-            x0[e] *= r;                          // n
-            x1[e] *= r;
-            if (on[u]) {                         // (an absent head's zeros times r could be 0 * inf)
-              gw[BWD ? e : 0] = fmaf(g0, x0[e], gw[BWD ? e : 0]);
-              gw[BWD ? 8 + e : 0] = fmaf(g1, x1[e], gw[BWD ? 8 + e : 0]);
-            }
-            d0[e] = g0 * w0[e];                  // dn
-            d1[e] = g1 * w1[e];
-            dot = fmaf(d0[e], x0[e], fmaf(d1[e], x1[e], dot));
-          }
-          dot = sum_lanes<L>(held ? dot : 0.0f) * P.inv_d;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            out0[e] = r * (d0[e] - x0[e] * dot);
-            out1[e] = r * (d1[e] - x1[e] * dot);
-          }
+        for (int e = 0; e < 8; ++e) {
+          const float z0 = x0[e] * r * w0[e], z1 = x1[e] * r * w1[e];
+          out0[e] = rotated ? z0 * c[e] - z1 * s[e] : z0;
+          out1[e] = rotated ? z1 * c[e] + z0 * s[e] : z1;
         }
         if (on[u]) {
           const long long ao = t * A.out_row + (long long)(h0 + grp + u * step) * A.out_head;
@@ -220,24 +199,173 @@ __global__ void __launch_bounds__(THREADS, BWD ? 2 : 3) qk_kernel(const __grid_c
       }
     }
   }
+}
 
-  if (BWD) {
-    // this CTA's sums: lanes of equal l within the warp, then the warps in order
-    __shared__ float red[WARPS][16 * L];
+constexpr int RESIDENT = 2;                           // CTAs of the gradient that a multiprocessor holds
+template <bool BF16>
+struct Ahead {
+  static constexpr int PIECES = BF16 ? 4 : 8;         // 16-byte pieces of a head that a thread holds: x and dy
+  static constexpr int DEPTH = BF16 ? 4 : 2;
+  static constexpr int BYTES = DEPTH * PIECES * THREADS * 16;
+};
+
+// L threads a head (a power of two; threads past d / 16 hold nothing).
+template <bool BF16, int L>
+__global__ void __launch_bounds__(THREADS, RESIDENT) qk_backward_kernel(const __grid_constant__ QkParams P) {
+  using AH = Ahead<BF16>;
+  constexpr int G = 32 / L;                       // heads a warp holds at once
+  extern __shared__ uint4 slots[];                // [DEPTH][PIECES][THREADS]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int l = lane % L, grp = lane / L;
+  const bool held = l * 16 < P.d;
+  const int nrot = P.rot >> 4;
+  const bool rotated = l < nrot;
+  // runs of 8 values: the halves of the rotated pairs, or 16 consecutive values past the rotated part
+  const int o0 = rotated ? 8 * l : P.rot + 16 * (l - nrot);
+  const int o1 = rotated ? (P.rot >> 1) + 8 * l : o0 + 8;
+  const bool second = (int)blockIdx.x >= P.blocks0;
+  const Part& A = P.part[second ? 1 : 0];
+  const int slices = P.slices[second ? 1 : 0];
+  const int block = second ? blockIdx.x - P.blocks0 : blockIdx.x;
+  const int blocks = second ? gridDim.x - P.blocks0 : P.blocks0;
+  const int step = G * slices;
+
+  Raw8<BF16> wr0 = {}, wr1 = {};                  // the weight as it lies in memory (bf16: half the registers)
+  if (held) {
+    wr0 = load8<BF16>(A.w, o0);
+    wr1 = load8<BF16>(A.w, o1);
+  }
+  float gw[16];                                   // sums for the weight's gradient
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = gw[BWD ? e : 0];
-#pragma unroll
-      for (int o = L; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (grp == 0 && held) red[warp][(e < 8 ? o0 : o1) + (e & 7)] = v;
+  for (int e = 0; e < 16; ++e) gw[e] = 0.0f;
+
+  // this warp's heads: items (row, slice) it, it + stride, ...; in each slice G + grp + k step.  The position of a walk is
+  // the warp's, so that the shuffles agree.
+  const long long items = P.T * slices, stride = (long long)blocks * WARPS;
+  struct Walk {
+    long long it, t;
+    int h0;
+  };
+  auto row_of = [&](Walk& w) {
+    w.t = slices == 1 ? w.it : w.it / slices;
+    w.h0 = (int)(w.it - w.t * slices) * G;
+  };
+  auto step_on = [&](Walk& w) -> bool {           // true: at another row
+    w.h0 += step;
+    if (w.h0 < A.heads) return false;
+    w.it += stride;
+    row_of(w);
+    return true;
+  };
+  auto ask = [&](const Walk& w, uint32_t stage) {
+    if (w.it < items && held && w.h0 + grp < A.heads) {
+      const uint32_t slot = (uint32_t)__cvta_generic_to_shared(slots + stage * (AH::PIECES * THREADS) + threadIdx.x);
+      const long long at = w.t * A.x_row + (long long)(w.h0 + grp) * A.x_head;
+      constexpr int RUN = (BF16 ? 1 : 2) * THREADS * 16;
+      copy8<BF16>(slot, A.x, at + o0);
+      copy8<BF16>(slot + RUN, A.x, at + o1);
+      const long long ad = w.t * A.dy_row + (long long)(w.h0 + grp) * A.dy_head;
+      copy8<BF16>(slot + 2 * RUN, A.dy, ad + o0);
+      copy8<BF16>(slot + 3 * RUN, A.dy, ad + o1);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < P.d; i += THREADS) {
-      float v = 0.0f;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  Walk now = {(long long)block * WARPS + warp, 0, 0};
+  row_of(now);
+  Walk next = now;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) v += red[w][i];
-      P.partial[(long long)blockIdx.x * P.d + i] = v;
+  for (int k = 0; k < AH::DEPTH - 1; ++k) {
+    ask(next, k);
+    step_on(next);
+  }
+  uint32_t stage = 0;
+  bool fresh = true;                              // a row whose angles are not here yet
+  float c[8], s[8];
+  while (now.it < items) {
+    ask(next, stage == 0 ? AH::DEPTH - 1 : stage - 1);     // into the slots read last
+    step_on(next);
+    if (fresh) {
+      if (rotated) {
+        long long pos = P.pos[now.t];
+        if ((unsigned long long)pos >= (unsigned long long)P.n_positions) {
+          raise_status(P.status, ADMMQ_ERR_SHAPE);
+          pos = 0;
+        }
+        const float4* pc = reinterpret_cast<const float4*>(P.cos + pos * (P.rot >> 1) + 8 * l);
+        const float4* ps = reinterpret_cast<const float4*>(P.sin + pos * (P.rot >> 1) + 8 * l);
+        const float4 c0 = __ldg(pc), c1 = __ldg(pc + 1), s0 = __ldg(ps), s1 = __ldg(ps + 1);
+        c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+        s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          c[e] = 1.0f;
+          s[e] = 0.0f;
+        }
+      }
     }
+    asm volatile("cp.async.wait_group %0;" ::"n"(AH::DEPTH - 1) : "memory");
+    const bool on = held && now.h0 + grp < A.heads;
+    const uint4* mine = slots + stage * (AH::PIECES * THREADS) + threadIdx.x;
+    constexpr int RUN = (BF16 ? 1 : 2) * THREADS;
+    float x0[8], x1[8], out0[8], out1[8], w0[8], w1[8];
+    unpack8<BF16>(on ? slot8<BF16>(mine) : Raw8<BF16>{}, x0);
+    unpack8<BF16>(on ? slot8<BF16>(mine + RUN) : Raw8<BF16>{}, x1);
+    float ss = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(x0[e], x0[e], fmaf(x1[e], x1[e], ss));
+    const float r = rsqrtf(fmaf(sum_lanes<L>(ss), P.inv_d, P.eps));
+    unpack8<BF16>(wr0, w0);
+    unpack8<BF16>(wr1, w1);
+    float d0[8], d1[8];
+    unpack8<BF16>(on ? slot8<BF16>(mine + 2 * RUN) : Raw8<BF16>{}, d0);
+    unpack8<BF16>(on ? slot8<BF16>(mine + 3 * RUN) : Raw8<BF16>{}, d1);
+    float dot = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float g0 = rotated ? d0[e] * c[e] + d1[e] * s[e] : d0[e];
+      const float g1 = rotated ? d1[e] * c[e] - d0[e] * s[e] : d1[e];
+      x0[e] *= r;                              // n
+      x1[e] *= r;
+      if (on) {                                // (an absent head's zeros times r could be 0 * inf)
+        gw[e] = fmaf(g0, x0[e], gw[e]);
+        gw[8 + e] = fmaf(g1, x1[e], gw[8 + e]);
+      }
+      d0[e] = g0 * w0[e];                      // dn
+      d1[e] = g1 * w1[e];
+      dot = fmaf(d0[e], x0[e], fmaf(d1[e], x1[e], dot));
+    }
+    dot = sum_lanes<L>(held ? dot : 0.0f) * P.inv_d;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      out0[e] = r * (d0[e] - x0[e] * dot);
+      out1[e] = r * (d1[e] - x1[e] * dot);
+    }
+    if (on) {
+      const long long ao = now.t * A.out_row + (long long)(now.h0 + grp) * A.out_head;
+      store8<BF16>(A.out, ao + o0, out0);
+      store8<BF16>(A.out, ao + o1, out1);
+    }
+    fresh = step_on(now);
+    if (++stage == AH::DEPTH) stage = 0;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // this CTA's sums: lanes of equal l within the warp, then the warps in order
+  __shared__ float red[WARPS][16 * L];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float v = gw[e];
+#pragma unroll
+    for (int o = L; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (grp == 0 && held) red[warp][(e < 8 ? o0 : o1) + (e & 7)] = v;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < P.d; i += THREADS) {
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) v += red[w][i];
+    P.partial[(long long)blockIdx.x * P.d + i] = v;
   }
 }
 
@@ -270,9 +398,17 @@ qk_weight_grad_kernel(const float* __restrict__ partial, int blocks0, int blocks
   }
 }
 
-template <bool BF16, bool BWD, int L>
-void launch_l(const QkParams& P, int blocks, cudaStream_t stream) {
-  qk_kernel<BF16, BWD, L, (BF16 && !BWD ? 2 : 1)><<<blocks, THREADS, 0, stream>>>(P);
+template <bool BF16, int L>
+cudaError_t launch_l(const QkParams& P, bool backward, int blocks, cudaStream_t stream) {
+  if (backward) {
+    constexpr int BYTES = Ahead<BF16>::BYTES;
+    const cudaError_t e = ensure_dynamic_smem((const void*)qk_backward_kernel<BF16, L>, BYTES);
+    if (e != cudaSuccess) return e;
+    qk_backward_kernel<BF16, L><<<blocks, THREADS, BYTES, stream>>>(P);
+  } else {
+    qk_forward_kernel<BF16, L, (BF16 ? 2 : 1)><<<blocks, THREADS, 0, stream>>>(P);
+  }
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -299,39 +435,43 @@ cudaError_t launch_qk(const admmq_qk_args& a, bool backward, cudaStream_t stream
   int L = 1;
   while (L * 16 < a.head_dim) L *= 2;
   const int G = 32 / L;
-  // Whole rows a warp while there are enough rows to give every multiprocessor 16 warps; below that a row is cut, to
-  // the point where a thread holds one head.  CTAs: the work's, and for the backward kernel at most the two an SM
-  // holds, shared out by the number of heads.
-  const long long want = (long long)sms * 16;
+  // Forward: whole rows a warp while there are enough rows to give every multiprocessor 16 warps; below that a row is cut,
+  // to the point where a thread holds one head.  Backward: at most the resident CTAs, shared out by the number of heads,
+  // and rows cut until a warp has a dozen pieces (with four or five whole rows the slowest warp takes a sixth longer than
+  // the mean).
+  const bool bf = a.dtype == ADMMQ_BF16;
+  const int heads[2] = {a.q_heads, a.k_heads};
   long long n[2] = {0, 0};
   for (int q = 0; q < 2; ++q) {
-    const int heads = q == 0 ? a.q_heads : a.k_heads, most = (heads + G - 1) / G;
+    P.slices[q] = 1;
+    if (heads[q] == 0) continue;
+    long long cap = 0x3fffffffLL, want = (long long)sms * 16;
+    if (backward) {
+      const long long ctas = RESIDENT * sms < QK_GRAD_BLOCKS ? RESIDENT * sms : QK_GRAD_BLOCKS;
+      cap = ctas * heads[q] / (heads[0] + heads[1]);
+      cap = cap < 1 ? 1 : q == 0 && heads[1] > 0 && cap == ctas ? ctas - 1 : cap;
+      want = cap * WARPS * 12;
+    }
+    const int most = (heads[q] + G - 1) / G;
     const long long sl = a.n_rows > 0 ? (want + a.n_rows - 1) / a.n_rows : 1;
-    P.slices[q] = (int)(sl > most ? (most > 0 ? most : 1) : sl);
-    n[q] = heads > 0 ? (a.n_rows * P.slices[q] + WARPS - 1) / WARPS : 0;
-  }
-  if (backward) {
-    const int cap = 2 * sms < QK_GRAD_BLOCKS ? 2 * sms : QK_GRAD_BLOCKS, heads = a.q_heads + a.k_heads;
-    int c1 = a.k_heads > 0 ? (int)((long long)cap * a.k_heads / heads) : 0;
-    if (a.k_heads > 0 && c1 < 1) c1 = 1;
-    const int c0 = cap - c1 > 0 ? cap - c1 : 1;
-    n[0] = n[0] < c0 ? n[0] : c0;
-    n[1] = n[1] < c1 ? n[1] : c1;
+    P.slices[q] = (int)(sl > most ? most : sl);
+    n[q] = (a.n_rows * P.slices[q] + WARPS - 1) / WARPS;
+    if (!backward && n[q] > cap) return cudaErrorInvalidValue;
+    n[q] = n[q] < cap ? n[q] : cap;
   }
   P.blocks0 = (int)n[0];
   const long long blocks = n[0] + n[1];
-  if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
-  const bool bf = a.dtype == ADMMQ_BF16;
   if (blocks > 0) {
-#define QK_CASE(LL)                                                                     \
-  case LL:                                                                              \
-    if (bf) backward ? launch_l<true, true, LL>(P, (int)blocks, stream) : launch_l<true, false, LL>(P, (int)blocks, stream); \
-    else backward ? launch_l<false, true, LL>(P, (int)blocks, stream) : launch_l<false, false, LL>(P, (int)blocks, stream);  \
+    cudaError_t e = cudaSuccess;
+#define QK_CASE(LL)                                                                                                   \
+  case LL:                                                                                                            \
+    e = bf ? launch_l<true, LL>(P, backward, (int)blocks, stream) : launch_l<false, LL>(P, backward, (int)blocks, stream);        \
     break;
     switch (L) {
       QK_CASE(1) QK_CASE(2) QK_CASE(4) QK_CASE(8) QK_CASE(16)
     }
 #undef QK_CASE
+    if (e != cudaSuccess) return e;
   }
   if (backward) {
     const dim3 grid((a.head_dim + 31) / 32, 2);

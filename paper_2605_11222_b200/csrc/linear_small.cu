@@ -17,7 +17,7 @@
 // and split the input channels it took 12700, and such a launch does not overlap the one before it.
 //
 // shrink: h[t][r] = scale_a sum_i x[t][i] in_a[r][i].  Bound: memory, one pass over the rows and over the adapters in
-// use.  Two forms: a CTA for each row and 8 ranks (a warp a rank) for few rows, and tiles of 16 or 32 rows on mma.sync
+// use.  Two forms: a CTA for each row and two ranks for few rows, and tiles of 16 or 32 rows on mma.sync
 // for more, where the passes over a tile are one per distinct adapter in it.
 #include <cooperative_groups.h>
 
@@ -252,31 +252,37 @@ struct ShrinkParams {
   float* h;                       // [T][rank]
 };
 
-// One row and 8 ranks a CTA, a warp a rank.
+// One row and two ranks a CTA, four warps a rank: 4096 channels are four loads of a thread for the row and four for the
+// adapter, all under way at once.  (A warp a rank made four rounds of them, 5.2 us for one row, and the projection's last
+// step waits for it.)
 __global__ void __launch_bounds__(THREADS) shrink_rows_kernel(const __grid_constant__ ShrinkParams P) {
   pdl_launch();
+  __shared__ float part[WARPS];
   const long long t = blockIdx.x;
-  const int r = blockIdx.y * WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
+  const int r = blockIdx.y * 2 + half, first = (threadIdx.x & 127) * 8;
+  const bf16* x = P.x + t * P.ldx;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
   const int a = row_adapter_of(P.row_adapter, t, P.n);
+  const bf16* m = P.mat + ((long long)(a < 0 ? 0 : a) * P.rank + r) * P.K;
   float v = 0.0f;
-  if (a >= 0) {
-    const bf16* x = P.x + t * P.ldx;
-    const bf16* m = P.mat + ((long long)a * P.rank + r) * P.K;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = lane * 8; i < P.K; i += 4 * 256) {
-      uint4 xv[4], mv[4];
+#pragma unroll 1
+  for (int i = first; i < P.K; i += 4 * 1024) {
+    uint4 xv[4], mv[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const bool in = i + 256 * u < P.K;
-        xv[u] = in ? __ldg(reinterpret_cast<const uint4*>(x + i + 256 * u)) : make_uint4(0, 0, 0, 0);
-        mv[u] = in ? __ldg(reinterpret_cast<const uint4*>(m + i + 256 * u)) : make_uint4(0, 0, 0, 0);
-      }
+    for (int u = 0; u < 4; ++u) xv[u] = i + 1024 * u < P.K ? __ldg(reinterpret_cast<const uint4*>(x + i + 1024 * u)) : zero;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] = dot8(xv[u], mv[u], s[u]);
-    }
-    v = warp_sum((s[0] + s[1]) + (s[2] + s[3])) * P.scale[a];
+    for (int u = 0; u < 4; ++u) mv[u] = i + 1024 * u < P.K ? __ldg(reinterpret_cast<const uint4*>(m + i + 1024 * u)) : zero;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v = dot8(xv[u], mv[u], v);
   }
-  if (lane == 0) P.h[t * P.rank + r] = v;
+  v = warp_sum(v);
+  if (lane == 0) part[warp] = v;
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const float* s = part + 4 * threadIdx.x;
+    P.h[t * P.rank + blockIdx.y * 2 + threadIdx.x] = a >= 0 ? ((s[0] + s[1]) + (s[2] + s[3])) * P.scale[a] : 0.0f;
+  }
 }
 
 // Tiles of 16 MT rows and 8 NT ranks.  A cluster shares a tile: its CTAs, and the warps in them, split the contracted
@@ -446,7 +452,7 @@ cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, cons
                           const int* row_adapter, float* h, cudaStream_t stream) {
   const ShrinkParams P = {x, ldx, T, K, ad.in, ad.scale, ad.n, ad.rank, row_adapter, h};
   if (T <= SHRINK_ROWS_MAX) {
-    shrink_rows_kernel<<<dim3((unsigned)T, ad.rank / 8), THREADS, 0, stream>>>(P);
+    shrink_rows_kernel<<<dim3((unsigned)T, ad.rank / 2), THREADS, 0, stream>>>(P);
     return cudaGetLastError();
   }
   const int sms = device_sms();

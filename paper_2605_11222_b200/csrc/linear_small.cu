@@ -41,7 +41,7 @@ struct SmallParams {
   int slice;                      // blocks of 64 input channels in shared memory at once
   uint32_t group_inv;             // ceil(2^32 / blocks of a group); 1: a block is a group, 0: one group
   int x_stride;                   // elements of a copied row
-  int warps_log;                  // 2^warps_log warps copy a row
+  int warps_log, out_log;         // 2^warps_log warps copy a row, 2^out_log lanes finish an output
   int at_grid, at_x, at_sx, at_up;   // bytes: after the codes, the grid, the rows, the sums of x
   const bf16* up;                 // adapters' output side [n][rank][d_out], NULL: none
   const int* row_adapter;
@@ -77,6 +77,7 @@ template <int MT, int NT>
 __global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_small_kernel(const __grid_constant__ SmallParams P) {
   constexpr int CH = 16 * MT, ROWS = 8 * NT;
   extern __shared__ __align__(16) uint8_t work[];
+  __shared__ int own[ROWS];                                            // adapters of the rows, -1: none
   bf16* x_s = reinterpret_cast<bf16*>(work + P.at_x);
   float* sx = reinterpret_cast<float*>(work + P.at_sx);
   bf16* up_s = reinterpret_cast<bf16*>(work + P.at_up);
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_smal
   const int j0 = (int)blockIdx.x * CH;
   const int p = P.L.d_out, n = P.L.d_in, T = P.T, rank = P.rank;
   const int rows_in = min(CH, p - j0);                                 // output channels of the tile
+  if (tid < ROWS) own[tid] = P.up != nullptr && tid < T ? row_adapter_of(P.row_adapter, tid, P.n_adapters) : -1;
   // rows to warps, 2^warps_log to a row
   const int my_row = warp >> P.warps_log, lanes = 32 << P.warps_log, my_lane = tid & (lanes - 1);
 
@@ -146,97 +148,99 @@ __global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_smal
   __syncthreads();
 
   // ---- products, block by block
+  const int b0 = nb * warp / MAIN_WARPS;
+  const uint2* cs = reinterpret_cast<const uint2*>(work) + (b0 * CH + g) * 4 + q;
+  const float2* gs = reinterpret_cast<const float2*>(work + P.at_grid) + b0 * CH + g;
+  const bf16* xp = x_s + g * P.x_stride + b0 * CODE_BLOCK + 16 * q;
+  const float* sp = sx + b0 * T + 2 * q;
 #pragma unroll 1
-  for (int b = nb * warp / MAIN_WARPS; b < nb * (warp + 1) / MAIN_WARPS; ++b) {
-    float acc[MT][NT][4], s0[NT], s1[NT];          // s0, s1: sums of x of the rows 8 t + 2 q and the next
+  for (int b = nb * (warp + 1) / MAIN_WARPS - b0; b > 0; --b) {
+    float acc[MT][NT][4];
+    uint4 xv[NT][2];
+    uint2 c[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) c[m][hh] = cs[(16 * m + 8 * hh) * 4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      s0[t] = 8 * t + 2 * q < T ? sx[b * T + 8 * t + 2 * q] : 0.0f;
-      s1[t] = 8 * t + 2 * q + 1 < T ? sx[b * T + 8 * t + 2 * q + 1] : 0.0f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[m][t][e] = 0.0f;
-    }
-    const uint2* cs = reinterpret_cast<const uint2*>(work) + b * (CH * 4);
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {                  // 8 channels of this thread
-      uint4 xv[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        xv[t] = 8 * t + g < T ? *reinterpret_cast<const uint4*>(x_s + (8 * t + g) * P.x_stride + b * CODE_BLOCK + 16 * q + 8 * w)
-                              : make_uint4(0, 0, 0, 0);
-      uint32_t c[MT][2];
+      xv[t][0] = xv[t][1] = make_uint4(0, 0, 0, 0);
+      if (8 * t + g < T) {
+        xv[t][0] = *reinterpret_cast<const uint4*>(xp + 8 * t * P.x_stride);
+        xv[t][1] = *reinterpret_cast<const uint4*>(xp + 8 * t * P.x_stride + 8);
+      }
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) c[m][hh] = reinterpret_cast<const uint32_t*>(cs + (16 * m + 8 * hh + g) * 4 + q)[w];
+        for (int e = 0; e < 4; ++e) acc[m][t][e] = 0.0f;
+    }
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {                // pairs 2 s and 2 s + 1 of the word
+    for (int w = 0; w < 2; ++w)                    // 8 channels of this thread
+#pragma unroll
+      for (int s = 0; s < 2; ++s)                  // pairs 2 s and 2 s + 1 of the word
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const uint32_t a[4] = {((c[m][0] >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c[m][1] >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c[m][0] >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c[m][1] >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u};
+          const uint32_t c0 = w == 0 ? c[m][0].x : c[m][0].y, c1 = w == 0 ? c[m][1].x : c[m][1].y;
+          const uint32_t a[4] = {((c0 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c1 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c0 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u,
+                                 ((c1 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma_bf16(acc[m][t], a, s == 0 ? xv[t].x : xv[t].z, s == 0 ? xv[t].y : xv[t].w);
+          for (int t = 0; t < NT; ++t)
+            mma_bf16(acc[m][t], a, s == 0 ? xv[t][w].x : xv[t][w].z, s == 0 ? xv[t][w].y : xv[t][w].w);
         }
+    // the block's share of y; s0, s1: sums of x of the rows 8 t + 2 q and the next
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float s0 = 8 * t + 2 * q < T ? sp[8 * t] : 0.0f, s1 = 8 * t + 2 * q + 1 < T ? sp[8 * t + 1] : 0.0f;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const float2 g0 = gs[16 * m], g1 = gs[16 * m + 8];
+        const float z0 = fmaf(-128.0f, g0.x, g0.y), z1 = fmaf(-128.0f, g1.x, g1.y);
+        y[m][t][0] = fmaf(g0.x, acc[m][t][0], fmaf(z0, s0, y[m][t][0]));
+        y[m][t][1] = fmaf(g0.x, acc[m][t][1], fmaf(z0, s1, y[m][t][1]));
+        y[m][t][2] = fmaf(g1.x, acc[m][t][2], fmaf(z1, s0, y[m][t][2]));
+        y[m][t][3] = fmaf(g1.x, acc[m][t][3], fmaf(z1, s1, y[m][t][3]));
       }
     }
-    const float2* gs = reinterpret_cast<const float2*>(work + P.at_grid) + b * CH;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const float2 g0 = gs[16 * m + g], g1 = gs[16 * m + 8 + g];
-      const float z0 = fmaf(-128.0f, g0.x, g0.y), z1 = fmaf(-128.0f, g1.x, g1.y);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        y[m][t][0] += fmaf(g0.x, acc[m][t][0], z0 * s0[t]);
-        y[m][t][1] += fmaf(g0.x, acc[m][t][1], z0 * s1[t]);
-        y[m][t][2] += fmaf(g1.x, acc[m][t][2], z1 * s0[t]);
-        y[m][t][3] += fmaf(g1.x, acc[m][t][3], z1 * s1[t]);
-      }
-    }
+    cs += CH * 4;
+    gs += CH;
+    xp += CODE_BLOCK;
+    sp += T;
   }
   }
   __syncthreads();
-  float* red = reinterpret_cast<float*>(work);     // [warp][ROWS][CH + 1]
+  float* red = reinterpret_cast<float*>(work);     // [row][channel][17 warps]
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      float* o = red + ((warp * ROWS + 8 * t + 2 * q) * (CH + 1) + 16 * m + g);
+      float* o = red + ((8 * t + 2 * q) * CH + 16 * m + g) * (MAIN_WARPS + 1) + warp;
       o[0] = y[m][t][0];
-      o[CH + 1] = y[m][t][1];
-      o[8] = y[m][t][2];
-      o[CH + 9] = y[m][t][3];
+      o[CH * (MAIN_WARPS + 1)] = y[m][t][1];
+      o[8 * (MAIN_WARPS + 1)] = y[m][t][2];
+      o[(CH + 8) * (MAIN_WARPS + 1)] = y[m][t][3];
     }
   __syncthreads();
   if (P.up != nullptr) pdl_wait();                 // h is complete from here on
+  // ---- 2^out_log lanes an output, the warps' sums and the ranks shared out among them
+  const int lanes_out = 1 << P.out_log, sub = lane & (lanes_out - 1);
 #pragma unroll 1
-  for (int o = tid; o < T * CH; o += MAIN_THREADS) {
-    const int t = o / CH, c = o % CH;
-    if (c >= rows_in) continue;
+  for (int o = tid >> P.out_log; o < T * CH; o += MAIN_THREADS >> P.out_log) {
+    const int t = o / CH, c = o % CH, a = own[t];
     float v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < MAIN_WARPS; ++w) v += red[(w * ROWS + t) * (CH + 1) + c];
-    if (P.up != nullptr) {
-      const int a = row_adapter_of(P.row_adapter, t, P.n_adapters);
-      if (a >= 0) {
-        const float* h = P.h + t * rank;
-        float d = 0.0f;
-        if (P.up_copied) {
 #pragma unroll 4
-          for (int r = 0; r < rank; ++r) d = fmaf(h[r], __bfloat162float(up_s[(t * rank + r) * CH + c]), d);
-        } else {
-          const bf16* up = P.up + (long long)a * rank * p + j0 + c;
-#pragma unroll 8
-          for (int r = 0; r < rank; ++r) d = fmaf(h[r], __bfloat162float(up[(long long)r * p]), d);
-        }
-        v += d;
-      }
+    for (int w = sub; w < MAIN_WARPS; w += lanes_out) v += red[o * (MAIN_WARPS + 1) + w];
+    if (a >= 0 && c < rows_in) {
+      const bf16* up = P.up_copied ? up_s + t * rank * CH + c : P.up + (long long)a * rank * p + j0 + c;
+      const long long ld = P.up_copied ? CH : p;
+#pragma unroll 4
+      for (int r = sub; r < rank; r += lanes_out) v = fmaf(P.h[t * rank + r], __bfloat162float(up[r * ld]), v);
     }
-    P.y[t * P.ldy + j0 + c] = __float2bfloat16_rn(v);
+    const uint32_t mask = lanes_out == 32 ? 0xffffffffu : ((1u << lanes_out) - 1u) << (lane & -lanes_out);
+#pragma unroll 1
+    for (int d = lanes_out >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(mask, v, d);
+    if (sub == 0 && c < rows_in) P.y[t * P.ldy + j0 + c] = __float2bfloat16_rn(v);
   }
 }
 
@@ -415,13 +419,14 @@ cudaError_t launch_tile(const ShrinkParams& P, int sms, cudaStream_t stream) {
 
 template <int MT, int NT>
 cudaError_t launch_small(SmallParams& P, cudaStream_t stream) {
-  constexpr int CH = 16 * MT, RED = MAIN_WARPS * 8 * NT * (CH + 1) * 4;
+  constexpr int CH = 16 * MT, RED = 8 * NT * CH * (MAIN_WARPS + 1) * 4;
   P.slice = P.L.nib < SLICE_MAX ? P.L.nib : SLICE_MAX;
   while (P.T * P.slice * CODE_BLOCK * 2 > X_BYTES_MAX) P.slice = (P.slice + 1) / 2;
   const int group = P.L.gs == P.L.d_in ? 0 : P.L.gs / CODE_BLOCK;
   P.group_inv = group <= 1 ? (uint32_t)group : (uint32_t)(((1ULL << 32) + group - 1) / group);
   P.x_stride = P.slice * CODE_BLOCK + 8;
   while (P.T << (P.warps_log + 1) <= MAIN_WARPS) ++P.warps_log;
+  while (P.out_log < 4 && P.T * CH << (P.out_log + 1) <= MAIN_THREADS) ++P.out_log;
   P.at_grid = P.slice * CH * 32;
   P.at_x = P.at_grid + P.slice * CH * 8;
   P.at_sx = P.at_x + P.T * P.x_stride * 2;

@@ -60,11 +60,18 @@ long long rows_of(const Tensor& t, long long width, int index) {
   need(t.size(1) == width && (t.size(0) == 0 || t.stride(1) == 1), ADMMQ_ERR_SHAPE);
   return t.size(0) > 1 ? t.stride(0) : width;
 }
-PyObject* pair(const Tensor& a, const Tensor& b) {
-  PyObject* r = PyTuple_New(2);
-  if (!r) return nullptr;
-  PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(a));
-  PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(b));
+// A tuple of tensors; an undefined one is None.
+PyObject* tuple_of(std::initializer_list<Tensor> tensors) {
+  PyObject* r = PyTuple_New(static_cast<Py_ssize_t>(tensors.size()));
+  Py_ssize_t i = 0;
+  for (const Tensor& t : tensors) {
+    PyObject* o = r ? THPVariable_Wrap(t) : nullptr;       // (an undefined tensor wraps as None)
+    if (!o) {
+      Py_XDECREF(r);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(r, i++, o);
+  }
   return r;
 }
 PyObject* status_of(const Refused& r) {
@@ -92,19 +99,14 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const int st = call(layer, nullptr, t, nullptr, x.const_data_ptr(), ld, y.mutable_data_ptr(), m, nullptr, status,
                           on_device.stream);
       need(st == ADMMQ_OK, st);
-      PyObject* r = PyTuple_New(2);
-      if (!r) return nullptr;
-      PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(y));
-      Py_INCREF(Py_None);
-      PyTuple_SET_ITEM(r, 1, Py_None);
-      return r;
+      return tuple_of({y, Tensor()});
     }
     need(integer(a[9]) == t, ADMMQ_ERR_SHAPE);
     const Tensor h = make({t, integer(a[8])}, at::kFloat, index);
     const int st = call(layer, pointer<const admmq_adapters>(a[7]), t, pointer<const int>(a[10]), x.const_data_ptr(), ld,
                         y.mutable_data_ptr(), m, static_cast<float*>(h.mutable_data_ptr()), status, on_device.stream);
     need(st == ADMMQ_OK, st);
-    return pair(y, h);
+    return tuple_of({y, h});
   } catch (const Refused& r) {
     return status_of(r);
   }
@@ -155,7 +157,7 @@ PyObject* adapter_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.d_grad_up = gu.mutable_data_ptr();
     const int st = admmq_adapter_grad(&g, on_device.stream);
     need(st == ADMMQ_OK, st);
-    return pair(gd, gu);
+    return tuple_of({gd, gu});
   } catch (const Refused& r) {
     return status_of(r);
   }
@@ -179,7 +181,7 @@ PyObject* checkpoint_save(PyObject*, PyObject* o) {
                                          t > 1 ? x.stride(0) : n, static_cast<signed char*>(codes.mutable_data_ptr()),
                                          static_cast<float*>(scale.mutable_data_ptr()), on_device.stream);
     need(st == ADMMQ_OK, st);
-    return pair(codes, scale);
+    return tuple_of({codes, scale});
   } catch (const Refused& r) {
     return status_of(r);
   }
@@ -271,7 +273,7 @@ PyObject* qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!back) {
       const int st = admmq_qk_norm_rope(&g, on_device.stream);
       need(st == ADMMQ_OK, st);
-      return pair(oq, ok);
+      return tuple_of({oq, ok});
     }
     const Tensor &dq = tensor(a[9]), &dk = tensor(a[10]);
     heads_of(dq, t, hq, d, type, index, &g.dy_q_row, &g.dy_q_head);
@@ -287,13 +289,7 @@ PyObject* qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g.d_workspace = work.mutable_data_ptr();
     const int st = admmq_qk_norm_rope_backward(&g, on_device.stream);
     need(st == ADMMQ_OK, st);
-    PyObject* r = PyTuple_New(4);
-    if (!r) return nullptr;
-    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(oq));
-    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(ok));
-    PyTuple_SET_ITEM(r, 2, THPVariable_Wrap(gq));
-    PyTuple_SET_ITEM(r, 3, THPVariable_Wrap(gk));
-    return r;
+    return tuple_of({oq, ok, gq, gk});
   } catch (const Refused& r) {
     return status_of(r);
   }

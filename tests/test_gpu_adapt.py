@@ -253,7 +253,7 @@ def test_adapter_grads_are_the_same_bits_every_time():
         assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
-@pytest.mark.parametrize("T", [11, 150])
+@pytest.mark.parametrize("T", [11, 150, 13000])
 def test_gradients_agree_with_differences(T):
     """The output is linear in x and in each adapter matrix, so a difference over any step is the derivative; what is left
     is the rounding of the outputs to bf16, EPS |y| each with independent signs."""
@@ -286,10 +286,11 @@ def test_gradients_agree_with_differences(T):
         assert abs(got - want) <= noise, (name, float(got), float(want), float(noise))
 
 
-def test_strided_rows_outputs_and_another_stream():
+@pytest.mark.parametrize("T", [9, 37, 20000])                  # one form of the projection each
+def test_strided_rows_outputs_and_another_stream(T):
     from paper_2605_11222_b200 import adapt
     g = _gen(5)
-    n, p, T = 256, 136, 37
+    n, p = 256, 136
     codes, scale, zero = _layer(g, n, p, 3, 64)
     layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 3, 64), _bank(g, 2, 8, n, p), _plan("mixed", T, 2, 1)
     big = _randn(g, T, n + 24).bfloat16()
@@ -310,7 +311,7 @@ def test_strided_rows_outputs_and_another_stream():
     assert torch.equal(y, y2) and torch.equal(h, h2)
 
 
-@pytest.mark.parametrize("T", [5, 40])
+@pytest.mark.parametrize("T", [5, 40, 20000])
 def test_forward_in_a_cuda_graph(T):
     from paper_2605_11222_b200 import adapt
     g = _gen(6)
@@ -331,7 +332,7 @@ def test_forward_in_a_cuda_graph(T):
     assert torch.equal(y, want)
 
 
-@pytest.mark.parametrize("T", [6, 50])
+@pytest.mark.parametrize("T", [6, 50, 40000])
 def test_a_bad_row_stays_in_its_row(T):
     """A NaN or infinity in one row's input does not reach another row, whatever adapters they have."""
     from paper_2605_11222_b200 import adapt
@@ -601,3 +602,16 @@ def test_qk_refusals_and_positions_out_of_range():
         adapt.check_device_status(DEV)
     assert e.value.status == B.ERR_SHAPE
     adapt.check_device_status(DEV)
+
+
+def test_the_example_trains_its_adapters():
+    """The operators together, as the example uses them: the loss falls (the gradients point the right way through the
+    rotation, the norm, the codes and the 8-bit inputs), and a request without an adapter gets the bare layer."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import adapt_attention_input as ex
+    losses, dx, same = ex.main(hidden=512, steps=12, rank=8, rows=200, quiet=True)
+    assert losses[-1] < 0.9 * losses[0] and all(math.isfinite(v) for v in losses)
+    assert dx.shape == (200, 512) and torch.isfinite(dx.float()).all()
+    assert same

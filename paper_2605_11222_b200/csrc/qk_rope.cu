@@ -212,6 +212,7 @@ struct Ahead {
 // L threads a head (a power of two; threads past d / 16 hold nothing).
 template <bool BF16, int L>
 __global__ void __launch_bounds__(THREADS, RESIDENT) qk_backward_kernel(const __grid_constant__ QkParams P) {
+  pdl_launch();
   using AH = Ahead<BF16>;
   constexpr int G = 32 / L;                       // heads a warp holds at once
   extern __shared__ uint4 slots[];                // [DEPTH][PIECES][THREADS]
@@ -375,6 +376,7 @@ template <bool BF16>
 __global__ void __launch_bounds__(1024)
 qk_weight_grad_kernel(const float* __restrict__ partial, int blocks0, int blocks, int d, void* gq, void* gk) {
   __shared__ float red[32][33];
+  pdl_wait();                                     // launched beside the end of the kernel that makes the partial sums
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int i = blockIdx.x * 32 + tx, q = blockIdx.y;
   const int b0 = q == 0 ? 0 : blocks0, b1 = q == 0 ? blocks0 : blocks;
@@ -474,11 +476,17 @@ cudaError_t launch_qk(const admmq_qk_args& a, bool backward, cudaStream_t stream
     if (e != cudaSuccess) return e;
   }
   if (backward) {
-    const dim3 grid((a.head_dim + 31) / 32, 2);
-    if (bf)
-      qk_weight_grad_kernel<true><<<grid, 1024, 0, stream>>>(P.partial, P.blocks0, (int)blocks, a.head_dim, a.d_grad_wq, a.d_grad_wk);
-    else
-      qk_weight_grad_kernel<false><<<grid, 1024, 0, stream>>>(P.partial, P.blocks0, (int)blocks, a.head_dim, a.d_grad_wq, a.d_grad_wk);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((a.head_dim + 31) / 32, 2);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = blocks > 0 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, bf ? qk_weight_grad_kernel<true> : qk_weight_grad_kernel<false>,
+                              (const float*)P.partial, P.blocks0, (int)blocks, a.head_dim, a.d_grad_wq, a.d_grad_wk);
   }
   return cudaGetLastError();
 }

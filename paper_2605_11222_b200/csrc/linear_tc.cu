@@ -19,9 +19,12 @@
 // travel in a ring of their own ahead of the rows.
 //   warp 0      rows (tile loads), and the adapters' output sides
 //   warp 1      MMA issuer; tensor memory
-//   warp 2      codes and (Delta, z0) pairs (bulk copies)
-//   warp 3      the distinct adapters of the tile's rows
-//   warps 4-19  expand codes, write masked h, and move the finished tile out
+//   warps 2-3   codes and (Delta, z0) pairs (bulk copies), every other step each: a thread takes some 250 cycles to issue a
+//               copy, backward there are four a step, and one thread's were its bound (input gradient of 900 rows of
+//               4096 -> 4096: 48.6 us with one, 36.2 with two, 37.7 with four)
+//   warp 4      the distinct adapters of the tile's rows (5-7: none; a warp reads the quarter of tensor memory that its
+//               number modulo 4 names)
+//   warps 8-23  expand codes, write masked h, and move the finished tile out
 // Every wait is bounded: on expiry the kernel records ADMMQ_ERR_TIMEOUT, lets its copies and MMAs in flight finish
 // (bounded as well), frees tensor memory and returns; CTAs of a cluster meet the same barriers on that path.
 #include "linear_tc.cuh"
@@ -34,7 +37,8 @@ std::atomic<int> g_linear_hold_loads{0};
 namespace {
 
 constexpr int BM = 128;
-constexpr int ROLE_WARPS = 4, EXPAND_WARPS = 16, GROUPS = 4, GROUP_WARPS = EXPAND_WARPS / GROUPS;
+constexpr int ROLE_WARPS = 8, FIRST_CODE_WARP = 2, CODE_WARPS = 2;
+constexpr int EXPAND_WARPS = 16, GROUPS = 4, GROUP_WARPS = EXPAND_WARPS / GROUPS;
 constexpr int WARPS = ROLE_WARPS + EXPAND_WARPS, THREADS = 32 * WARPS;
 constexpr int W_BYTES = BM * BK * 2;                 // 16 KB: 128 runs of 64 weights
 constexpr int MAX_SPLIT = 8;
@@ -85,6 +89,39 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
   return v;
 }
 
+// Rows r0 <= r < r1 of the finished tile: a warp a row, 4 values a lane, the S partials summed in rank order, their loads
+// under way together.  A tile that is not split has eight rows of a warp under way (900 rows of 4096 -> 4096: 36.3 us row
+// by row, 34.5); with several rows of a split one the partials' loads get in each other's way (64 rows: 12.5 us, 13.3).
+template <int S>
+__device__ __forceinline__ void move_out(const TcParams& P, uint32_t sums, long long t0, int r0, int r1, int m0) {
+  constexpr int R = S == 1 ? 8 : 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = m0 + 4 * lane;
+  for (int r = r0 + warp; r < r1; r += R * WARPS) {
+    float4 w[R][S];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (i == 0 || r + i * WARPS < r1) {
+        const uint32_t at = sums + (uint32_t)((r + i * WARPS) * BM + 4 * lane) * 4u;
+#pragma unroll
+        for (int k = 0; k < S; ++k) w[i][k] = ld_cluster_f4(S == 1 ? at : map_to_cta(at, (uint32_t)k));
+      }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float4 v = w[i][0];
+#pragma unroll
+      for (int k = 1; k < S; ++k) {
+        v.x += w[i][k].x;
+        v.y += w[i][k].y;
+        v.z += w[i][k].z;
+        v.w += w[i][k].w;
+      }
+      if (r + i * WARPS < r1 && m < P.M)             // M is a multiple of 8
+        *reinterpret_cast<uint2*>(P.y + (t0 + r + i * WARPS) * P.ldy + m) =
+            make_uint2(float2_to_bf16x2(v.x, v.y), float2_to_bf16x2(v.z, v.w));
+    }
+  }
+}
+
 template <bool GRAD, int NT>
 __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_constant__ TcParams P) {
   using C = Cfg<NT>;
@@ -93,7 +130,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   __shared__ __align__(8) uint64_t bars[2 * ST + 2 * CS + 3];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s, n_list;
-  __shared__ uint32_t fill_state[4];
+  __shared__ uint32_t fill_state[2 + 2 * CODE_WARPS];
   __shared__ int own[NT];                            // adapter of every row of the tile, -1: none
   __shared__ int list[NT];                           // the distinct ones, rising
 
@@ -113,7 +150,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
 
   if (threadIdx.x == 0) {
     abort_s = 0;
-    for (int i = 0; i < 4; ++i) fill_state[i] = 0u;
+    for (int i = 0; i < 2 + 2 * CODE_WARPS; ++i) fill_state[i] = 0u;
     for (int s = 0; s < ST; ++s) {
       mbar_init(full + 8 * s, 1 + GROUP_WARPS);        // the producer with its bytes, and the expanding group's warps
       mbar_init(empty + 8 * s, 1);
@@ -245,21 +282,21 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
     }
     if (ok && elect_one()) tc_commit(done_bar);
     __syncwarp();
-  } else if (warp == 2) {
+  } else if (warp >= FIRST_CODE_WARP && warp < FIRST_CODE_WARP + CODE_WARPS) {
     // ===================== codes and grid =====================
     if (lane == 0 && !P.hold_loads) {
       uint32_t armed = 0u, par = 0u;
-      for (int it = 0; it < nkb; ++it) {
+      for (int it = warp - FIRST_CODE_WARP; it < nkb; it += CODE_WARPS) {
         const uint32_t s = it % CS, ph = (uint32_t)(it / CS) & 1u;
         if (!wait.one(c_empty + 8 * s, ph ^ 1u)) break;
         armed |= 1u << s;
         par = (par & ~(1u << s)) | (ph << s);
         load_codes<GRAD>(P.L, m0, kb0 + it, ring + ST * C::STAGE_BYTES + s * CODE_STAGE_BYTES, c_full + 8 * s);
       }
-      fill_state[2] = armed;
-      fill_state[3] = par;
+      fill_state[2 + 2 * (warp - FIRST_CODE_WARP)] = armed;
+      fill_state[3 + 2 * (warp - FIRST_CODE_WARP)] = par;
     }
-  } else if (warp == 3) {
+  } else if (warp == 4) {
     // ===================== the tile's adapters =====================
     if (P.n_adapters > 0) {
       for (int i = lane; i < NT; i += 32) own[i] = t0 + i < P.T ? row_adapter_of(P.row_adapter, t0 + i, P.n_adapters) : -1;
@@ -278,10 +315,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       __syncwarp();
       if (lane == 0) mbar_arrive(list_bar);
     }
-  } else {
+  } else if (warp >= ROLE_WARPS) {
     // ===================== expanding warps =====================
     const int g = (warp - ROLE_WARPS) / GROUP_WARPS;
     const int v = threadIdx.x - 32 * ROLE_WARPS - g * 32 * GROUP_WARPS;     // 0..127 within the group
+    uint32_t s = (uint32_t)g, ph = 0, cs = (uint32_t)g, cph = 0;
     bool waited = false, ok = true;
     int nl = 0, steps = nkb;
     Extra ex = {0, 0};
@@ -295,17 +333,20 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         steps = nkb + ex.count;
       }
       if (it >= steps) break;
-      const uint32_t s = it % ST, ph = (uint32_t)(it / ST) & 1u;
       uint8_t* w_s = ring_ptr + s * C::STAGE_BYTES;
       uint8_t* x_s = w_s + W_BYTES;
       if (it < nkb) {
-        const uint32_t cs = it % CS;
-        ok = wait.all(c_full + 8 * cs, (uint32_t)(it / CS) & 1u);
+        ok = wait.all(c_full + 8 * cs, cph);
         if (!ok) break;
         const uint8_t* cst = ring_ptr + ST * C::STAGE_BYTES + cs * CODE_STAGE_BYTES;
         const CodeRun r0 = read_codes<GRAD>(P.L, cst, v, m0, kb0 + it), r1 = read_codes<GRAD>(P.L, cst, v + 128, m0, kb0 + it);
         __syncwarp();
         if (lane == 0) mbar_arrive(c_empty + 8 * cs);
+        cs += GROUPS;
+        if (cs >= CS) {
+          cs -= CS;
+          cph ^= 1u;
+        }
         const Weights32 e0 = expand_unit(r0), e1 = expand_unit(r1);     // in registers, before the stage is needed
         ok = wait.all(empty + 8 * s, ph ^ 1u);
         if (!ok) break;
@@ -337,6 +378,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads what was just written
       __syncwarp();
       if (lane == 0) mbar_arrive(full + 8 * s);
+      s += GROUPS;
+      if (s >= ST) {
+        s -= ST;
+        ph ^= 1u;
+      }
     }
     if (!waited) pdl_wait();                         // (so that this launch ends after the one it overlaps)
     // ---- the finished tile: tensor memory -> fp32 [t][m] in shared memory, over the stages
@@ -360,11 +406,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   __syncthreads();
   if (abort_s) {
     if (threadIdx.x == 0) {
-      const uint32_t armed = fill_state[0], par = fill_state[1], carmed = fill_state[2], cpar = fill_state[3];
+      const uint32_t armed = fill_state[0], par = fill_state[1];
       for (int s = 0; s < ST; ++s)
         if (armed >> s & 1u) mbar_wait_quiet(full + 8 * s, par >> s & 1u);
-      for (int s = 0; s < CS; ++s)
-        if (carmed >> s & 1u) mbar_wait_quiet(c_full + 8 * s, cpar >> s & 1u);
+      for (int i = 2; i < 2 + 2 * CODE_WARPS; i += 2)
+        for (int s = 0; s < CS; ++s)
+          if (fill_state[i] >> s & 1u) mbar_wait_quiet(c_full + 8 * s, fill_state[i + 1] >> s & 1u);
     }
     if (threadIdx.x == 32) {
       tc_commit(drain_bar);
@@ -374,23 +421,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   }
   if (splits > 1) cluster_sync_all();
   if (!abort_s) {
-    // ---- rows of this CTA's share: a warp a row, 4 values a lane, summed over the cluster in rank order
-    const int r0 = NT * split / splits, r1 = NT * (split + 1) / splits;
-    const int m = m0 + 4 * lane;
-    for (int r = r0 + warp; r < r1; r += WARPS) {
-      if (t0 + r >= P.T) break;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < splits; ++k) {
-        const float4 w = ld_cluster_f4(map_to_cta(ring + (uint32_t)(r * BM + 4 * lane) * 4u, (uint32_t)k));
-        v.x += w.x;
-        v.y += w.y;
-        v.z += w.z;
-        v.w += w.w;
-      }
-      if (m < P.M)                                   // M is a multiple of 8
-        *reinterpret_cast<uint2*>(P.y + (t0 + r) * P.ldy + m) =
-            make_uint2(float2_to_bf16x2(v.x, v.y), float2_to_bf16x2(v.z, v.w));
-    }
+    const int r0 = NT * split / splits, r1 = (int)min((long long)(NT * (split + 1) / splits), P.T - t0);
+    if (splits == 1) move_out<1>(P, ring, t0, r0, r1, m0);
+    else if (splits == 2) move_out<2>(P, ring, t0, r0, r1, m0);
+    else if (splits == 4) move_out<4>(P, ring, t0, r0, r1, m0);
+    else move_out<8>(P, ring, t0, r0, r1, m0);
   }
   if (splits > 1) cluster_sync_all();                // no CTA leaves while its partial is read
   if (warp == 1) {
@@ -471,6 +506,35 @@ cudaError_t launch(TcParams& P, const bf16* x, long long ldx, const AdapterView*
   return cudaLaunchKernelEx(&cfg, kernel, P);
 }
 
+// Clusters of `splits` CTAs that run at once on the current device (a multiprocessor holds one CTA in every form); 0 on
+// error.  A cluster lies within one group of multiprocessors, and the groups' sizes are not multiples of its own.
+int clusters_at_once(int splits) {
+  static_assert(Cfg<64>::SMEM > 116 * 1024 && Cfg<128>::SMEM > 116 * 1024, "one CTA a multiprocessor");
+  constexpr int MAX_DEVICES = 64;
+  static std::atomic<int> known[MAX_DEVICES][MAX_SPLIT + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
+  int n = known[dev][splits].load(std::memory_order_relaxed);
+  if (n == 0) {
+    const auto kernel = linear_tc_kernel<false, 256>;
+    if (ensure_dynamic_smem((const void*)kernel, Cfg<256>::SMEM) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(splits);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg<256>::SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = splits;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return 0;
+    known[dev][splits].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 template <bool GRAD>
 cudaError_t dispatch(TcParams& P, const bf16* x, long long ldx, const AdapterView* ad, int nt, int splits,
                      cudaStream_t stream) {
@@ -505,12 +569,16 @@ cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView*
   if (sms <= 0) return cudaErrorInvalidDevice;
   // Which form: the K steps that the busiest multiprocessor makes, with a step's time in each form (measured: 0.50 us in
   // one CTA on 256 rows, 0.75 us in a pair on 512).  6011 rows of 4096 -> 4096: 201 us in single CTAs, 153 in pairs; 333
-  // rows of 1024 -> 4096: 17 us in single CTAs that split K, 24 in pairs.
+  // rows of 1024 -> 4096: 12.5 us in single CTAs that split K, 24 in pairs.
   const int nt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
   const long long tiles = (long long)P.tiles_m * ((T + nt - 1) / nt);
   const long long pair_tiles = (long long)((P.M + PAIR_VALUES - 1) / PAIR_VALUES) * ((T + PAIR_ROWS - 1) / PAIR_ROWS);
+  // K is split while every cluster runs at once: sixteen clusters of eight do not (333 rows of 4096 -> 1024: 23.1 us in
+  // eight parts and two turns, 16.8 in four).
   int splits = 1;
-  while (2 * splits <= MAX_SPLIT && tiles * 2 * splits <= sms && P.num_kb >= 4 * splits) splits *= 2;
+  while (2 * splits <= MAX_SPLIT && P.num_kb >= 4 * splits && tiles * 2 * splits <= sms &&
+         tiles <= clusters_at_once(2 * splits))
+    splits *= 2;
   const long long single = (tiles * splits + sms - 1) / sms * ((P.num_kb + splits - 1) / splits);
   const long long pair = (2 * pair_tiles + sms - 1) / sms * P.num_kb;
   if (3 * pair < 2 * single)

@@ -71,10 +71,13 @@ cudaError_t ensure_dynamic_smem(const void* kernel, int bytes);
 // ---- linear_small.cu ----
 constexpr int SMALL_ROWS = 16;   // rows up to which linear_small runs
 cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, const AdapterView& ad,
-                          const int* row_adapter, float* h, cudaStream_t stream);
+                          const int* row_adapter, float* h, int* status, cudaStream_t stream);
 cudaError_t launch_linear_small(const PackedLayer& L, const AdapterView* ad, int T, const int* row_adapter,
                                 const bf16* x, long long ldx, bf16* y, long long ldy, const float* h,
                                 cudaStream_t stream);
+// ---- shrink_tc.cu ----
+cudaError_t launch_shrink_tc(const bf16* x, long long ldx, long long T, int K, const AdapterView& ad,
+                             const int* row_adapter, float* h, int* status, cudaStream_t stream);
 // ---- linear_tc.cu ----
 cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView* ad, long long T,
                              const int* row_adapter, const bf16* x, long long ldx, bf16* y, long long ldy,

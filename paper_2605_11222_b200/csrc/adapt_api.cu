@@ -119,7 +119,7 @@ admmq_status linear(bool grad, const admmq_packed_layer* layer, const admmq_adap
   if (bank) {
     ad = {(const bf16*)(grad ? bank->d_up : bank->d_down), (const bf16*)(grad ? bank->d_down : bank->d_up),
           bank->d_scale, bank->n_adapters, bank->rank};
-    const cudaError_t e = launch_shrink((const bf16*)x, ldx, n_rows, K, ad, row_adapter, h, stream);
+    const cudaError_t e = launch_shrink((const bf16*)x, ldx, n_rows, K, ad, row_adapter, h, d_status, stream);
     if (e != cudaSuccess) return ADMMQ_ERR_CUDA;
   }
   if (!grad && n_rows <= SMALL_ROWS)

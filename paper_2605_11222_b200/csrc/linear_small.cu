@@ -455,20 +455,23 @@ constexpr long long SHRINK_ROWS_MAX = 64;
 }  // namespace
 
 cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, const AdapterView& ad,
-                          const int* row_adapter, float* h, cudaStream_t stream) {
+                          const int* row_adapter, float* h, int* status, cudaStream_t stream) {
   const ShrinkParams P = {x, ldx, T, K, ad.in, ad.scale, ad.n, ad.rank, row_adapter, h};
   if (T <= SHRINK_ROWS_MAX) {
     shrink_rows_kernel<<<dim3((unsigned)T, ad.rank / 2), THREADS, 0, stream>>>(P);
     return cudaGetLastError();
   }
+  // On the tensor cores' tiles a row costs the same at any rank, here it costs the adapters' rows again for every 16 or 32
+  // of the rows.  K = 4096: rank 16, 2048 rows 8.4 us here, 10.8 there, 16384 rows 32 and 31 (K = 12288: 6011 rows 56 and
+  // 37); rank 32, 520 rows 7.5 and 9.7, 1100 rows 17.6 and 10.8; rank 128, 200 rows 12.3 and 14.5, 520 rows 26 and 15.
+  if (ad.rank > 16 ? T * ad.rank >= 32768 : T > 4096)
+    return launch_shrink_tc(x, ldx, T, K, ad, row_adapter, h, status, stream);
   const int sms = device_sms();
   if (sms <= 0) return cudaErrorInvalidDevice;
   // Tiles of 32 rows read the adapters half as often; tiles of 16 meet fewer distinct adapters and are more.
-  if (T > 1024) {
+  if (T > 1024) {                                // (rank 24 has up to 1365 rows here)
     if (ad.rank <= 8) return launch_tile<2, 1>(P, sms, stream);
     if (ad.rank <= 16) return launch_tile<2, 2>(P, sms, stream);
-    if (ad.rank <= 32) return launch_tile<2, 4>(P, sms, stream);
-    if (ad.rank <= 64) return launch_tile<2, 8>(P, sms, stream);
   }
   if (ad.rank <= 8) return launch_tile<1, 1>(P, sms, stream);
   if (ad.rank <= 16) return launch_tile<1, 2>(P, sms, stream);

@@ -80,14 +80,6 @@ __host__ __device__ constexpr uint32_t idesc_of(uint32_t n_cols, bool m_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (m_major ? 1u << 15 : 0u) | ((n_cols >> 3) << 17) |
          ((uint32_t)(BM >> 4) << 24);
 }
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(addr)
-               : "memory");
-  return v;
-}
 
 // Rows r0 <= r < r1 of the finished tile: a warp a row, 4 values a lane, the S partials summed in rank order, their loads
 // under way together.  A tile that is not split has eight rows of a warp under way (900 rows of 4096 -> 4096: 36.3 us row

@@ -51,6 +51,15 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&v)[16]) {
       : "memory");
 }
 
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr)
+               : "memory");
+  return v;
+}
+
 // Copies of K step kb for the 128 values from m0 (below the matrix's end, or nothing is copied and the barrier is
 // completed all the same).  Runs past the matrix are not copied: read_codes gives them a grid of (0, 0).
 template <bool GRAD>

@@ -241,6 +241,85 @@ def test_projections_are_the_same_bits_every_time(T, n, p, na, r):
     adapt.check_device_status(DEV)
 
 
+# (rows, contracted channels, adapters, rank, plan): stacked adapters that fit a pass and that do not, ranks that leave
+# lanes over, channels that end inside a step, tiles past the rows, contracted channels split over several blocks
+CONTRACTIONS = [
+    (256, 8, 1, 128, "one"),
+    (257, 1000, 3, 128, "each"),
+    (512, 128, 2, 64, "none"),
+    (600, 576, 12, 64, "each"),
+    (1024, 200, 3, 32, "mixed"),
+    (1100, 4096, 2, 32, "one"),
+    (1400, 72, 5, 24, "mixed"),
+    (4097, 136, 20, 8, "each"),
+    (4200, 520, 3, 16, "mixed"),
+    (5000, 264, 2, 40, "mixed"),
+    (4500, 2048, 9, 16, "each"),
+]
+
+
+@pytest.mark.parametrize("T,n,na,r,kind", CONTRACTIONS)
+def test_contraction_of_many_rows(T, n, na, r, kind):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + n)
+    codes, scale, zero = _layer(g, n, 8, 4, 0)
+    back = _layer(g, 8, n, 4, 0)
+    bank, turned = _bank(g, na, r, n, 8), _bank(g, na, r, 8, n)
+    plan = _plan(kind, T, na, T)
+    x = _randn(g, T, n + 8).bfloat16()[:, :n]     # rows that are not adjacent
+    for layer, b, mat, run in ((adapt.QuantLinear(codes, scale, zero, 4, 0), bank, bank.down, "forward"),
+                               (adapt.QuantLinear(*back, 4, 0), turned, turned.up, "grad_input")):
+        _, h = getattr(layer, run)(x, b, plan)
+        adapt.check_device_status(DEV)
+        for t in range(0, T, 1000):               # (the plain form gathers a matrix a row)
+            rows = slice(t, min(T, t + 1000))
+
+            class Part:
+                row_adapter = plan.row_adapter[rows]
+            want, size = _shrink64(x[rows], mat, b, Part)
+            _within(h[rows], want, ACC * size + 1e-30)
+        for _ in range(10):
+            assert torch.equal(getattr(layer, run)(x, b, plan)[1], h)
+
+
+def test_a_bad_row_stays_in_its_row_of_the_contraction():
+    from paper_2605_11222_b200 import adapt
+    g = _gen(31)
+    codes, scale, zero = _layer(g, 512, 8, 4, 128)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 128), _bank(g, 3, 64, 512, 8), _plan("each", 700, 3)
+    x = _randn(g, 700, 512).bfloat16()
+    _, want = layer.forward(x, bank, plan)
+    x[333, 5] = float("nan")
+    x[12, 7] = float("inf")
+    _, h = layer.forward(x, bank, plan)
+    keep = torch.ones(700, dtype=torch.bool, device=DEV)
+    keep[[12, 333]] = False
+    assert torch.equal(h[keep], want[keep])
+    on = (plan.row_adapter[[12, 333]] >= 0)
+    assert not torch.isfinite(h[[12, 333]][on]).any() and (h[[12, 333]][~on] == 0).all()
+
+
+def test_a_wait_of_the_contraction_that_runs_out_is_reported():
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(3)
+    codes, scale, zero = _layer(g, 1024, 256, 4, 128)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 128), _bank(g, 3, 64, 1024, 256), _plan("each", 600, 3)
+    x = _randn(g, 600, 1024).bfloat16()
+    want, wanth = layer.forward(x, bank, plan)
+    lib = adapt._library()
+    assert lib.admmq_test_linear_set_wait(200000, 1) == B.OK
+    try:
+        layer.forward(x, bank, plan)
+        with pytest.raises(adapt.AdmmqError) as e:
+            adapt.check_device_status(DEV)
+        assert e.value.status == B.ERR_TIMEOUT
+    finally:
+        assert lib.admmq_test_linear_set_wait(2_000_000_000, 0) == B.OK
+    got, h = layer.forward(x, bank, plan)
+    adapt.check_device_status(DEV)
+    assert torch.equal(got, want) and torch.equal(h, wanth)
+
+
 def test_adapter_grads_are_the_same_bits_every_time():
     from paper_2605_11222_b200 import adapt
     g = _gen(9)

@@ -17,8 +17,8 @@
 // and split the input channels it took 12700, and such a launch does not overlap the one before it.
 //
 // shrink: h[t][r] = scale_a sum_i x[t][i] in_a[r][i].  Bound: memory, one pass over the rows and over the adapters in
-// use.  Two forms: a CTA for each row and two ranks for few rows, and tiles of 16 or 32 rows on mma.sync
-// for more, where the passes over a tile are one per distinct adapter in it.
+// use.  Three forms: a CTA for each row and two ranks for few rows, tiles of 16 or 32 rows on mma.sync for more, where
+// the passes over a tile are one per distinct adapter in it, and for many the tiles of shrink_tc.cu.
 #include <cooperative_groups.h>
 
 #include "adapt.h"

@@ -71,7 +71,7 @@ cudaError_t ensure_dynamic_smem(const void* kernel, int bytes);
 // ---- linear_small.cu ----
 constexpr int SMALL_ROWS = 16;   // rows up to which linear_small runs
 cudaError_t launch_shrink(const bf16* x, long long ldx, long long T, int K, const AdapterView& ad,
-                          const int* row_adapter, float* h, int* status, cudaStream_t stream);
+                          const int* row_adapter, float* h, int spare, int* status, cudaStream_t stream);
 cudaError_t launch_linear_small(const PackedLayer& L, const AdapterView* ad, int T, const int* row_adapter,
                                 const bf16* x, long long ldx, bf16* y, long long ldy, const float* h,
                                 cudaStream_t stream);
@@ -79,6 +79,12 @@ cudaError_t launch_linear_small(const PackedLayer& L, const AdapterView* ad, int
 cudaError_t launch_shrink_tc(const bf16* x, long long ldx, long long T, int K, const AdapterView& ad,
                              const int* row_adapter, float* h, int* status, cudaStream_t stream);
 // ---- linear_tc.cu ----
+struct TcPlan {
+  bool pair;                     // CTA pairs (linear_pair.cu)
+  int nt, splits, tiles_m;
+  long long ctas;
+};
+TcPlan plan_linear_tc(bool grad, const PackedLayer& L, long long T, int sms);
 cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView* ad, long long T,
                              const int* row_adapter, const bf16* x, long long ldx, bf16* y, long long ldy,
                              const float* h, int* status, cudaStream_t stream);

@@ -1,4 +1,5 @@
 // C entry points of admmq_adapt.h: argument checks and kernel selection, plus packing and the check of a bank.
+#include <algorithm>
 #include <atomic>
 
 #include "../../include/admmq_testing.h"
@@ -119,7 +120,12 @@ admmq_status linear(bool grad, const admmq_packed_layer* layer, const admmq_adap
   if (bank) {
     ad = {(const bf16*)(grad ? bank->d_up : bank->d_down), (const bf16*)(grad ? bank->d_down : bank->d_up),
           bank->d_scale, bank->n_adapters, bank->rank};
-    const cudaError_t e = launch_shrink((const bf16*)x, ldx, n_rows, K, ad, row_adapter, h, d_status, stream);
+    // multiprocessors that the projection leaves to the contraction, which it overlaps
+    const int sms = device_sms();
+    if (sms <= 0) return ADMMQ_ERR_CUDA;
+    const bool small = !grad && n_rows <= SMALL_ROWS;
+    const int spare = small ? 0 : (int)std::max(0LL, sms - plan_linear_tc(grad, L, n_rows, sms).ctas);
+    const cudaError_t e = launch_shrink((const bf16*)x, ldx, n_rows, K, ad, row_adapter, h, spare, d_status, stream);
     if (e != cudaSuccess) return ADMMQ_ERR_CUDA;
   }
   if (!grad && n_rows <= SMALL_ROWS)

@@ -209,10 +209,10 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
         } else {
           const int e = ex.first + it - nkb;
           const int first = e / per * P.cap, na = min(P.cap, nl - first), r0 = (e % per) * BK;
+          const int box_bytes = P.box_rows * 128;
           // an odd number of boxes of 8 or 24 rows leaves half of a 16-deep MMA step: a box past the last adapter (it
           // reads as zero) fills it
           const int boxes = na + ((na * P.box_rows) % 16 != 0 ? 1 : 0);
-          const int box_bytes = P.box_rows * 128;
           mbar_expect_tx(fb, 2 * boxes * box_bytes);
           for (int b = 0; b < boxes; ++b) {
             const int a = b < na ? list[first + b] : P.n_adapters;
@@ -538,9 +538,37 @@ cudaError_t dispatch(TcParams& P, const bf16* x, long long ldx, const AdapterVie
 
 }  // namespace
 
+// Form, tile and number of CTAs of a call.
+TcPlan plan_linear_tc(bool grad, const PackedLayer& L, long long T, int sms) {
+  const int M = grad ? L.d_in : L.d_out, num_kb = ((grad ? L.d_out : L.d_in) + BK - 1) / BK;
+  TcPlan p = {};
+  p.tiles_m = (M + BM - 1) / BM;
+  // Which form: the K steps that the busiest multiprocessor makes, with a step's time in each form (measured: 0.50 us in
+  // one CTA on 256 rows, 0.75 us in a pair on 512).  4096 -> 4096: 2048 rows 63 us in single CTAs, 51 in pairs; 900 rows
+  // 34 and 48.  333 rows of 1024 -> 4096: 12.5 us in single CTAs that split K, 21 in pairs.
+  p.nt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
+  const long long tiles = (long long)p.tiles_m * ((T + p.nt - 1) / p.nt);
+  const long long pair_tiles = (long long)((M + PAIR_VALUES - 1) / PAIR_VALUES) * ((T + PAIR_ROWS - 1) / PAIR_ROWS);
+  // K is split while every cluster runs at once: sixteen clusters of eight do not (333 rows of 4096 -> 1024: 23.1 us in
+  // eight parts and two turns, 16.8 in four).
+  p.splits = 1;
+  while (2 * p.splits <= MAX_SPLIT && num_kb >= 4 * p.splits && tiles * 2 * p.splits <= sms &&
+         tiles <= clusters_at_once(2 * p.splits))
+    p.splits *= 2;
+  const long long single = (tiles * p.splits + sms - 1) / sms * ((num_kb + p.splits - 1) / p.splits);
+  const long long pair = (2 * pair_tiles + sms - 1) / sms * num_kb;
+  p.pair = 3 * pair < 2 * single;
+  p.ctas = p.pair ? sms : tiles * p.splits;
+  return p;
+}
+
 cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView* ad, long long T,
                              const int* row_adapter, const bf16* x, long long ldx, bf16* y, long long ldy,
                              const float* h, int* status, cudaStream_t stream) {
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  const TcPlan plan = plan_linear_tc(grad, L, T, sms);
+  if (plan.pair) return launch_linear_pair(grad, L, ad, T, row_adapter, x, ldx, y, ldy, h, status, sms, stream);
   TcParams P = {};
   P.L = L;
   P.M = grad ? L.d_in : L.d_out;
@@ -553,29 +581,12 @@ cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView*
   P.h = h;
   P.y = y;
   P.ldy = ldy;
-  P.tiles_m = (P.M + BM - 1) / BM;
   P.status = status;
   P.wait_limit = g_linear_wait_limit.load(std::memory_order_relaxed);
   P.hold_loads = g_linear_hold_loads.load(std::memory_order_relaxed);
-  const int sms = device_sms();
-  if (sms <= 0) return cudaErrorInvalidDevice;
-  // Which form: the K steps that the busiest multiprocessor makes, with a step's time in each form (measured: 0.50 us in
-  // one CTA on 256 rows, 0.75 us in a pair on 512).  6011 rows of 4096 -> 4096: 201 us in single CTAs, 153 in pairs; 333
-  // rows of 1024 -> 4096: 12.5 us in single CTAs that split K, 24 in pairs.
-  const int nt = T <= 64 ? 64 : T <= 128 ? 128 : 256;
-  const long long tiles = (long long)P.tiles_m * ((T + nt - 1) / nt);
-  const long long pair_tiles = (long long)((P.M + PAIR_VALUES - 1) / PAIR_VALUES) * ((T + PAIR_ROWS - 1) / PAIR_ROWS);
-  // K is split while every cluster runs at once: sixteen clusters of eight do not (333 rows of 4096 -> 1024: 23.1 us in
-  // eight parts and two turns, 16.8 in four).
-  int splits = 1;
-  while (2 * splits <= MAX_SPLIT && P.num_kb >= 4 * splits && tiles * 2 * splits <= sms &&
-         tiles <= clusters_at_once(2 * splits))
-    splits *= 2;
-  const long long single = (tiles * splits + sms - 1) / sms * ((P.num_kb + splits - 1) / splits);
-  const long long pair = (2 * pair_tiles + sms - 1) / sms * P.num_kb;
-  if (3 * pair < 2 * single)
-    return launch_linear_pair(grad, L, ad, T, row_adapter, x, ldx, y, ldy, h, status, sms, stream);
-  return grad ? dispatch<true>(P, x, ldx, ad, nt, splits, stream) : dispatch<false>(P, x, ldx, ad, nt, splits, stream);
+  P.tiles_m = plan.tiles_m;
+  return grad ? dispatch<true>(P, x, ldx, ad, plan.nt, plan.splits, stream)
+              : dispatch<false>(P, x, ldx, ad, plan.nt, plan.splits, stream);
 }
 
 }  // namespace admmq

@@ -241,6 +241,28 @@ def test_projections_are_the_same_bits_every_time(T, n, p, na, r):
     adapt.check_device_status(DEV)
 
 
+@pytest.mark.parametrize("r", [8, 16, 24, 32])
+@pytest.mark.parametrize("T", [70, 300])
+def test_adapters_of_a_tile_in_runs_and_with_gaps(T, r):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + r)
+    n, p, na = 256, 200, 12
+    codes, scale, zero = _layer(g, n, p, 4, 64)
+    layer, bank = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, na, r, n, p)
+    W = _weight64(codes, scale, zero)
+    x, dy = _randn(g, T, n).bfloat16(), _randn(g, T, p).bfloat16()
+    for ids in ([0, 1, 2, 3], [4, 5, 6, 7, 8, 9, 10, 11], [11, 9, 10], [0, 2, 3, 7, 8, 11], [5, -1, 6], list(range(na))):
+        cuts = [T * i // len(ids) for i in range(len(ids) + 1)]
+        plan = adapt.RequestPlan([b - a for a, b in zip(cuts, cuts[1:])], ids, na)
+        for run, v, w, inn, out in ((layer.forward, x, W.T, bank.down, bank.up), (layer.grad_input, dy, W, bank.up, bank.down)):
+            y, _ = run(v, bank, plan)
+            h, _ = _shrink64(v, inn, bank, plan)
+            delta, sq_delta = _expand64(h, out, plan)
+            want, sq = v.double() @ w + delta, v.double() ** 2 @ w ** 2 + sq_delta
+            _within(y, want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * sq.sqrt() * math.sqrt(w.shape[0] + r) + 1e-30)
+    adapt.check_device_status(DEV)
+
+
 # (rows, contracted channels, adapters, rank, plan): stacked adapters that fit a pass and that do not, ranks that leave
 # lanes over, channels that end inside a step, tiles past the rows, contracted channels split over several blocks
 CONTRACTIONS = [

@@ -44,6 +44,11 @@ admmq_status admmq_test_w_update_series(admmq_ctx* ctx, const float* d_W0, int d
  * process, since those calls have no context.  hold_loads = 0 and 2e9 cycles restore normal operation. */
 admmq_status admmq_test_linear_set_wait(long long wait_limit_cycles, int hold_loads);
 
+/* The rings of the projection on CTA pairs, for a test that walks its schedule: groups of warps that expand the weights
+ * (K step s is group s % groups'), stages of operands and of rows, slots of codes and the barriers that say they have
+ * landed (code step c: slot c % code_slots, barrier c % code_barriers).  Host-side only. */
+void admmq_test_pair_rings(int* groups, int* stages, int* row_stages, int* code_slots, int* code_barriers);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,7 @@
 // Waits are bounded as in the other tensor-core kernels.  No multicast load anywhere.
 #include <atomic>
 
+#include "../../include/admmq_testing.h"
 #include "linear_tc.cuh"
 
 namespace admmq {
@@ -38,6 +39,7 @@ struct Cfg {
   // A step's rows are on their way for about 1000 cycles before the MMAs need them, its weights for 2000: rings of
   // different depth.  Barriers go with the weights' ring.
   static constexpr int XST = 3, WST = 5, CST = 4;
+  static constexpr int CBARS = 2 * CST;                // barriers of the codes' slots: every slot has two, taken in turn
   static constexpr int W_AT = XST * NMB * X_BYTES, C_AT = W_AT + WST * W_BYTES, OUT_AT = C_AT + CST * CODE_STAGE_BYTES;
   static constexpr int SMEM = OUT_AT + MOVE_WARPS * OUT_BYTES + 1024;
   static constexpr int ROWS = NMB * 256;
@@ -103,11 +105,11 @@ __host__ __device__ constexpr uint32_t idesc_pair(bool n_major) {
 template <bool GRAD>
 __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_constant__ PairParams P) {
   using C = Cfg;
-  constexpr int XST = C::XST, WST = C::WST, CS = C::CST;
-  static_assert(CS % GROUPS == 0 && WST >= GROUPS, "see stage_free");
+  constexpr int XST = C::XST, WST = C::WST, CS = C::CST, CB = C::CBARS;
+  static_assert(WST >= GROUPS && CB % CS == 0 && CB % GROUPS == 0 && CB + 1 >= GROUPS + WST, "see stage_free");
   static_assert(XST <= WST, "a step whose rows' stage is free has its weights' stage free");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * WST + 2 * CS + 9];
+  __shared__ __align__(8) uint64_t bars[2 * WST + CB + CS + 9];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
   __shared__ uint32_t fill_state[4];
@@ -126,7 +128,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
   // full: a step's operands are in place (leader); done: its MMAs have read them (both CTAs); codes landed and read;
   // accumulators complete and moved out; a tile's adapters listed and no longer needed
   const uint32_t full = smem_u32(&bars[0]), done = full + 8 * WST;
-  const uint32_t c_full = done + 8 * WST, c_empty = c_full + 8 * CS;
+  const uint32_t c_full = done + 8 * WST, c_empty = c_full + 8 * CB;
   const uint32_t t_full = c_empty + 8 * CS, t_empty = t_full + 16, l_full = t_empty + 16, l_empty = l_full + 16;
   const uint32_t drain_bar = l_empty + 16;
 
@@ -138,10 +140,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
       mbar_init(full + 8 * s, 1 + 2 * GROUP_WARPS);
       mbar_init(done + 8 * s, 1);
     }
-    for (int s = 0; s < CS; ++s) {
-      mbar_init(c_full + 8 * s, 1);
-      mbar_init(c_empty + 8 * s, GROUP_WARPS);
-    }
+    for (int s = 0; s < CB; ++s) mbar_init(c_full + 8 * s, 1);
+    for (int s = 0; s < CS; ++s) mbar_init(c_empty + 8 * s, GROUP_WARPS);
     for (int b = 0; b < 2; ++b) {
       mbar_init(t_full + 8 * b, 1);
       mbar_init(t_empty + 8 * b, 2 * 4);             // leader's: the four moving warps of both CTAs
@@ -171,9 +171,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
     return ok ? list_n[n & 1] : 0;
   };
   // A wait by parity is only sound for a waiter that knows the phase before to be over.  Roles that walk every step know
-  // it; an expanding group sees every fourth.  Its ring of codes is a multiple of the groups long, so that it meets a
-  // slot only after itself; and steps are done in order, so that step it - 4 - WST done (its wait before) covers
-  // it - 2 WST, and it - WST done (asked first) covers it - XST - WST.
+  // it; an expanding group sees every fourth.  Stages: steps are done in order, so that step it - 4 - WST done (its wait
+  // before) covers it - 2 WST, and it - WST done (asked first) covers it - XST - WST.  Codes: they are counted by weights'
+  // steps (ct), without the adapters' steps that lie between those of two tiles, so that the group that takes a slot
+  // changes from tile to tile.  The phase before that of ct on its barrier is ct - CB.  With no adapter step since then it
+  // was this group's own, 8 steps ago; with one or more it was step it - 9 or an earlier one, which step it - 4 - WST done
+  // covers.  (One barrier a slot is not enough: ct - 4 may be another group's, and its copy still on the way.)
   // waits until the stage of step `it` in a ring of `depth` stages is free: step it - depth is done
   auto stage_free = [&](uint32_t it, uint32_t depth, bool whole_warp) -> bool {
     if (it < depth) return true;
@@ -308,12 +311,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
       for (int tile = pair; tile < P.num_tiles && ok; tile += pairs) {
         const int m0 = (tile % P.tiles_m) * 256 + (int)rank * HALF;
         for (int kb = 0; kb < P.num_kb; ++kb, ++ct) {
-          const uint32_t s = ct % CS, ph = (ct / CS) & 1u;
-          ok = wait.one(c_empty + 8 * s, ph ^ 1u);
+          const uint32_t s = ct % CS, b = ct % CB;
+          ok = wait.one(c_empty + 8 * s, (ct / CS & 1u) ^ 1u);
           if (!ok) break;
-          armed |= 1u << s;
-          par = (par & ~(1u << s)) | (ph << s);
-          load_codes<GRAD>(P.L, m0, kb, ring + C::C_AT + s * CODE_STAGE_BYTES, c_full + 8 * s);
+          armed |= 1u << b;
+          par = (par & ~(1u << b)) | ((ct / CB & 1u) << b);
+          load_codes<GRAD>(P.L, m0, kb, ring + C::C_AT + s * CODE_STAGE_BYTES, c_full + 8 * b);
         }
       }
       fill_state[2] = armed;
@@ -427,7 +430,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
         uint8_t* w_s = ring_ptr + C::W_AT + s * W_BYTES;
         if (k < P.num_kb) {
           const uint32_t ct = n * P.num_kb + k, cs = ct % CS;
-          ok = wait.all(c_full + 8 * cs, (ct / CS) & 1u);
+          ok = wait.all(c_full + 8 * (ct % CB), (ct / CB) & 1u);
           if (!ok) break;
           const uint8_t* cst = ring_ptr + C::C_AT + cs * CODE_STAGE_BYTES;
           const CodeRun r0 = read_codes<GRAD>(P.L, cst, v, m0, k), r1 = read_codes<GRAD>(P.L, cst, v + 128, m0, k);
@@ -492,7 +495,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_pair_kernel(const __grid_co
           if (armed >> s & 1u) mbar_wait_quiet(full + 8 * s, par >> s & 1u);
       }
       const uint32_t armed = fill_state[2], par = fill_state[3];
-      for (int s = 0; s < CS; ++s)
+      for (int s = 0; s < CB; ++s)
         if (armed >> s & 1u) mbar_wait_quiet(c_full + 8 * s, par >> s & 1u);
     }
     if (threadIdx.x == 32 && rank == 0) {
@@ -598,3 +601,11 @@ cudaError_t launch_linear_pair(bool grad, const PackedLayer& L, const AdapterVie
 }
 
 }  // namespace admmq
+
+extern "C" void admmq_test_pair_rings(int* groups, int* stages, int* row_stages, int* code_slots, int* code_barriers) {
+  *groups = admmq::GROUPS;
+  *stages = admmq::Cfg::WST;
+  *row_stages = admmq::Cfg::XST;
+  *code_slots = admmq::Cfg::CST;
+  *code_barriers = admmq::Cfg::CBARS;
+}

@@ -188,3 +188,37 @@ def test_request_plan(adapt):
     for a in (-2, 2):
         with pytest.raises(adapt.AdmmqError):
             adapt.RequestPlan([1], [a], 2, device="cpu")
+
+
+def test_waits_by_parity_of_the_pair_form_know_the_phase_before(adapt):
+    """The projection on CTA pairs shares its K steps out to groups of warps by step number, adapter steps counted, and its
+    codes to slots and barriers by code step, adapter steps not counted.  A group waits on a barrier by parity, which is
+    sound only if it knows the phase before to be over: it took those codes itself, or they belong to a step that a wait
+    of its own has seen done (steps are done in order, and a step's codes have landed before it is done)."""
+    out = [C.c_int() for _ in range(5)]
+    adapt._library().admmq_test_pair_rings(*[C.byref(o) for o in out])
+    groups, stages, row_stages, slots, barriers = [o.value for o in out]
+    assert row_stages <= stages and barriers % slots == 0
+    rng = np.random.default_rng(1)
+    cases = [(kb, [e] * 12) for kb in (1, 2, 3, 4, 7, 64) for e in range(9)]
+    cases += [(kb, rng.integers(0, 6, 60).tolist()) for kb in (1, 2, 3, 5, 8, 64) for _ in range(20)]
+    for num_kb, extras in cases:
+        done = [-1] * groups                       # last step that the group's waits have seen done
+        taken = [set() for _ in range(groups)]     # code steps that it took
+        step_of = []                               # of every code step
+        it = 0
+        for extra in extras:                       # the tiles of a pair
+            for k in range(num_kb + extra):
+                g = it % groups
+                if k < num_kb:
+                    ct = len(step_of)
+                    step_of.append(it)
+                    before = ct - barriers
+                    assert before < 0 or before in taken[g] or step_of[before] <= done[g], (num_kb, extras, it)
+                    taken[g].add(ct)
+                depths = (stages,) if k < num_kb else (stages, row_stages)
+                for depth in depths:               # the stage is free: step it - depth is done
+                    last = it - depth
+                    assert last < stages or last - stages <= done[g], (num_kb, extras, it)
+                    done[g] = max(done[g], last)
+                it += 1

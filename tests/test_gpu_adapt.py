@@ -241,6 +241,45 @@ def test_projections_are_the_same_bits_every_time(T, n, p, na, r):
     adapt.check_device_status(DEV)
 
 
+@pytest.mark.parametrize("k", [64, 192, 576])                # contracted channels: one, three and nine K steps
+@pytest.mark.parametrize("r", [24, 64, 128])                 # two adapters in a K step, one, half of one
+def test_pairs_with_several_tiles_and_changing_numbers_of_adapters(k, r):
+    """216 tiles of 512 rows and 256 values, so that every pair of multiprocessors has two or three, from one to the next
+    with another number of adapter steps (0 to 5 adapters in 512 rows)."""
+    from paper_2605_11222_b200 import adapt
+    T, m, na = 24 * 512, 2304, 6
+    g = _gen(k + r)
+    lengths, ids = [], []
+    for tile in range(24):
+        n = (5 * tile + tile // 6) % 6                         # distinct adapters of the tile
+        for i in range(max(1, n)):
+            lengths.append(512 // max(1, n) if i else 512 - 512 // max(1, n) * (max(1, n) - 1))
+            ids.append((tile + i) % na if n else -1)
+    plan = adapt.RequestPlan(lengths, ids, na)
+    assert plan.n_rows == T
+    for grad in (False, True):
+        n, p = (m, k) if grad else (k, m)
+        codes, scale, zero = _layer(g, n, p, 4, 64)
+        layer, bank = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, na, r, n, p)
+        W = _weight64(codes, scale, zero)
+        v = _randn(g, T, k).bfloat16()
+        run, w, inn, out = (layer.grad_input, W, bank.up, bank.down) if grad else (layer.forward, W.T, bank.down, bank.up)
+        first = run(v, bank, plan)
+        want, sq = v.double() @ w, v.double() ** 2 @ w ** 2
+        for a in range(na):
+            t = (plan.row_adapter == a).nonzero()[:, 0]
+            f64 = bank.scale[a].double() * (v[t].double() @ inn[a].double().T)
+            want[t] += f64 @ out[a].double()
+            sq[t] += f64 ** 2 @ out[a].double() ** 2
+        _within(first[0], want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * sq.sqrt() * math.sqrt(k + r) + 1e-30)
+        for _ in range(30):
+            assert torch.equal(run(v, bank, plan)[0], first[0])
+        # without a bank
+        want, sq = v.double() @ w, v.double() ** 2 @ w ** 2
+        _within(run(v)[0], want, EPS * want.abs() + SIX * EPS * sq.sqrt() + ACC * sq.sqrt() * math.sqrt(k) + 1e-30)
+        adapt.check_device_status(DEV)
+
+
 @pytest.mark.parametrize("r", [8, 16, 24, 32])
 @pytest.mark.parametrize("T", [70, 300])
 def test_adapters_of_a_tile_in_runs_and_with_gaps(T, r):

@@ -44,6 +44,12 @@ admmq_status admmq_test_w_update_series(admmq_ctx* ctx, const float* d_W0, int d
  * process, since those calls have no context.  hold_loads = 0 and 2e9 cycles restore normal operation. */
 admmq_status admmq_test_linear_set_wait(long long wait_limit_cycles, int hold_loads);
 
+/* A whole-warp wait as the tensor-core projections make it, on a barrier that is completed some 2^21 cycles after the
+ * launch: lanes 0..15 give up after limit_low cycles, lanes 16..31 after limit_high (1000 to 2e9 each).  d_out[32] receives
+ * every lane's answer, 1 for completed; d_status the time-out if a lane met one. */
+admmq_status admmq_test_warp_wait(long long limit_low, long long limit_high, int* d_out, int* d_status,
+                                  void* cuda_stream);
+
 /* The rings of the projection on CTA pairs, for a test that walks its schedule: groups of warps that expand the weights
  * (K step s is group s % groups'), stages of operands and of rows, slots of codes and the barriers that say they have
  * landed (code step c: slot c % code_slots, barrier c % code_barriers).  Host-side only. */

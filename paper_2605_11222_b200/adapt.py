@@ -78,6 +78,7 @@ def _library():
         lib.admmq_qk_norm_rope.argtypes = [vp, vp]
         lib.admmq_qk_norm_rope_backward.argtypes = [vp, vp]
         lib.admmq_test_linear_set_wait.argtypes = [cll, ci]
+        lib.admmq_test_warp_wait.argtypes = [cll, cll, vp, vp, vp]
         lib.admmq_test_pair_rings.restype, lib.admmq_test_pair_rings.argtypes = None, [vp] * 5
         _lib = lib
     return _lib

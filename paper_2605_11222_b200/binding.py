@@ -34,7 +34,7 @@ EXPORTS = [
     "admmq_packed_bytes", "admmq_grid_bytes", "admmq_pack_layer", "admmq_adapters_check", "admmq_linear_forward",
     "admmq_linear_grad_input", "admmq_adapter_grad", "admmq_checkpoint_save", "admmq_checkpoint_restore",
     "admmq_qk_workspace_bytes", "admmq_qk_norm_rope", "admmq_qk_norm_rope_backward", "admmq_test_linear_set_wait",
-    "admmq_test_pair_rings",
+    "admmq_test_pair_rings", "admmq_test_warp_wait",
 ]
 T_HESSIAN_PRODUCT, T_TRANSPOSE, T_FACTOR, T_WUPDATE_PRODUCT1, T_TRIDIAG_SOLVE, T_WUPDATE_PRODUCT2, \
     T_GRADIENT_PRODUCT, T_LOCAL_SEARCH, T_ROW_SPLIT, T_WUPDATE_ONE_PLANE = range(10)

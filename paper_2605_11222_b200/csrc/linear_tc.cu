@@ -27,6 +27,7 @@
 //   warps 8-23  expand codes, write masked h, and move the finished tile out
 // Every wait is bounded: on expiry the kernel records ADMMQ_ERR_TIMEOUT, lets its copies and MMAs in flight finish
 // (bounded as well), frees tensor memory and returns; CTAs of a cluster meet the same barriers on that path.
+#include "../../include/admmq_testing.h"
 #include "linear_tc.cuh"
 
 namespace admmq {
@@ -426,6 +427,28 @@ __global__ void __launch_bounds__(THREADS, 1) linear_tc_kernel(const __grid_cons
   }
 }
 
+// The answer of a whole-warp wait in every lane, on a barrier that is completed 2^21 cycles after the start; the two halves
+// of the warp have limits and abort flags of their own.
+__global__ void warp_wait_kernel(long long limit_low, long long limit_high, int* out, int* status) {
+  __shared__ __align__(8) uint64_t bar_s;
+  __shared__ int flags[2];
+  const uint32_t bar = smem_u32(&bar_s);
+  const int half = (threadIdx.x & 31) >> 4;
+  if (threadIdx.x < 2) flags[threadIdx.x] = 0;
+  if (threadIdx.x == 0) mbar_init(bar, 1);
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const Waiter wait = {&flags[half], status, half ? limit_high : limit_low};
+    out[threadIdx.x] = wait.all(bar, 0u) ? 1 : 0;
+  } else if (threadIdx.x == 32) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1LL << 21)) {
+    }
+    mbar_arrive(bar);
+  }
+  __syncthreads();
+}
+
 // ------------------------------------------------------------------ host side
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -590,3 +613,11 @@ cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView*
 }
 
 }  // namespace admmq
+
+extern "C" admmq_status admmq_test_warp_wait(long long limit_low, long long limit_high, int* d_out, int* d_status,
+                                             void* cuda_stream) {
+  if (limit_low < 1000 || limit_high < 1000 || limit_low > 2000000000LL || limit_high > 2000000000LL || !d_out || !d_status)
+    return ADMMQ_ERR_INVALID_ARG;
+  admmq::warp_wait_kernel<<<1, 64, 0, (cudaStream_t)cuda_stream>>>(limit_low, limit_high, d_out, d_status);
+  return cudaGetLastError() == cudaSuccess ? ADMMQ_OK : ADMMQ_ERR_CUDA;
+}

@@ -106,12 +106,12 @@ struct Waiter {
     if (mbar_try_wait(bar, parity)) return true;
     return poll_slow(bar, parity, abort_flag, status, limit);
   }
-  // a whole warp, all lanes polling in one instruction
+  // A whole warp, all lanes polling in one instruction.  The answer is one for the warp: lanes give up by their own clocks,
+  // and where the barrier completes just then some would go on to warp-wide instructions that the others never reach.
   __device__ __forceinline__ bool all(uint32_t bar, uint32_t parity) const {
     bool ok = true;
     if (!mbar_try_wait(bar, parity)) ok = poll_slow(bar, parity, abort_flag, status, limit);
-    __syncwarp();
-    return ok;
+    return __all_sync(0xffffffffu, ok) != 0;
   }
 };
 // Descriptors differ in their low words only (address, and the leading offset of the second form).

@@ -122,9 +122,10 @@ __global__ void __launch_bounds__(THREADS, 2) shrink_tc_kernel(const __grid_cons
       ph ^= 1u;
     }
   };
+  bool live = true;                                  // as of the last barrier: the same for all, whoever gives up after it
   for (int pass = 0; pass < passes; ++pass) {
     const int first = pass * cap, na = min(cap, nl - first);
-    if (!abort_s) {
+    if (live) {
       if ((warp == 0 || warp == 2) && lane == 0 && !P.hold_loads) {
         uint32_t armed = fill_state[warp], par = fill_state[warp + 1];
         for (int k = 0; k < nkb; ++k) {
@@ -176,7 +177,8 @@ __global__ void __launch_bounds__(THREADS, 2) shrink_tc_kernel(const __grid_cons
       }
     }
     __syncthreads();                                 // (the other warps sleep here rather than poll beside the loops)
-    if (!abort_s) {
+    live = abort_s == 0;                             // (no wait runs from here to the next pass)
+    if (live) {
       // ---- sums: tensor memory -> fp32 [t][lane] in shared memory, over the stages
       tc_fence_after();
       const int q = warp & 3;
@@ -195,7 +197,7 @@ __global__ void __launch_bounds__(THREADS, 2) shrink_tc_kernel(const __grid_cons
     }
     __syncthreads();
     if (splits > 1) cluster_sync_all();
-    if (!abort_s) {
+    if (live) {
       for (int i = threadIdx.x; i < (r1 - r0) * quads; i += THREADS) {
         const int r = r0 + i / quads, a = own[r];
         int slot = 0;

@@ -575,6 +575,21 @@ def test_a_wait_that_runs_out_is_reported():
     assert torch.equal(got, want)
 
 
+def test_a_whole_warp_wait_gives_every_lane_the_same_answer():
+    """Also where some lanes give up before the barrier completes and the others would have seen it complete: the roles of
+    the projections go on to warp-wide instructions by this answer."""
+    from paper_2605_11222_b200 import adapt, binding as B
+    lib = adapt._library()
+    out = torch.full((32,), 7, dtype=torch.int32, device=DEV)
+    long, short = 1_000_000_000, 20_000
+    for low, high, answer in ((long, long, 1), (short, long, 0), (long, short, 0), (short, short, 0)):
+        word = torch.zeros(1, dtype=torch.int32, device=DEV)
+        assert lib.admmq_test_warp_wait(low, high, out.data_ptr(), word.data_ptr(),
+                                        torch.cuda.current_stream().cuda_stream) == B.OK
+        assert out.tolist() == [answer] * 32
+        assert int(word) == (B.OK if answer else B.ERR_TIMEOUT)
+
+
 # ------------------------------------------------------------------ checkpoints
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,n", [(0, 64), (1, 8), (3, 128), (5, 136), (77, 4096), (200, 1000), (2, 12288)])

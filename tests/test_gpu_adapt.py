@@ -575,6 +575,31 @@ def test_a_wait_that_runs_out_is_reported():
     assert torch.equal(got, want)
 
 
+# one CTA a tile with K split over a cluster, one without, pairs with one tile each, pairs with several
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("T,n,p,r", [(200, 4096, 512, 24), (900, 4096, 4096, 8), (20000, 256, 136, 16), (40000, 256, 392, 72)])
+def test_a_wait_that_runs_out_is_reported_in_every_form_and_direction(T, n, p, r, grad):
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(T + r)
+    codes, scale, zero = _layer(g, n, p, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, 3, r, n, p), _plan("mixed", T, 3, 2)
+    run, v = (layer.grad_input, _randn(g, T, p).bfloat16()) if grad else (layer.forward, _randn(g, T, n).bfloat16())
+    want = run(v, bank, plan), run(v)
+    adapt.check_device_status(DEV)
+    lib = adapt._library()
+    for args in ((v, bank, plan), (v,)):
+        assert lib.admmq_test_linear_set_wait(200000, 1) == B.OK
+        try:
+            run(*args)
+            with pytest.raises(adapt.AdmmqError) as e:
+                adapt.check_device_status(DEV)
+            assert e.value.status == B.ERR_TIMEOUT
+        finally:
+            assert lib.admmq_test_linear_set_wait(2_000_000_000, 0) == B.OK
+        assert torch.equal(run(v, bank, plan)[0], want[0][0]) and torch.equal(run(v)[0], want[1][0])
+        adapt.check_device_status(DEV)
+
+
 def test_a_whole_warp_wait_gives_every_lane_the_same_answer():
     """Also where some lanes give up before the barrier completes and the others would have seen it complete: the roles of
     the projections go on to warp-wide instructions by this answer."""

@@ -13,8 +13,9 @@ The common forms of the calls (new outputs, no conversion) go through the extens
 call that fails, take the path written here, which names what is wrong.
 
 torch is used for device memory and streams only; every step runs in the library's kernels, on the current stream of
-the tensors' device.  Argument errors raise AdmmqError before anything is enqueued; errors met on the device are kept in
-a status word, which `check_device_status` reads (it synchronises) and clears.
+the tensors' device.  Argument errors raise AdmmqError before anything is enqueued; errors met on the device by the calls
+that return at once are kept in a status word, one a device, which `check_device_status` reads (it synchronises) and clears.
+What QuantLinear and AdapterBank check of their arguments on the device they wait for, and raise, themselves.
 """
 from __future__ import annotations
 
@@ -119,6 +120,16 @@ def _status(index: int) -> int:
     return w[0]
 
 
+def _call_and_wait(fn, where: str, index: int, *args):
+    """fn(*args, status word, stream) with a word of its own, waited for: its error is not another call's, nor taken by
+    one."""
+    word = torch.zeros(1, dtype=torch.int32, device=f"cuda:{index}")
+    _call(fn, where, index, *args, word.data_ptr())
+    st = int(word.item())
+    if st != B.OK:
+        raise AdmmqError(st, where)
+
+
 def check_device_status(device: Union[str, torch.device] = "cuda:0", where: str = "device status"):
     """Waits for the device, raises AdmmqError for the first error that a call of this module met on it, and clears it."""
     device = torch.device(device)
@@ -179,9 +190,7 @@ class AdapterBank:
             self.check()
 
     def check(self):
-        _call(_library().admmq_adapters_check, "admmq_adapters_check", self.index, self._ref, self.d_in, self.d_out,
-              _status(self.index))
-        check_device_status(self.device, "admmq_adapters_check")
+        _call_and_wait(_library().admmq_adapters_check, "admmq_adapters_check", self.index, self._ref, self.d_in, self.d_out)
 
 
 class RequestPlan:
@@ -304,10 +313,9 @@ class QuantLinear:
         _need(nb > 0 and ng > 0, "QuantLinear: d_in and d_out multiples of 8, the group a multiple of 64", B.ERR_SHAPE)
         self.packed = torch.empty(nb, dtype=torch.uint8, device=self.device)
         self.grid = torch.empty(ng, dtype=torch.uint8, device=self.device)
-        _call(lib.admmq_pack_layer, "admmq_pack_layer", self.index, codes.data_ptr(), scale.data_ptr(), zero.data_ptr(),
-              self.d_in, self.d_out, bits, group_size, self.packed.data_ptr(), self.grid.data_ptr(),
-              _status(self.index))
-        check_device_status(self.device, "admmq_pack_layer")
+        _call_and_wait(lib.admmq_pack_layer, "admmq_pack_layer", self.index, codes.data_ptr(), scale.data_ptr(),
+                       zero.data_ptr(), self.d_in, self.d_out, bits, group_size, self.packed.data_ptr(),
+                       self.grid.data_ptr())
         self._c = PackedLayer(C.sizeof(PackedLayer), self.d_in, self.d_out, group_size, self.packed.data_ptr(),
                               self.grid.data_ptr())
         self._ref, self._status = C.addressof(self._c), _status(self.index)

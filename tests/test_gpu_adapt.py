@@ -615,6 +615,59 @@ def test_a_whole_warp_wait_gives_every_lane_the_same_answer():
         assert int(word) == (B.OK if answer else B.ERR_TIMEOUT)
 
 
+def _leave_an_error(adapt):
+    """A call whose error stays in the device's status word: a position past the table."""
+    q, w = torch.ones(1, 1, 16, device=DEV), torch.ones(16, device=DEV)
+    cos, pos = torch.ones(2, 8, device=DEV), torch.full((1,), 2, dtype=torch.int32, device=DEV)
+    adapt.qk_norm_rope(q, q, w, w, cos, cos, pos)
+
+
+def test_a_sound_layer_and_bank_do_not_meet_another_calls_error():
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(41)
+    codes, scale, zero = _layer(g, 128, 64, 4, 64)
+    adapt.check_device_status(DEV)
+    _leave_an_error(adapt)
+    adapt.QuantLinear(codes, scale, zero, 4, 64)
+    _bank(g, 2, 8, 128, 64).check()
+    with pytest.raises(adapt.AdmmqError) as e:                       # and the error is still there
+        adapt.check_device_status(DEV)
+    assert e.value.status == B.ERR_SHAPE
+    adapt.check_device_status(DEV)
+
+
+def test_threads_do_not_take_each_others_errors():
+    import threading
+    from paper_2605_11222_b200 import adapt, binding as B
+    codes, scale, zero = _layer(_gen(42), 64, 8, 3, 0)
+    codes[5, 60] = 8
+    adapt.check_device_status(DEV)
+    seen, stop = [], threading.Event()
+
+    def packs():
+        for _ in range(200):
+            try:
+                adapt.QuantLinear(codes, scale, zero, 3)
+                seen.append(B.OK)
+            except adapt.AdmmqError as e:
+                seen.append(e.status)
+        stop.set()
+
+    def checks():
+        while not stop.is_set():
+            try:
+                adapt.check_device_status(DEV)
+            except adapt.AdmmqError as e:
+                seen.append(e.status)
+
+    threads = [threading.Thread(target=f) for f in (packs, checks)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert seen == [B.ERR_INVALID_ARG] * 200
+
+
 # ------------------------------------------------------------------ checkpoints
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,n", [(0, 64), (1, 8), (3, 128), (5, 136), (77, 4096), (200, 1000), (2, 12288)])

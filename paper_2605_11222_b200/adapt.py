@@ -22,6 +22,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import threading
 from typing import Optional, Sequence, Union
 
 import numpy as np
@@ -108,15 +109,20 @@ _current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda
 
 
 _status_words: dict = {}
+_status_lock = threading.Lock()
 
 
 def _status(index: int) -> int:
-    """Pointer of a device's status word, made (zeroed) at its first use."""
+    """Pointer of a device's status word, made (zeroed) at its first use and kept for good."""
     w = _status_words.get(index)
     if w is None:
-        word = torch.zeros(4, dtype=torch.int32, device=f"cuda:{index}")
-        torch.cuda.synchronize(index)
-        w = _status_words[index] = (word.data_ptr(), word)
+        with _status_lock:                       # one word, whichever threads come first: kernels keep its pointer
+            w = _status_words.get(index)
+            if w is None:
+                with torch.inference_mode(False):    # (cleared in place later, in whatever mode)
+                    word = torch.zeros(4, dtype=torch.int32, device=f"cuda:{index}")
+                torch.cuda.synchronize(index)
+                w = _status_words[index] = (word.data_ptr(), word)
     return w[0]
 
 
@@ -137,10 +143,12 @@ def check_device_status(device: Union[str, torch.device] = "cuda:0", where: str 
     _status(index)
     word = _status_words[index][1]
     torch.cuda.synchronize(index)
-    st = int(word[0].item())
+    with _status_lock:                           # (an error that is there stays until it is cleared here)
+        st = int(word[0].item())
+        if st != B.OK:
+            word.zero_()
+            torch.cuda.synchronize(index)
     if st != B.OK:
-        word.zero_()
-        torch.cuda.synchronize(index)
         raise AdmmqError(st, where)
 
 

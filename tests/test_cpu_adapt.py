@@ -222,3 +222,32 @@ def test_waits_by_parity_of_the_pair_form_know_the_phase_before(adapt):
                     assert last < stages or last - stages <= done[g], (num_kb, extras, it)
                     done[g] = max(done[g], last)
                 it += 1
+
+
+def test_threads_share_one_status_word(adapt, monkeypatch):
+    """Two threads at a device's first call: one word, since kernels keep the pointer that the call was given."""
+    import threading
+    import time
+    index, made, got = 77, [], []
+    zeros, start = torch.zeros, threading.Barrier(8)
+
+    def slow_zeros(*size, **kw):
+        made.append(zeros(*size, dtype=kw["dtype"]))
+        time.sleep(0.02)
+        return made[-1]
+
+    def first_call():
+        start.wait()
+        got.append(adapt._status(index))
+
+    monkeypatch.setattr(torch, "zeros", slow_zeros)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+    threads = [threading.Thread(target=first_call) for _ in range(8)]
+    try:
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert len(made) == 1 and got == [made[0].data_ptr()] * 8
+    finally:
+        adapt._status_words.pop(index, None)

@@ -668,6 +668,21 @@ def test_threads_do_not_take_each_others_errors():
     assert seen == [B.ERR_INVALID_ARG] * 200
 
 
+def test_status_word_made_and_cleared_in_different_modes():
+    from paper_2605_11222_b200 import adapt
+    adapt.check_device_status(DEV)
+    kept = dict(adapt._status_words)             # (calls hold the pointer of the word that was there)
+    try:
+        adapt._status_words.clear()
+        with torch.inference_mode():
+            _leave_an_error(adapt)
+        with pytest.raises(adapt.AdmmqError):
+            adapt.check_device_status(DEV)
+    finally:
+        adapt._status_words.clear()
+        adapt._status_words.update(kept)
+
+
 # ------------------------------------------------------------------ checkpoints
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,n", [(0, 64), (1, 8), (3, 128), (5, 136), (77, 4096), (200, 1000), (2, 12288)])

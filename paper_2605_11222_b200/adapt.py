@@ -16,6 +16,11 @@ torch is used for device memory and streams only; every step runs in the library
 the tensors' device.  Argument errors raise AdmmqError before anything is enqueued; errors met on the device by the calls
 that return at once are kept in a status word, one a device, which `check_device_status` reads (it synchronises) and clears.
 What QuantLinear and AdapterBank check of their arguments on the device they wait for, and raise, themselves.
+
+No call records an autograd graph: the gradients have calls of their own.  QuantLinear.forward and qk_norm_rope refuse an
+x, q or k that requires grad while grad mode is on, where a graph would end without a word; call them in torch.no_grad(),
+from a torch.autograd.Function, or with detached tensors.  (Adapters and norm weights may require grad: whoever trains them
+puts what adapter_grads and qk_norm_rope_backward return into their .grad.)
 """
 from __future__ import annotations
 
@@ -154,6 +159,12 @@ def check_device_status(device: Union[str, torch.device] = "cuda:0", where: str 
 
 def _fail(status: int, what: str):
     raise AdmmqError(status, what)
+
+
+def _no_graph(name: str, *inputs: torch.Tensor):
+    if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
+        _fail(B.ERR_INVALID_ARG, f"{name}: an input requires grad, and the call records no graph (use torch.no_grad() or "
+              "detach(), and the call that forms the gradient)")
 
 
 def _rows(t: torch.Tensor, width: int, index: int, name: str) -> int:
@@ -372,6 +383,7 @@ class QuantLinear:
             r = self._quick(False, x, bank, plan)
             if r.__class__ is tuple:
                 return r
+        _no_graph("admmq_linear_forward", x)
         return self._run((_lib or _library()).admmq_linear_forward, "admmq_linear_forward", x, self.d_in, self.d_out, bank, plan,
                          out, h)
 
@@ -454,6 +466,8 @@ def _qk(fn, name, q, k, wq, wk, cos, sin, positions, eps, dq, dk, out_q, out_k):
             _fast.qk(word, q, k, wq, wk, cos, sin, positions, eps, dq, dk)
         if r.__class__ is tuple:
             return r
+    if dq is None:
+        _no_graph(name, q, k)
     dt, index = q.dtype, q.get_device()
     bf16 = dt is torch.bfloat16
     if not q.is_cuda or not (bf16 or dt is torch.float32):

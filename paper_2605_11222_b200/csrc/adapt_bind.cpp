@@ -6,6 +6,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -54,6 +55,8 @@ struct Current {
     stream = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(index)).stream();
   }
 };
+// An input that requires grad, with grad mode on: a graph that would end here.
+bool in_a_graph(const Tensor& t) { return t.requires_grad() && c10::GradMode::is_enabled(); }
 // A [rows, width] bf16 tensor of adjacent values; returns its row stride (that of a single row does not matter).
 long long rows_of(const Tensor& t, long long width, int index) {
   need(t.dim() == 2 && on(t, at::kBFloat16, index));
@@ -92,6 +95,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int* status = pointer<int>(a[5]);
     const Tensor& x = tensor(a[6]);
     const long long ld = rows_of(x, k, index), t = x.size(0);
+    need(grad || !in_a_graph(x));
     const auto call = grad ? admmq_linear_grad_input : admmq_linear_forward;
     const Current on_device(index);
     const Tensor y = make({t, m}, at::kBFloat16, index);
@@ -230,6 +234,7 @@ PyObject* qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
                  &sin = tensor(a[6]), &pos = tensor(a[7]);
     const at::ScalarType type = q.scalar_type();
     need(q.is_cuda() && (type == at::kBFloat16 || type == at::kFloat));
+    need(back || !(in_a_graph(q) || in_a_graph(k)));
     need(q.dim() == 3 && k.dim() == 3, ADMMQ_ERR_SHAPE);
     const int index = static_cast<int>(q.get_device());
     const long long t = q.size(0), hq = q.size(1), hk = k.size(1), d = q.size(2);

@@ -251,3 +251,14 @@ def test_threads_share_one_status_word(adapt, monkeypatch):
         assert len(made) == 1 and got == [made[0].data_ptr()] * 8
     finally:
         adapt._status_words.pop(index, None)
+
+
+def test_queries_in_a_graph_are_refused_before_anything_else(adapt):
+    from paper_2605_11222_b200 import binding as B
+    q, w = torch.ones(1, 1, 16), torch.ones(16)
+    args = (w, w, torch.ones(2, 8), torch.ones(2, 8), torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(adapt.AdmmqError, match="requires grad") as e:
+        adapt.qk_norm_rope(q.clone().requires_grad_(), q, *args)
+    assert e.value.status == B.ERR_INVALID_ARG
+    with torch.no_grad(), pytest.raises(adapt.AdmmqError, match="on a GPU"):
+        adapt.qk_norm_rope(q.clone().requires_grad_(), q, *args)

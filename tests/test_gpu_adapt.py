@@ -683,6 +683,57 @@ def test_status_word_made_and_cleared_in_different_modes():
         adapt._status_words.update(kept)
 
 
+@pytest.mark.parametrize("T", [5, 40])
+def test_an_input_in_a_graph_is_refused(T):
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(43)
+    codes, scale, zero = _layer(g, 128, 64, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, 2, 8, 128, 64), _plan("mixed", T, 2)
+    x = _randn(g, T, 128).bfloat16()
+    want = layer.forward(x, bank, plan)
+    out = torch.empty_like(want[0])
+    leaf = x.clone().requires_grad_()
+    for v in (leaf, leaf * 1):
+        for call in (lambda: layer.forward(v), lambda: layer.forward(v, bank, plan), lambda: layer.forward(v, bank, plan, out=out)):
+            with pytest.raises(adapt.AdmmqError, match="requires grad") as e:
+                call()
+            assert e.value.status == B.ERR_INVALID_ARG
+        with torch.no_grad():
+            assert torch.equal(layer.forward(v, bank, plan)[0], want[0])
+    assert torch.equal(layer.forward(leaf.detach(), bank, plan)[0], want[0])
+    with torch.inference_mode():
+        assert torch.equal(layer.forward(x.clone(), bank, plan)[0], want[0])
+    # adapters that require grad: as before
+    bank = adapt.AdapterBank(bank.down.requires_grad_(), bank.up.requires_grad_(), bank.scale)
+    assert torch.equal(layer.forward(x, bank, plan)[0], want[0])
+    # a graph's node of its own
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return layer.forward(x, bank, plan)[0]
+
+        @staticmethod
+        def backward(ctx, dy):
+            return layer.grad_input(dy, bank, plan)[0]
+
+    y = Layer.apply(leaf)
+    dy = _randn(g, T, 64).bfloat16()
+    y.backward(dy)
+    assert torch.equal(y, want[0]) and torch.equal(leaf.grad, layer.grad_input(dy, bank, plan)[0])
+    # queries and keys
+    q, w = _randn(g, T, 2, 64), torch.ones(64, device=DEV)
+    cos, pos = torch.ones(T, 32, device=DEV), torch.arange(T, device=DEV, dtype=torch.int32)
+    want = adapt.qk_norm_rope(q, q, w, w, cos, cos, pos)
+    leaf = q.clone().requires_grad_()
+    for a, b in ((leaf, q), (q, leaf)):
+        with pytest.raises(adapt.AdmmqError, match="requires grad"):
+            adapt.qk_norm_rope(a, b, w, w, cos, cos, pos)
+        with torch.no_grad():
+            assert all(torch.equal(s, t) for s, t in zip(adapt.qk_norm_rope(a, b, w, w, cos, cos, pos), want))
+    adapt.qk_norm_rope(q, q, w.clone().requires_grad_(), w, cos, cos, pos)
+    adapt.check_device_status(DEV)
+
+
 # ------------------------------------------------------------------ checkpoints
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,n", [(0, 64), (1, 8), (3, 128), (5, 136), (77, 4096), (200, 1000), (2, 12288)])

@@ -3,10 +3,10 @@
 // linear_small: y[t][j] = sum_i x[t][i] W[j][i], up to 16 rows.  Bound: memory, half a byte a weight, but at a few
 // megabytes the time is a chain of latencies: the launch, the loads, the products, one exchange, the store.  With
 // W = z0 + Delta k a group of input channels contributes  Delta sum k x + z0 sum x, so the tensor cores multiply the
-// codes themselves: 0x4300 | k is the bf16 number 128 + k, two codes leave a packed word per shift and mask, and
-//   y = sum over groups of  Delta (sum (128 + k) x) + (z0 - 128 Delta) sum x
-// in fp32, without a rounding of any weight.  (The offset 128 costs 7 of the 24 bits of the fp32 sums: 2^-17 relative,
-// under the 2^-8 of the output.)
+// codes themselves: 0x4180 | k << 3 is the bf16 number 16 + k, two codes leave a packed word per shift and mask, and
+//   y = sum over groups of  Delta (sum (16 + k) x) + (z0 - 16 Delta) sum x
+// in fp32, without a rounding of any weight.  (The offset is the smallest whose sums with every code lie between two powers
+// of two, so that the code is a field of the number; it costs 4 of the 24 bits of the fp32 sums.)
 // A CTA owns 16 (or 32) output channels.  Asynchronous copies bring a slice of the rows, the codes and the grid to shared
 // memory, all of a layer of 4096 input channels at once; sixteen warps split the slice and their sums meet at the end.
 // Channels are taken in an order that lets a thread read 16 of them from consecutive addresses for the codes and for x
@@ -181,10 +181,10 @@ __global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_smal
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           const uint32_t c0 = w == 0 ? c[m][0].x : c[m][0].y, c1 = w == 0 ? c[m][1].x : c[m][1].y;
-          const uint32_t a[4] = {((c0 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c1 >> (8 * s)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c0 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u,
-                                 ((c1 >> (8 * s + 4)) & 0x000F000Fu) | 0x43004300u};
+          const uint32_t a[4] = {((s == 0 ? c0 << 3 : c0 >> 5) & 0x00780078u) | 0x41804180u,
+                                 ((s == 0 ? c1 << 3 : c1 >> 5) & 0x00780078u) | 0x41804180u,
+                                 ((c0 >> (8 * s + 1)) & 0x00780078u) | 0x41804180u,
+                                 ((c1 >> (8 * s + 1)) & 0x00780078u) | 0x41804180u};
 #pragma unroll
           for (int t = 0; t < NT; ++t)
             mma_bf16(acc[m][t], a, s == 0 ? xv[t][w].x : xv[t][w].z, s == 0 ? xv[t][w].y : xv[t][w].w);
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(MAIN_THREADS, MT* NT == 1 ? 2 : 1) linear_smal
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const float2 g0 = gs[16 * m], g1 = gs[16 * m + 8];
-        const float z0 = fmaf(-128.0f, g0.x, g0.y), z1 = fmaf(-128.0f, g1.x, g1.y);
+        const float z0 = fmaf(-16.0f, g0.x, g0.y), z1 = fmaf(-16.0f, g1.x, g1.y);
         y[m][t][0] = fmaf(g0.x, acc[m][t][0], fmaf(z0, s0, y[m][t][0]));
         y[m][t][1] = fmaf(g0.x, acc[m][t][1], fmaf(z0, s1, y[m][t][1]));
         y[m][t][2] = fmaf(g1.x, acc[m][t][2], fmaf(z1, s0, y[m][t][2]));

@@ -615,6 +615,32 @@ def test_a_whole_warp_wait_gives_every_lane_the_same_answer():
         assert int(word) == (B.OK if answer else B.ERR_TIMEOUT)
 
 
+@pytest.mark.parametrize("T,p", [(1, 64), (5, 136), (16, 200), (12, 8200)])
+@pytest.mark.parametrize("n,group", [(64, 0), (512, 128), (4096, 0)])
+def test_few_rows_keep_sums_that_fp32_holds(T, p, n, group):
+    """Whole numbers: Delta = 1, z0 = -8, and in every 64 input channels two of 2^17 or -2^17 with the code 8 (weight 0)
+    beside sixteen of 1 to 3 and zeros.  The terms (16 + k) x of the 64, and the sums of them, stay below 2^23 (24 * 2^18
+    + 31 * 48), as do those of sum x times z0 - 16 Delta = -24, so every step is exact and the result, a whole number of at
+    most 8 * 48 * blocks, is too; it is rounded once, to bf16."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + n)
+    blocks = n // 64
+    codes = torch.randint(0, 16, (p, n), generator=g, device=DEV, dtype=torch.uint8)
+    x = torch.zeros(T, n, device=DEV)
+    for b in range(blocks):
+        at = torch.randperm(64, generator=g, device=DEV) + 64 * b
+        sign = torch.randint(0, 2, (T, 1), generator=g, device=DEV) * 2 - 1
+        x[:, at[:2]] = 2.0 ** 17 * sign
+        codes[:, at[:2]] = 8
+        x[:, at[2:18]] = torch.randint(1, 4, (T, 16), generator=g, device=DEV).float()
+    groups = n // (group or n)
+    scale, zero = torch.ones(p, groups, device=DEV), torch.full((p, groups), -8.0, device=DEV)
+    y, _ = adapt.QuantLinear(codes, scale, zero, 4, group).forward(x.bfloat16())
+    assert torch.equal(x.bfloat16().float(), x)
+    want = x.double() @ (codes.double() - 8).T
+    assert torch.equal(y, want.float().bfloat16())
+
+
 def _leave_an_error(adapt):
     """A call whose error stays in the device's status word: a position past the table."""
     q, w = torch.ones(1, 1, 16, device=DEV), torch.ones(16, device=DEV)

@@ -113,7 +113,7 @@ admmq_status admmq_adapter_grad(const admmq_adapter_grad_args* args, void* cuda_
  *   scale = max |x| / 127,  code = round(x / scale) to nearest, ties to even, in [-127, 127]
  * (code 0 where scale is 0; a block that holds a non-finite value gets scale NaN and is restored as NaN).
  * x: [n_rows][ldx] fp32 or bf16, width a multiple of 8; codes [n_rows][width] int8, scale
- * [n_rows][ceil(width / 128)].  restore writes scale * code as out [n_rows][ldo] of the given type. */
+ * [n_rows][ceil(width / 128)], at most 2^31 - 1 of them.  restore writes scale * code as out [n_rows][ldo] of the given type. */
 admmq_status admmq_checkpoint_save(const void* d_x, admmq_dtype dtype, long long n_rows, int width, long long ldx,
                                    signed char* d_codes, float* d_scale, void* cuda_stream);
 admmq_status admmq_checkpoint_restore(const signed char* d_codes, const float* d_scale, long long n_rows, int width,

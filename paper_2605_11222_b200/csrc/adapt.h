@@ -91,6 +91,8 @@ cudaError_t launch_linear_tc(bool grad, const PackedLayer& L, const AdapterView*
 // ---- adapter_grad.cu ----
 cudaError_t launch_adapter_grad(const admmq_adapter_grad_args& a, cudaStream_t stream);
 // ---- checkpoint8.cu ----
+// Most blocks of a checkpoint: of rows of two blocks or more, 2^31 and their values do not fit a device (180 GB).
+constexpr long long CHECKPOINT_MAX_BLOCKS = 0x7fffffffLL;
 cudaError_t launch_checkpoint_save(const void* x, int is_bf16, long long T, int width, long long ldx, int8_t* codes,
                                    float* scale, cudaStream_t stream);
 cudaError_t launch_checkpoint_restore(const int8_t* codes, const float* scale, long long T, int width, void* out,

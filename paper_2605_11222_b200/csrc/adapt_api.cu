@@ -97,6 +97,10 @@ admmq_status check_bank(const admmq_adapters* b) {
   return b->rank < 8 || b->rank > ADMMQ_ADAPT_MAX_RANK || b->rank % 8 ? ADMMQ_ERR_SHAPE : ADMMQ_OK;
 }
 bool rows_ok(long long n) { return n >= 0 && n <= ADMMQ_ADAPT_MAX_ROWS; }
+bool checkpoint_ok(long long n_rows, int width) {
+  return width >= 8 && width <= (1 << 20) && width % 8 == 0 && rows_ok(n_rows) &&
+         n_rows * ((width + ADMMQ_CHECKPOINT_BLOCK - 1) / ADMMQ_CHECKPOINT_BLOCK) <= CHECKPOINT_MAX_BLOCKS;
+}
 
 admmq_status linear(bool grad, const admmq_packed_layer* layer, const admmq_adapters* bank, long long n_rows,
                     const int* row_adapter, const void* x, long long ldx, void* y, long long ldy, float* h,
@@ -244,7 +248,7 @@ admmq_status admmq_adapter_grad(const admmq_adapter_grad_args* a, void* cuda_str
 admmq_status admmq_checkpoint_save(const void* d_x, admmq_dtype dtype, long long n_rows, int width, long long ldx,
                                    signed char* d_codes, float* d_scale, void* cuda_stream) {
   if (dtype != ADMMQ_F32 && dtype != ADMMQ_BF16) return ADMMQ_ERR_INVALID_ARG;
-  if (width < 8 || width > (1 << 20) || width % 8 || !rows_ok(n_rows)) return ADMMQ_ERR_SHAPE;
+  if (!checkpoint_ok(n_rows, width)) return ADMMQ_ERR_SHAPE;
   if (ldx < width || ldx % (dtype == ADMMQ_BF16 ? 8 : 4)) return ADMMQ_ERR_SHAPE;
   if (n_rows == 0) return ADMMQ_OK;
   if (!aligned(d_x, 16) || !aligned(d_codes, 16) || !aligned(d_scale, 4)) return ADMMQ_ERR_INVALID_ARG;
@@ -254,7 +258,7 @@ admmq_status admmq_checkpoint_save(const void* d_x, admmq_dtype dtype, long long
 admmq_status admmq_checkpoint_restore(const signed char* d_codes, const float* d_scale, long long n_rows, int width,
                                       void* d_out, admmq_dtype dtype, long long ldo, void* cuda_stream) {
   if (dtype != ADMMQ_F32 && dtype != ADMMQ_BF16) return ADMMQ_ERR_INVALID_ARG;
-  if (width < 8 || width > (1 << 20) || width % 8 || !rows_ok(n_rows)) return ADMMQ_ERR_SHAPE;
+  if (!checkpoint_ok(n_rows, width)) return ADMMQ_ERR_SHAPE;
   if (ldo < width || ldo % (dtype == ADMMQ_BF16 ? 8 : 4)) return ADMMQ_ERR_SHAPE;
   if (n_rows == 0) return ADMMQ_OK;
   if (!aligned(d_out, 16) || !aligned(d_codes, 16) || !aligned(d_scale, 4)) return ADMMQ_ERR_INVALID_ARG;

@@ -22,16 +22,10 @@ constexpr int PAIRS = THREADS / LANES * UNROLL;   // (row, block) pairs of one C
 struct Pairs {
   long long row0;
   uint32_t blk0, nb, inv;                   // inv = ceil(2^32 / nb): exact quotients for numbers below 2^32 / nb
-  __device__ __forceinline__ Pairs(long long T, uint32_t nb_, uint32_t inv_) : nb(nb_), inv(inv_) {
-    const long long first = (long long)blockIdx.x * PAIRS;
-    if (T * nb <= 0x7fffffffLL) {
-      const uint32_t r = (uint32_t)first / nb;
-      row0 = r;
-      blk0 = (uint32_t)first - r * nb;
-    } else {
-      row0 = first / nb;
-      blk0 = (uint32_t)(first - row0 * nb);
-    }
+  __device__ __forceinline__ Pairs(uint32_t nb_, uint32_t inv_) : nb(nb_), inv(inv_) {
+    const uint32_t first = blockIdx.x * (uint32_t)PAIRS, r = first / nb;      // (at most 2^31 pairs)
+    row0 = r;
+    blk0 = first - r * nb;
   }
   __device__ __forceinline__ void at(uint32_t off, long long& row, int& blk) const {
     const uint32_t n = blk0 + off, r = nb == 1 ? n : __umulhi(n, inv);
@@ -64,7 +58,7 @@ checkpoint_save_kernel(const void* __restrict__ x, long long T, int width, long 
   constexpr int Q = BF16 ? 1 : 2;           // 16-byte loads of 8 values
   constexpr int LN = LANES / 2, TAKE = 2;   // threads of a block, blocks of a thread
   static_assert(THREADS / LN * TAKE == PAIRS, "the CTA's pairs");
-  const Pairs pairs(T, nb, nb_inv);
+  const Pairs pairs(nb, nb_inv);
   const int sub = threadIdx.x / LN, lane = threadIdx.x % LN;
   uint4 raw[TAKE][2][Q];
   long long row[TAKE];
@@ -157,7 +151,7 @@ template <bool BF16>
 __global__ void __launch_bounds__(THREADS)
 checkpoint_restore_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scale, long long T, int width,
                           uint32_t nb, uint32_t nb_inv, void* __restrict__ out, long long ldo) {
-  const Pairs pairs(T, nb, nb_inv);
+  const Pairs pairs(nb, nb_inv);
   const int sub = threadIdx.x / LANES, lane = threadIdx.x % LANES;
   uint2 raw[UNROLL];
   float s[UNROLL];
@@ -198,20 +192,17 @@ checkpoint_restore_kernel(const int8_t* __restrict__ codes, const float* __restr
 
 }  // namespace
 
-// CTAs for T rows of nb blocks, and ceil(2^32 / nb); false if the grid cannot hold them.
-static bool plan_pairs(long long T, int nb, unsigned* ctas, uint32_t* inv) {
-  const long long n = (T * nb + PAIRS - 1) / PAIRS;
-  *ctas = (unsigned)n;
+// CTAs for T rows of nb blocks (at most CHECKPOINT_MAX_BLOCKS in all), and ceil(2^32 / nb).
+static unsigned plan_pairs(long long T, int nb, uint32_t* inv) {
   *inv = (uint32_t)(((1ULL << 32) + nb - 1) / nb);            // (nb = 1 does not use it)
-  return n <= 0x7fffffffLL;
+  return (unsigned)((T * nb + PAIRS - 1) / PAIRS);
 }
 
 cudaError_t launch_checkpoint_save(const void* x, int is_bf16, long long T, int width, long long ldx, int8_t* codes,
                                    float* scale, cudaStream_t stream) {
   const int nb = (width + BLOCK - 1) / BLOCK;
-  unsigned ctas;
   uint32_t inv;
-  if (!plan_pairs(T, nb, &ctas, &inv)) return cudaErrorInvalidValue;
+  const unsigned ctas = plan_pairs(T, nb, &inv);
   if (is_bf16)
     checkpoint_save_kernel<true><<<ctas, THREADS, 0, stream>>>(x, T, width, ldx, nb, inv, codes, scale);
   else
@@ -222,9 +213,8 @@ cudaError_t launch_checkpoint_save(const void* x, int is_bf16, long long T, int 
 cudaError_t launch_checkpoint_restore(const int8_t* codes, const float* scale, long long T, int width, void* out,
                                       int is_bf16, long long ldo, cudaStream_t stream) {
   const int nb = (width + BLOCK - 1) / BLOCK;
-  unsigned ctas;
   uint32_t inv;
-  if (!plan_pairs(T, nb, &ctas, &inv)) return cudaErrorInvalidValue;
+  const unsigned ctas = plan_pairs(T, nb, &inv);
   if (is_bf16)
     checkpoint_restore_kernel<true><<<ctas, THREADS, 0, stream>>>(codes, scale, T, width, nb, inv, out, ldo);
   else

@@ -262,3 +262,11 @@ def test_queries_in_a_graph_are_refused_before_anything_else(adapt):
     assert e.value.status == B.ERR_INVALID_ARG
     with torch.no_grad(), pytest.raises(adapt.AdmmqError, match="on a GPU"):
         adapt.qk_norm_rope(q.clone().requires_grad_(), q, *args)
+
+
+def test_a_checkpoint_of_more_blocks_than_a_device_holds_is_refused(adapt):
+    from paper_2605_11222_b200 import binding as B
+    lib = adapt._library()
+    for rows, width in ((2 ** 30, 136), (2 ** 30, 256), (2 ** 24, 16384), (2 ** 18, 2 ** 20)):      # 2^31 blocks and more
+        assert lib.admmq_checkpoint_save(FAKE, 1, rows, width, width, FAKE, FAKE, None) == B.ERR_SHAPE
+        assert lib.admmq_checkpoint_restore(FAKE, FAKE, rows, width, FAKE, 1, width, None) == B.ERR_SHAPE

@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadmmq.so")
 BIND = os.path.join(HERE, "_adapt.so")
+BIND_FOR = os.path.join(OBJ, "_adapt.for")     # the Python and the torch that _adapt.so was built for
 SOURCES = ["api.cu", "elem.cu", "gemm_simt.cu", "gemm_tc.cu", "tridiag.cu", "tridiag_blocked.cu", "local_search.cu", "pair_swap.cu",
            "objective_static.cu", "adapt_api.cu", "linear_small.cu", "shrink_tc.cu", "linear_tc.cu", "linear_pair.cu", "adapter_grad.cu", "checkpoint8.cu",
            "qk_rope.cu"]
@@ -55,10 +56,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def _bind_for() -> str:
+    """What _adapt.so depends on besides this repository: it uses internals of torch and of the running Python."""
+    import torch
+    return f"python {sys.version} torch {torch.__version__} abi {int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+
+
+def _bind_is_current(sources) -> bool:
+    if _newer(sources, BIND) or not os.path.exists(BIND_FOR):
+        return False
+    with open(BIND_FOR) as f:
+        return f.read() == _bind_for()
+
+
 def _build_bind(force: bool, headers) -> None:
     """The Python calls of the operators (CPython and torch C++, no device code)."""
     src = os.path.join(CSRC, "adapt_bind.cpp")
-    if not force and not _newer([src] + headers, BIND):
+    if not force and _bind_is_current([src] + headers):
         return
     import sysconfig
 
@@ -74,6 +88,8 @@ def _build_bind(force: bool, headers) -> None:
                         "-Wl,-rpath,$ORIGIN"], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"building {BIND} failed:\n{r.stdout}\n{r.stderr}")
+    with open(BIND_FOR, "w") as f:
+        f.write(_bind_for())
 
 
 if __name__ == "__main__":

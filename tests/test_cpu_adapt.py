@@ -270,3 +270,33 @@ def test_a_checkpoint_of_more_blocks_than_a_device_holds_is_refused(adapt):
     for rows, width in ((2 ** 30, 136), (2 ** 30, 256), (2 ** 24, 16384), (2 ** 18, 2 ** 20)):      # 2^31 blocks and more
         assert lib.admmq_checkpoint_save(FAKE, 1, rows, width, width, FAKE, FAKE, None) == B.ERR_SHAPE
         assert lib.admmq_checkpoint_restore(FAKE, FAKE, rows, width, FAKE, 1, width, None) == B.ERR_SHAPE
+
+
+def test_the_extension_is_rebuilt_for_another_torch_or_python(adapt, monkeypatch, tmp_path):
+    """It is compiled against their internals: a change of either makes it stale, whatever the sources' dates."""
+    import os
+    import subprocess
+    from paper_2605_11222_b200 import build
+    so, runs = tmp_path / "_adapt.so", []
+
+    def compiler(cmd, **kw):
+        runs.append(cmd)
+        so.write_bytes(b"")
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(build, "BIND", os.fspath(so))
+    monkeypatch.setattr(build, "BIND_FOR", os.fspath(tmp_path / "_adapt.for"), raising=False)
+    monkeypatch.setattr(build.subprocess, "run", compiler)
+    build._build_bind(False, [])
+    build._build_bind(False, [])
+    assert len(runs) == 1
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.0")
+        build._build_bind(False, [])
+        assert len(runs) == 2
+    build._build_bind(False, [])                 # and back
+    assert len(runs) == 3
+    with monkeypatch.context() as m:
+        m.setattr("sys.version", "0.0.0 of another build")
+        build._build_bind(False, [])
+        assert len(runs) == 4

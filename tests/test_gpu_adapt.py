@@ -879,6 +879,47 @@ def test_qk_norm_rope_backward(T, hq, hk, d, rot, dtype):
         _within(gw, ww, half * ww.abs() + 64 * 2.0 ** -24 * (ga * n.abs()).sum((0, 1)) + 1e-30)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,hq,hk,d,rot", [(1, 3, 2, 64, 32), (7, 1, 1, 128, 128), (260, 5, 2, 96, 64), (3000, 2, 3, 64, 64)])
+def test_qk_strides_of_every_argument(T, hq, hk, d, rot, dtype):
+    """Inputs, upstream gradients and outputs as views into joint buffers of different widths, heads apart and out of
+    order: the bits of the dense call, and nothing written beside the views."""
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + 7)
+    q, k, wq, wk, cos, sin, pos = _qk_inputs(T, hq, hk, d, rot, dtype, g)
+    dyq, dyk = _randn(g, T, hq, d).to(dtype), _randn(g, T, hk, d).to(dtype)
+
+    def views(a, b, pad):
+        """a and b in one buffer: b's heads first, each head followed by `pad` other values, `pad` more at a row's end."""
+        buf = torch.full((T, (hq + hk) * (d + pad) + pad), 9.0, dtype=dtype, device=DEV)
+        vb = buf[:, :hk * (d + pad)].view(T, hk, d + pad)[..., :d]
+        va = buf[:, hk * (d + pad):(hq + hk) * (d + pad)].view(T, hq, d + pad)[..., :d]
+        if a is not None:
+            va.copy_(a)
+            vb.copy_(b)
+        return va, vb, buf
+
+    def untouched(va, vb, buf):
+        va.fill_(9.0)
+        vb.fill_(9.0)
+        return bool((buf == 9).all())
+
+    sq, sk, _ = views(q, k, 8)
+    sdq, sdk, _ = views(dyq, dyk, 24)
+    dense = adapt.qk_norm_rope(q.contiguous(), k.contiguous(), wq, wk, cos, sin, pos)
+    assert all(torch.equal(a, b) for a, b in zip(adapt.qk_norm_rope(sq, sk, wq, wk, cos, sin, pos), dense))
+    oq, ok, buf = views(None, None, 16)
+    adapt.qk_norm_rope(sq, sk, wq, wk, cos, sin, pos, out_q=oq, out_k=ok)
+    assert torch.equal(oq, dense[0]) and torch.equal(ok, dense[1]) and untouched(oq, ok, buf)
+    dense = adapt.qk_norm_rope_backward(q.contiguous(), k.contiguous(), wq, wk, cos, sin, pos, dyq, dyk)
+    got = adapt.qk_norm_rope_backward(sq, sk, wq, wk, cos, sin, pos, sdq, sdk)
+    assert all(torch.equal(a, b) for a, b in zip(got, dense))
+    got = adapt.qk_norm_rope_backward(sq, sk, wq, wk, cos, sin, pos, sdq, sdk, out_q=oq, out_k=ok)
+    assert got[0] is oq and got[1] is ok
+    assert all(torch.equal(a, b) for a, b in zip(got, dense)) and untouched(oq, ok, buf)
+    adapt.check_device_status(DEV)
+
+
 def test_qk_gradient_agrees_with_differences():
     """Central differences of the fp32 forward call: error of order step^2 third derivatives plus the forward's
     rounding over the step; both are below 1e-3 of the gradient's scale at the step used."""

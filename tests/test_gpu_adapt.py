@@ -381,6 +381,25 @@ def test_a_wait_of_the_contraction_that_runs_out_is_reported():
     assert torch.equal(got, want) and torch.equal(h, wanth)
 
 
+@pytest.mark.parametrize("T,n,p,r", [(1, 64, 72, 8), (70, 264, 128, 24), (900, 512, 392, 64)])
+def test_adapter_grads_of_strided_rows_into_given_tensors(T, n, p, r):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + r)
+    bank, plan = _bank(g, 3, r, n, p), _plan("mixed", T, 3, 1)
+    x, dy = _randn(g, T, n + 40).bfloat16(), (_randn(g, T, p + 8) * 1e-3).bfloat16()
+    h, u = _randn(g, T, r), _randn(g, T, r) * 1e-3
+    xs, dys = x[:, 16:16 + n], dy[:, 8:]
+    for v, dense in ((xs, xs.contiguous()), (adapt.Checkpoint.save(xs), adapt.Checkpoint.save(xs.contiguous()))):
+        want = adapt.adapter_grads(bank, plan, dense, h, dys.contiguous(), u)
+        got = adapt.adapter_grads(bank, plan, v, h, dys, u)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        gd, gu = torch.full_like(bank.down, 9.0), torch.full_like(bank.up, 9.0)
+        for given in (dict(grad_down=gd, grad_up=gu), dict(grad_down=gd), dict(grad_up=gu)):
+            got = adapt.adapter_grads(bank, plan, v, h, dys, u, **given)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            assert got[0] is given.get("grad_down", got[0]) and got[1] is given.get("grad_up", got[1])
+
+
 def test_adapter_grads_are_the_same_bits_every_time():
     from paper_2605_11222_b200 import adapt
     g = _gen(9)
@@ -917,6 +936,24 @@ def test_qk_strides_of_every_argument(T, hq, hk, d, rot, dtype):
     got = adapt.qk_norm_rope_backward(sq, sk, wq, wk, cos, sin, pos, sdq, sdk, out_q=oq, out_k=ok)
     assert got[0] is oq and got[1] is ok
     assert all(torch.equal(a, b) for a, b in zip(got, dense)) and untouched(oq, ok, buf)
+    adapt.check_device_status(DEV)
+
+
+@pytest.mark.parametrize("T", [0, 1, 700])
+def test_queries_without_keys(T):
+    from paper_2605_11222_b200 import adapt
+    g = _gen(T + 9)
+    q, _, wq, wk, cos, sin, pos = _qk_inputs(T, 4, 0, 64, 64, torch.bfloat16, g)
+    k = torch.empty(T, 0, 64, dtype=torch.bfloat16, device=DEV)
+    dq = _randn(g, T, 4, 64).bfloat16()
+    both, back = adapt.qk_norm_rope(q, q, wq, wq, cos, sin, pos), adapt.qk_norm_rope_backward(q, q, wq, wq, cos, sin, pos, dq, dq)
+    yq, yk = adapt.qk_norm_rope(q, k, wq, wk, cos, sin, pos)
+    assert torch.equal(yq, both[0]) and yk.shape == (T, 0, 64)
+    gq, gk, gwq, gwk = adapt.qk_norm_rope_backward(q, k, wq, wk, cos, sin, pos, dq, torch.empty_like(k))
+    assert torch.equal(gq, back[0]) and gk.shape == (T, 0, 64) and bool((gwk == 0).all())
+    # another number of CTAs adds the weight's gradient in another order: two roundings of the output, and 64 half ulps of
+    # the sum of magnitudes (4 T terms of less than 2.5 on average) in each
+    assert bool(((gwq.float() - back[2].float()).abs() <= 2 * EPS * back[2].float().abs() + 2.0 ** -17 * 10 * T).all())
     adapt.check_device_status(DEV)
 
 

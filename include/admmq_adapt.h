@@ -75,7 +75,11 @@ admmq_status admmq_adapters_check(const admmq_adapters* bank, int d_in, int d_ou
  * grad_input: u_t = scale_a up_a   dy_t,  dx_t = W^T dy_t + down_a^T u_t      dy [n_rows][lddy], dx [n_rows][lddx] bf16
  * a = d_row_adapter[t]; a value outside [0, n_adapters) means none (h_t = u_t = 0).  bank NULL: no adapters, and
  * d_row_adapter and d_h / d_u are ignored.  d_h, d_u: [n_rows][rank] fp32, outputs (the backward pass reads them).
- * One launch without adapters, two with them, of which the second overlaps the first. */
+ * One launch without adapters, two with them, of which the second overlaps the first.
+ * Roundings.  Up to 16 rows the forward call multiplies the codes themselves, and y carries the rounding of its 32-bit sum
+ * to bf16 alone.  Above, and in grad_input always, the tensor cores take W (once z0 + Delta k is formed in fp32) and h or
+ * u as bf16 operands; so a row's last bits may change when its batch passes 16 rows, and the W of the gradient is the
+ * rounded one. */
 admmq_status admmq_linear_forward(const admmq_packed_layer* layer, const admmq_adapters* bank, long long n_rows,
                                   const int* d_row_adapter, const void* d_x, long long ldx, void* d_y, long long ldy,
                                   float* d_h, int* d_status, void* cuda_stream);

@@ -8,14 +8,15 @@
 // operands of mma.sync: the contraction runs over the rows, so both operands are read across their storage order.
 // Four CTAs a multiprocessor (rank 16) hide a tile's chain of arrival, conversion, barrier and products better than
 // more tiles in flight in fewer CTAs: 8192 rows of 12288 (8 bits) + 4096 columns take 66 us, with four tiles ahead in two
-// CTAs 84, with asynchronous copies to shared memory 129; what is left is the issue of some 200 instructions a warp and
-// tile, 80 of them the conversion of codes.  (The tensor work, 2 rank flop a value read, is far below what mma.sync
+// CTAs 84, with asynchronous copies to shared memory 129 (x in bf16 65 us); what is left is the way of every value through
+// shared memory, which is 74 % busy, and the issue of some 200 instructions a warp and tile, 80 of them the conversion of
+// codes.  (The tensor work, 2 rank flop a value read, is far below what mma.sync
 // delivers: tcgen05 would wait for the same loads.)
 // The shares of one (adapter, columns) tile form a cluster; their fp32 sums meet over distributed shared memory and
 // are added in rank order, so nothing goes through global memory and the result does not depend on timing.
 //
 // Rounding.  x^ = scale code: the code (at most 127) is exact in bf16 and the scale is multiplied into f in fp32, so
-// f scale is rounded once, as f is on the bf16 path: 2^-9 relative a term, the size of the output's own rounding.
+// f scale is rounded once, as f is on the bf16 path: at most 2^-8 relative a term, the size of the output's own rounding.
 #include <cooperative_groups.h>
 
 #include "adapt.h"

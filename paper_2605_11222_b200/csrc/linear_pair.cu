@@ -17,6 +17,9 @@
 // Adapters are further K steps: a step holds as many of the tile's adapters as fit in 64 rank rows; the N operand is
 // their output sides, the M operand is h in bf16, zero where a row has another adapter.
 // Waits are bounded as in the other tensor-core kernels.  No multicast load anywhere.
+// 6011 rows of 4096 -> 4096 without adapters: 153 us, the tensor pipe busy 68 % of the cycles.  192 tiles on 74 pairs are
+// 2.6 turns, of which three are paid for, and a tile takes some 17000 cycles beside its 65000 of MMAs (its start, and its way
+// out of tensor memory, which one set of accumulators does not overlap).
 #include <atomic>
 
 #include "../../include/admmq_testing.h"

@@ -3,7 +3,7 @@
 //   grad_input  dx[t][m] = sum_k dy[t][k] W[k][m] + sum_r u[t][r] down_a[r][m]    (m: input channel, k: output channel)
 //
 // The product is formed as D[m][t]: weights are the M operand (128 rows of tensor memory), rows the N operand.  A K step
-// of 64 takes 128 x 64 weights, which eight warps expand from codes into the 128-byte-swizzled shared-memory tile:
+// of 64 takes 128 x 64 weights, which four warps expand from codes into the 128-byte-swizzled shared-memory tile:
 // 128 runs of 64 input channels of one output channel, in both directions -- forward they are 128 output channels
 // (K-major operand), backward 64 output channels times two runs (M-major operand); only the descriptors differ.
 // Weights are expanded in fp32 (z0 + Delta k, one fma) and rounded once to bf16: the rounding of a weight is random

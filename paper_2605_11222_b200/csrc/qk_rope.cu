@@ -13,7 +13,8 @@
 // the copy rate.  Backward the grid is the resident one: a thread sums the weight's gradient over all its rows in 16
 // registers, the CTA's sums go to a workspace, and a second launch adds them in a fixed order.  That leaves few warps, so
 // what a thread needs next, up to DEPTH heads ahead and across rows, is on its way into slots of shared memory of its
-// own (asynchronous copies: no registers, no barrier); with loads into registers 8192 rows took 58 us.
+// own (asynchronous copies: no registers, no barrier); with loads into registers 8192 rows took 58 us, so 55.  What bounds
+// it there is latency with 16 warps a multiprocessor (128 registers a thread): DRAM is 50 % busy, issue slots 60 %.
 #include "adapt.h"
 
 namespace admmq {

@@ -187,7 +187,8 @@ class AdapterBank:
     """Low-rank adapters of one layer: adapter a adds scale[a] * up[a]^T (down[a] x).
 
     down [n, rank, d_in] and up [n, rank, d_out] bf16 (both rank-major), scale [n] fp32; the tensors are used in place,
-    so a bank sees what an optimizer writes into them.  check: reads the bank once and raises if an entry is not
+    so a bank sees what an optimizer writes into them; one whose storage is replaced (`t.data = ...`, a module moved) needs a
+    new bank, and calls with the old one are refused.  check: reads the bank once and raises if an entry is not
     finite (rows of different requests share tensor-core tiles; call `check` again after loading other values)."""
 
     def __init__(self, down: torch.Tensor, up: torch.Tensor, scale: torch.Tensor, check: bool = True):
@@ -208,7 +209,13 @@ class AdapterBank:
         if check:
             self.check()
 
+    def _in_place(self, name: str):
+        c = self._c
+        if (self.down.data_ptr(), self.up.data_ptr(), self.scale.data_ptr()) != (c.d_down, c.d_up, c.d_scale):
+            _fail(B.ERR_INVALID_ARG, name + ": a tensor of the bank has other storage than when the bank was made")
+
     def check(self):
+        self._in_place("admmq_adapters_check")
         _call_and_wait(_library().admmq_adapters_check, "admmq_adapters_check", self.index, self._ref, self.d_in, self.d_out)
 
 
@@ -346,7 +353,7 @@ class QuantLinear:
         if plan is None or bank._fits != (self.d_in, self.d_out, self.index, plan.n_adapters) or plan.index != self.index:
             return B.ERR_SHAPE
         return _fast.linear(grad, self._ref, self.d_in, self.d_out, self.index, self._status, x, bank._ref, bank.rank,
-                            plan.n_rows, plan._ptr[0])
+                            plan.n_rows, plan._ptr[0], bank.down, bank.up, bank.scale)
 
     def _run(self, fn, name, x, k, m, bank, plan, out, factor):
         index = self.index
@@ -367,6 +374,7 @@ class QuantLinear:
             _fail(B.ERR_SHAPE, name + ": bank, plan and layer differ")
         if bank.index != index or plan.index != index:
             _fail(B.ERR_INVALID_ARG, name + ": bank and plan on the layer's device")
+        bank._in_place(name)
         if factor is None:
             factor = x.new_empty((t, bank.rank), dtype=torch.float32)
         else:

@@ -83,11 +83,11 @@ PyObject* status_of(const Refused& r) {
 }
 
 // linear(grad, layer, d_in, d_out, device, status, x) or
-// linear(grad, layer, d_in, d_out, device, status, x, bank, rank, n_rows, row_adapter) -> (y, h or None)
+// linear(grad, layer, d_in, d_out, device, status, x, bank, rank, n_rows, row_adapter, down, up, scale) -> (y, h or None)
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    need(n == 7 || n == 11);
+    need(n == 7 || n == 14);
     const bool grad = a[0] == Py_True;
     const auto* layer = pointer<const admmq_packed_layer>(a[1]);
     const long long d_in = integer(a[2]), d_out = integer(a[3]), k = grad ? d_out : d_in, m = grad ? d_in : d_out;
@@ -106,8 +106,11 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return tuple_of({y, Tensor()});
     }
     need(integer(a[9]) == t, ADMMQ_ERR_SHAPE);
+    const auto* bank = pointer<const admmq_adapters>(a[7]);
+    need(tensor(a[11]).const_data_ptr() == bank->d_down && tensor(a[12]).const_data_ptr() == bank->d_up &&
+         tensor(a[13]).const_data_ptr() == bank->d_scale);
     const Tensor h = make({t, integer(a[8])}, at::kFloat, index);
-    const int st = call(layer, pointer<const admmq_adapters>(a[7]), t, pointer<const int>(a[10]), x.const_data_ptr(), ld,
+    const int st = call(layer, bank, t, pointer<const int>(a[10]), x.const_data_ptr(), ld,
                         y.mutable_data_ptr(), m, static_cast<float*>(h.mutable_data_ptr()), status, on_device.stream);
     need(st == ADMMQ_OK, st);
     return tuple_of({y, h});

@@ -660,6 +660,27 @@ def test_few_rows_keep_sums_that_fp32_holds(T, p, n, group):
     assert torch.equal(y, want.float().bfloat16())
 
 
+@pytest.mark.parametrize("which", ["down", "up", "scale"])
+def test_a_bank_whose_tensor_has_other_storage_is_refused(which):
+    """The bank holds the addresses: with another storage behind the tensor they may be anyone's memory."""
+    from paper_2605_11222_b200 import adapt, binding as B
+    g = _gen(44)
+    codes, scale, zero = _layer(g, 128, 64, 4, 64)
+    layer, bank, plan = adapt.QuantLinear(codes, scale, zero, 4, 64), _bank(g, 2, 8, 128, 64), _plan("mixed", 9, 2)
+    x, out = _randn(g, 9, 128).bfloat16(), torch.empty(9, 64, dtype=torch.bfloat16, device=DEV)
+    layer.forward(x, bank, plan)
+    t = getattr(bank, which)
+    old = t.detach()                              # (keeps the old storage)
+    t.data = t.clone()
+    for call in (lambda: layer.forward(x, bank, plan), lambda: layer.forward(x, bank, plan, out=out),
+                 lambda: layer.grad_input(out, bank, plan), bank.check):
+        with pytest.raises(adapt.AdmmqError, match="storage") as e:
+            call()
+        assert e.value.status == B.ERR_INVALID_ARG
+    new = adapt.AdapterBank(bank.down, bank.up, bank.scale)
+    assert torch.isfinite(layer.forward(x, new, plan)[0].float()).all() and old.data_ptr() != t.data_ptr()
+
+
 def _leave_an_error(adapt):
     """A call whose error stays in the device's status word: a position past the table."""
     q, w = torch.ones(1, 1, 16, device=DEV), torch.ones(16, device=DEV)

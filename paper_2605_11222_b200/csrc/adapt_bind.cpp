@@ -15,7 +15,7 @@
 
 #include <optional>
 
-#include "../../include/admmq_adapt.h"
+#include "../../include/admmq_cache.h"
 
 namespace {
 
@@ -304,6 +304,100 @@ PyObject* qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The cache and the plan of a call, if their tensors are where they were: a[1] cache, a[2] plan, a[3..4] codes and scale,
+// a[5..6] tables and held.
+struct CacheCall {
+  const admmq_cache* cache;
+  const admmq_cache_plan* plan;
+  int* status;
+  int index;
+  explicit CacheCall(PyObject* const* a) {
+    status = pointer<int>(a[0]);
+    cache = pointer<const admmq_cache>(a[1]);
+    plan = pointer<const admmq_cache_plan>(a[2]);
+    const Tensor &codes = tensor(a[3]), &tables = tensor(a[5]);
+    need(codes.const_data_ptr() == cache->d_codes && tensor(a[4]).const_data_ptr() == cache->d_scale);
+    need(tables.const_data_ptr() == plan->d_tables && tensor(a[6]).const_data_ptr() == plan->d_held);
+    index = static_cast<int>(codes.get_device());
+    need(tables.is_cuda() && tables.get_device() == index);
+  }
+};
+
+// cache_write(status, cache, plan, codes, scale, tables, held, k, v) -> None
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    need(n == 9);
+    const CacheCall c(a);
+    const Tensor &k = tensor(a[7]), &v = tensor(a[8]);
+    const at::ScalarType type = k.scalar_type();
+    need(type == at::kBFloat16 || type == at::kFloat);
+    need(!in_a_graph(k) && !in_a_graph(v));
+    long long kr, kh, vr, vh;
+    heads_of(k, c.plan->n_rows, c.cache->kv_heads, c.cache->head_dim, type, c.index, &kr, &kh);
+    heads_of(v, c.plan->n_rows, c.cache->kv_heads, c.cache->head_dim, type, c.index, &vr, &vh);
+    const Current on_device(c.index);
+    const int st = admmq_cache_write(c.cache, c.plan, type == at::kFloat ? ADMMQ_F32 : ADMMQ_BF16, k.const_data_ptr(), kr, kh,
+                                     v.const_data_ptr(), vr, vh, c.status, on_device.stream);
+    need(st == ADMMQ_OK, st);
+    Py_RETURN_NONE;
+  } catch (const Refused& r) {
+    return status_of(r);
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_read(status, cache, plan, codes, scale, tables, held, bf16) -> (k, v)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    need(n == 8);
+    const CacheCall c(a);
+    const bool bf16 = a[7] == Py_True;
+    const long long h = c.cache->kv_heads, d = c.cache->head_dim;
+    const Current on_device(c.index);
+    const Tensor k = make({c.plan->n_rows, h, d}, bf16 ? at::kBFloat16 : at::kFloat, c.index);
+    const Tensor v = make({c.plan->n_rows, h, d}, bf16 ? at::kBFloat16 : at::kFloat, c.index);
+    const int st = admmq_cache_read(c.cache, c.plan, bf16 ? ADMMQ_BF16 : ADMMQ_F32, k.mutable_data_ptr(), h * d, d,
+                                    v.mutable_data_ptr(), h * d, d, c.status, on_device.stream);
+    need(st == ADMMQ_OK, st);
+    return tuple_of({k, v});
+  } catch (const Refused& r) {
+    return status_of(r);
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_attend(status, cache, plan, codes, scale, tables, held, q, softmax scale, window) -> (out, lse)
+PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    need(n == 10);
+    const CacheCall c(a);
+    const Tensor& q = tensor(a[7]);
+    const double scale = PyFloat_AsDouble(a[8]);
+    need(scale != -1.0 || !PyErr_Occurred());
+    const long long window = integer(a[9]), rows = c.plan->n_rows, heads = (long long)c.cache->kv_heads * c.plan->group,
+                    d = c.cache->head_dim;
+    need(window >= 0 && window <= 0x7fffffff);
+    need(!in_a_graph(q));
+    long long qr, qh;
+    heads_of(q, rows, heads, d, at::kBFloat16, c.index, &qr, &qh);
+    const Current on_device(c.index);
+    const Tensor out = make({rows, heads, d}, at::kBFloat16, c.index), lse = make({rows, heads}, at::kFloat, c.index);
+    const size_t bytes = admmq_cache_attend_workspace(c.cache, c.plan);
+    const Tensor work = make({static_cast<long long>(bytes < 16 ? 16 : bytes)}, at::kByte, c.index);
+    const int st = admmq_cache_attend(c.cache, c.plan, scale, static_cast<int>(window), q.const_data_ptr(), qr, qh,
+                                      out.mutable_data_ptr(), heads * d, d, static_cast<float*>(lse.mutable_data_ptr()),
+                                      work.mutable_data_ptr(), bytes, c.status, on_device.stream);
+    need(st == ADMMQ_OK, st);
+    return tuple_of({out, lse});
+  } catch (const Refused& r) {
+    return status_of(r);
+  }
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear)), METH_FASTCALL, nullptr},
     {"adapter_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adapter_grad)), METH_FASTCALL, nullptr},
@@ -311,6 +405,9 @@ PyMethodDef methods[] = {
     {"checkpoint_restore", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(checkpoint_restore)), METH_FASTCALL,
      nullptr},
     {"qk", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(qk)), METH_FASTCALL, nullptr},
+    {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
+    {"cache_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attend)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_adapt", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

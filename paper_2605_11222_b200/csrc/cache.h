@@ -1,0 +1,89 @@
+// Shared declarations of the kernels that keep keys and values in 8 bits and attend over them (admmq_cache.h).
+#pragma once
+#include <cuda_fp16.h>
+
+#include "../../include/admmq_cache.h"
+#include "adapt.h"
+
+namespace admmq {
+
+// Layout.  A block is 16 tokens of one page and head.  With P = head_dim rounded up to 64 (values past head_dim are never
+// read), its 32 P bytes are the keys' codes, then the values', one byte code + 128 each:
+//   keys    [P / 64][token 16][64]: value 64 h + e of a token at h * 1024 + token * 64 + e
+//   values  [P / 32][g 8][t 4][i 4][4 tokens]: value 32 c + 4 g + i at c * 512 + g * 64 + t * 16 + i * 4 + {0, 1, 2, 3} for
+//           tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+// so that lane 4 g + t of a warp finds in consecutive 16 bytes, and the warp in 512, what it feeds to m16n8k16 products as
+// their second operand: of the keys 16 values of token g (or g + 8), of the values the four tokens of its rows of the
+// product for four columns.  Blocks: [page][head][block of the page]; scales likewise, (key scale, value scale) each.
+constexpr int CBLOCK = ADMMQ_CACHE_BLOCK;
+
+struct CacheView {
+  uint8_t* codes;
+  float2* scale;
+  int n_pages, heads, d, p;          // p = d rounded up to 64
+  int page_shift, bpp;               // log2(page_size), blocks of a page
+  int block_bytes;                   // 32 p
+};
+// The rows of a call, as the device sees them.
+struct PlanView {
+  const int* tables;
+  const int* held;
+  const int* row_start;              // [n + 1]
+  const int2* blocks;                // (request, i): the i-th block that its rows touch, if they touch so many
+  const int4* small;                 // tiles of packed rows: (request, first packed row, first row, rows of the request)
+  const int4* big;
+  int n, max_pages, group, n_blocks, n_small, n_big;
+  long long capacity;                // positions of a table
+};
+constexpr int FEW_ROWS = 16, MANY_ROWS = 256;   // packed rows (token, query head) of a tile
+
+// Position of a request's first row; -1 where it takes no part.
+__device__ __forceinline__ long long first_position(const PlanView& pl, int request, int rows, int* status) {
+  const int at = pl.held[request];
+  if (at < 0) return -1;
+  if ((long long)at + rows > pl.capacity) {
+    raise_status(status, ADMMQ_ERR_SHAPE);
+    return -1;
+  }
+  return at;
+}
+// Index of block `b` (16 b = its first position) of a request and head 0; -1 for a page that does not exist.
+__device__ __forceinline__ long long block_index(const CacheView& c, const PlanView& pl, int request, int b, int* status) {
+  const int page = pl.tables[(long long)request * pl.max_pages + b / c.bpp];
+  if ((unsigned)page >= (unsigned)c.n_pages) {
+    raise_status(status, ADMMQ_ERR_SHAPE);
+    return -1;
+  }
+  return (long long)page * c.heads * c.bpp + b % c.bpp;
+}
+
+struct StoreArgs {
+  CacheView c;
+  PlanView pl;
+  const void *k, *v;                 // write: rows;  read: outputs
+  long long k_row, k_head, v_row, v_head;
+  int* status;
+};
+cudaError_t launch_cache_write(const StoreArgs& a, bool is_bf16, cudaStream_t stream);
+cudaError_t launch_cache_read(const StoreArgs& a, bool is_bf16, cudaStream_t stream);
+
+struct AttendArgs {
+  CacheView c;
+  PlanView pl;
+  const bf16* q;
+  bf16* out;
+  float* lse;
+  long long q_row, q_head, out_row, out_head;
+  float scale_log2;                  // scale * log2(e)
+  int window;
+  int* status;
+  // workspace of one kind of tiles: for every CTA two partial results, and what is to be joined
+  float* part;                       // [ctas][2][rows][p]
+  float2* part_ml;                   // [ctas][2][rows]: maximum (base 2) and sum
+  int4* joins;                       // [ctas]: (tile, head, last CTA, -), tile -1: nothing
+};
+constexpr int FEW_CTAS = 2;          // of an SM
+cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream);
+size_t attend_few_workspace(int p, int sms);
+
+}  // namespace admmq

@@ -1,0 +1,433 @@
+// Attention of a few rows over the 8-bit cache: one new token of a request, or a few drafted ones.
+//   z_j = scale q . k_j,  out = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m)
+//
+// Bound: reading the cache, once.  A warp takes 32 positions (two blocks) at a time: their codes come straight from memory
+// into registers, in the order of the second operand of m16n8k16 products (16 bytes a lane, 512 a warp and load), and the
+// next 32 positions' are under way while these are worked on.  The 16 rows of the product are the query heads of one key
+// head, of one token or of several; where fewer are in use the product's other rows cost nothing that the memory would not.
+// Codes become fp16 by placing them in the mantissa of 1024 + (code + 128) and subtracting 1152: exact, two instructions
+// for two.  Scales stay out of the products: the key scale multiplies the finished score, and the value scale s_b of a block
+// enters the exponent, w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m'), with m' the running maximum of that
+// exponent: w_j <= 1 whatever the scales are, so that fp16 holds it with 11 bits, and the sum of weights takes w_j / s_b.
+//
+// Work is shared out in equal parts (cache_schedule.cuh); four warps of a CTA take turns through its units, each with a
+// maximum, a sum and an accumulator of its own, joined in shared memory at the end of a piece.
+#include "cache_schedule.cuh"
+
+namespace admmq {
+namespace {
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS;
+constexpr float LN2 = 0.693147180559945309f;
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+// Codes of bytes 0, 1 (HIGH: 2, 3) of a word as two fp16 numbers.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t two_codes(uint32_t w) {
+  const uint32_t x = __byte_perm(w, 0x64646464u, HIGH ? 0x4342 : 0x4140);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int P>
+struct FewShared {
+  Schedule<THREADS> schedule;
+  uint4 q[P / 16][32];                               // first operand: [64 h + 4 s .. of every 16][lane]
+  float row_scale[FEW_ROWS];
+  float m[WARPS][FEW_ROWS], l[WARPS][FEW_ROWS];
+  __align__(16) float o[WARPS][FEW_ROWS][P + 4];
+};
+
+// 32 positions from `first`: two blocks' codes, and their scales.
+template <int P>
+struct Fetched {
+  uint4 k[2][P / 32], v[2][P / 32];
+  float2 s[2];
+};
+
+template <int P>
+__global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_kernel(const __grid_constant__ AttendArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  FewShared<P>& sh = *reinterpret_cast<FewShared<P>*>(smem_raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int group = a.pl.group, heads = a.c.heads, d = a.c.d;
+  pdl_launch();
+  pdl_wait();
+
+  const long long units = make_schedule<THREADS, UNIT, FEW_ROWS>(a, a.pl.small, a.pl.n_small, sh.schedule);
+  const long long total = units * heads;
+  const int ctas = active_ctas(total, LEAST_UNITS), cta = blockIdx.x;
+  if (cta >= ctas) {
+    if (tid == 0) a.joins[cta] = make_int4(-1, 0, 0, 0);
+    return;
+  }
+  const long long line_end = line_at(total, cta + 1, ctas);
+  int4 join = make_int4(-1, 0, 0, 0);
+
+  for (long long u = line_at(total, cta, ctas); u < line_end;) {
+    const Piece pc = find_piece<THREADS, UNIT, FEW_ROWS>(a, a.pl.small, a.pl.n_small, sh.schedule, u);
+    const long long stop = min(line_end, pc.end);
+    const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
+    if (u == pc.begin && stop < pc.end) join = make_int4(pc.tile, pc.head, cta_of(pc.end - 1, total, ctas), 0);
+
+    // ---- queries: each row times a power of two that brings its largest value to [2^13, 2^14), as fp16
+    {
+      const int r = tid >> 3, sub = tid & 7, pr = row0 + r, token = pr / group, head = pc.head * group + pr % group;
+      const bf16* src = a.q + (long long)(pc.job.z + token) * a.q_row + head * a.q_head;
+      uint2 raw[P / 32];
+      float top = 0.0f;
+      bool finite = true;
+#pragma unroll
+      for (int j = 0; j < P / 32; ++j) {
+        const int at = 4 * (sub + 8 * j);
+        raw[j] = r < nr && at < d ? __ldg(reinterpret_cast<const uint2*>(src + at)) : make_uint2(0, 0);
+        const float2 x = bf16x2_to_float2(raw[j].x), y = bf16x2_to_float2(raw[j].y);
+        top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+        finite &= isfinite(x.x) && isfinite(x.y) && isfinite(y.x) && isfinite(y.y);
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        finite &= __shfl_xor_sync(0xffffffffu, (int)finite, o) != 0;
+      }
+      float inv;
+      const float up = pow2_scale_for(top, &inv);
+#pragma unroll
+      for (int j = 0; j < P / 32; ++j) {
+        const int at = 4 * (sub + 8 * j);                // value 64 h + 16 t' + 4 s of the row
+        const float2 x = bf16x2_to_float2(raw[j].x), y = bf16x2_to_float2(raw[j].y);
+        uint32_t* dst = reinterpret_cast<uint32_t*>(&sh.q[(at >> 6) * 4 + ((at >> 2) & 3)][(r & 7) * 4 + ((at >> 4) & 3)]) + (r >> 3);
+        dst[0] = pack_f16(x.x * up, x.y * up);
+        dst[2] = pack_f16(y.x * up, y.y * up);
+      }
+      if (sub == 0) sh.row_scale[r] = finite ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
+    }
+    __syncthreads();
+    const float f0 = sh.row_scale[g], f1 = sh.row_scale[g + 8];
+    // the last position that rows g and g + 8 see
+    const int here0 = pc.span.at + (row0 + g) / group, here1 = pc.span.at + (row0 + g + 8) / group;
+    const int first_here = pc.span.at + row0 / group, last_here = pc.span.hi - 1;
+
+    float o[P / 8][4];
+#pragma unroll
+    for (int i = 0; i < P / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+
+    const int unit0 = (int)(u - pc.begin) + pc.span.lo / UNIT, unit1 = (int)(stop - pc.begin) + pc.span.lo / UNIT;
+    const int n_blocks = (pc.span.hi + CBLOCK - 1) / CBLOCK;
+    // places of a unit's two blocks; -1: none there
+    auto places = [&](int unit, long long (&at)[2]) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int blk = 2 * unit + b;
+        at[b] = -1;
+        if (unit < unit1 && blk < n_blocks) {
+          const long long i = block_index(a.c, a.pl, pc.job.x, blk, a.status);
+          if (i >= 0) at[b] = i + (long long)pc.head * a.c.bpp;
+        }
+      }
+    };
+    auto fetch_k = [&](Fetched<P>& f, const long long (&at)[2]) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f.s[b] = at[b] >= 0 ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
+        const uint8_t* p = a.c.codes + at[b] * a.c.block_bytes + lane * 16;
+#pragma unroll
+        for (int i = 0; i < P / 32; ++i) f.k[b][i] = at[b] >= 0 ? ldg_stream(p + i * 512) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    auto fetch_v = [&](Fetched<P>& f, const long long (&at)[2]) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint8_t* p = a.c.codes + at[b] * a.c.block_bytes + 16 * P + lane * 16;
+#pragma unroll
+        for (int i = 0; i < P / 32; ++i) f.v[b][i] = at[b] >= 0 ? ldg_stream(p + i * 512) : make_uint4(0, 0, 0, 0);
+      }
+    };
+
+    Fetched<P> f;
+    long long at[2], next[2];
+    int unit = unit0 + warp;
+    places(unit, at);
+    fetch_k(f, at);
+    fetch_v(f, at);
+    places(unit + WARPS, next);
+    for (; unit < unit1; unit += WARPS) {
+      // ---- scores of the 32 positions
+      float z[2][2][4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) z[b][j][0] = z[b][j][1] = z[b][j][2] = z[b][j][3] = 0.0f;
+#pragma unroll
+      for (int h = 0; h < P / 64; ++h)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const uint4 q = sh.q[h * 4 + s][lane];
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint4& w = f.k[b][2 * h + j];
+              const uint32_t c = s == 0 ? w.x : s == 1 ? w.y : s == 2 ? w.z : w.w;
+              mma_f16(z[b][j], q, two_codes<false>(c), two_codes<true>(c));
+            }
+        }
+      const float2 sc[2] = {f.s[0], f.s[1]};
+      const bool exists[2] = {at[0] >= 0, at[1] >= 0};
+      at[0] = next[0];
+      at[1] = next[1];
+      fetch_k(f, at);
+      // ---- exponents, base 2
+      const int pos = unit * UNIT;
+      const bool whole = pos + UNIT - 1 <= first_here && (a.window <= 0 || pos > last_here - a.window) && exists[0] && exists[1];
+      float most0 = -INFINITY, most1 = -INFINITY, inv_s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float vs = sc[b].y == 0.0f ? 1.0f : sc[b].y, lv = __log2f(vs), k0 = f0 * sc[b].x, k1 = f1 * sc[b].x;
+        inv_s[b] = __fdividef(1.0f, vs);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            z[b][j][e] = fmaf(z[b][j][e], k0, lv);
+            z[b][j][2 + e] = fmaf(z[b][j][2 + e], k1, lv);
+            if (!whole) {
+              const int p = pos + 16 * b + 8 * j + 2 * t + e;
+              if (!exists[b] || p > here0 || (a.window > 0 && p <= here0 - a.window)) z[b][j][e] = -INFINITY;
+              if (!exists[b] || p > here1 || (a.window > 0 && p <= here1 - a.window)) z[b][j][2 + e] = -INFINITY;
+            }
+            most0 = fmaxf(most0, z[b][j][e]);
+            most1 = fmaxf(most1, z[b][j][2 + e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int x = 1; x < 4; x <<= 1) {
+        most0 = fmaxf(most0, __shfl_xor_sync(0xffffffffu, most0, x));
+        most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, x));
+      }
+      most0 = fmaxf(most0, m0);
+      most1 = fmaxf(most1, m1);
+      if (__any_sync(0xffffffffu, most0 > m0 || most1 > m1)) {
+        const float a0 = most0 > m0 ? exp2_fast(m0 - most0) : 1.0f, a1 = most1 > m1 ? exp2_fast(m1 - most1) : 1.0f;
+        l0 *= a0;
+        l1 *= a1;
+#pragma unroll
+        for (int i = 0; i < P / 8; ++i) {
+          o[i][0] *= a0;
+          o[i][1] *= a0;
+          o[i][2] *= a1;
+          o[i][3] *= a1;
+        }
+        m0 = most0;
+        m1 = most1;
+      }
+      const float r0 = m0 == -INFINITY ? 0.0f : m0, r1 = m1 == -INFINITY ? 0.0f : m1;
+      uint4 w[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            z[b][j][e] = exp2_fast(z[b][j][e] - r0);
+            z[b][j][2 + e] = exp2_fast(z[b][j][2 + e] - r1);
+            s0 += z[b][j][e];
+            s1 += z[b][j][2 + e];
+          }
+        }
+        // (a block that the row sees nothing of adds nothing, even with a scale of NaN)
+        l0 = s0 == 0.0f ? l0 : fmaf(s0, inv_s[b], l0);
+        l1 = s1 == 0.0f ? l1 : fmaf(s1, inv_s[b], l1);
+        w[b] = make_uint4(pack_f16(z[b][0][0], z[b][0][1]), pack_f16(z[b][0][2], z[b][0][3]), pack_f16(z[b][1][0], z[b][1][1]),
+                          pack_f16(z[b][1][2], z[b][1][3]));
+      }
+      // ---- values
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < P / 32; ++c) {
+          const uint4& x = f.v[b][c];
+          mma_f16(o[4 * c], w[b], two_codes<false>(x.x), two_codes<true>(x.x));
+          mma_f16(o[4 * c + 1], w[b], two_codes<false>(x.y), two_codes<true>(x.y));
+          mma_f16(o[4 * c + 2], w[b], two_codes<false>(x.z), two_codes<true>(x.z));
+          mma_f16(o[4 * c + 3], w[b], two_codes<false>(x.w), two_codes<true>(x.w));
+        }
+      fetch_v(f, at);
+      places(unit + 2 * WARPS, next);
+    }
+
+    // ---- the warps' sums into one
+#pragma unroll
+    for (int x = 1; x < 4; x <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, x);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+    }
+    if (t == 0) {
+      sh.m[warp][g] = m0;
+      sh.m[warp][g + 8] = m1;
+      sh.l[warp][g] = l0;
+      sh.l[warp][g + 8] = l1;
+    }
+#pragma unroll
+    for (int c = 0; c < P / 32; ++c)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)           // columns 32 c + 8 t + 4 half + i of rows g and g + 8
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          *reinterpret_cast<float4*>(&sh.o[warp][g + 8 * r][32 * c + 8 * t + 4 * half]) =
+              make_float4(o[4 * c][2 * r + half], o[4 * c + 1][2 * r + half], o[4 * c + 2][2 * r + half], o[4 * c + 3][2 * r + half]);
+    __syncthreads();
+    const bool complete = u == pc.begin && stop == pc.end;
+    const int slot = 2 * cta + (u == pc.begin ? 1 : 0);
+    for (int i = tid; i < FEW_ROWS * P / 4; i += THREADS) {
+      const int r = i / (P / 4), at4 = 4 * (i % (P / 4));
+      if (r >= nr || at4 >= d) continue;
+      float m = sh.m[0][r];
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, sh.m[w][r]);
+      const float ref = m == -INFINITY ? 0.0f : m;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float k = exp2_fast(sh.m[w][r] - ref);
+        const float4 x = *reinterpret_cast<const float4*>(&sh.o[w][r][at4]);
+        acc.x = fmaf(x.x, k, acc.x);
+        acc.y = fmaf(x.y, k, acc.y);
+        acc.z = fmaf(x.z, k, acc.z);
+        acc.w = fmaf(x.w, k, acc.w);
+        l = fmaf(sh.l[w][r], k, l);
+      }
+      if (complete) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int pr = row0 + r, head = pc.head * group + pr % group;
+        const long long row = pc.job.z + pr / group;
+        *reinterpret_cast<uint2*>(a.out + row * a.out_row + head * a.out_head + at4) =
+            make_uint2(float2_to_bf16x2(acc.x * inv, acc.y * inv), float2_to_bf16x2(acc.z * inv, acc.w * inv));
+        if (at4 == 0 && a.lse) a.lse[row * (heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
+      } else {
+        *reinterpret_cast<float4*>(a.part + ((long long)slot * FEW_ROWS + r) * P + at4) = acc;
+        if (at4 == 0) a.part_ml[slot * FEW_ROWS + r] = make_float2(m, l);
+      }
+    }
+    __syncthreads();
+    u = stop;
+  }
+  if (tid == 0) a.joins[cta] = join;
+}
+
+// Adds up the partial results of a (tile, head) in the order of their CTAs.  A warp a row.
+template <int ROWS>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttendArgs a, const int4* tiles) {
+  pdl_launch();
+  pdl_wait();
+  const int first = blockIdx.x, lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5), p = a.c.p;
+  const int4 join = a.joins[first];
+  if (join.x < 0) return;
+  const int4 job = __ldg(tiles + join.x);
+  const int group = a.pl.group, nr = min(ROWS, job.w * group - job.y);
+  if (r >= nr) return;
+  const int last = join.z;
+  // slot of CTA c: 1 where the (tile, head) begins, 0 after
+  float m = -INFINITY;
+  for (int c = first + lane; c <= last; c += 32) m = fmaxf(m, a.part_ml[(2 * c + (c == first)) * ROWS + r].x);
+  m = warp_max(m);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+  const int at = 4 * lane;
+#pragma unroll 4
+  for (int c = first; c <= last; ++c) {
+    const int row = (2 * c + (c == first)) * ROWS + r;
+    const float2 ml = a.part_ml[row];
+    const float k = exp2_fast(ml.x - ref);
+    l = fmaf(ml.y, k, l);
+    const float* src = a.part + (long long)row * p + at;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (at + 128 * i < a.c.d) {
+        const float4 x = *reinterpret_cast<const float4*>(src + 128 * i);
+        acc[i].x = fmaf(x.x, k, acc[i].x);
+        acc[i].y = fmaf(x.y, k, acc[i].y);
+        acc[i].z = fmaf(x.z, k, acc[i].z);
+        acc[i].w = fmaf(x.w, k, acc[i].w);
+      }
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int pr = job.y + r, head = join.y * group + pr % group;
+  const long long row = job.z + pr / group;
+  bf16* dst = a.out + row * a.out_row + head * a.out_head + at;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (at + 128 * i < a.c.d)
+      *reinterpret_cast<uint2*>(dst + 128 * i) =
+          make_uint2(float2_to_bf16x2(acc[i].x * inv, acc[i].y * inv), float2_to_bf16x2(acc[i].z * inv, acc[i].w * inv));
+  if (lane == 0 && a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
+}
+
+template <int P>
+cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
+  const cudaError_t e = ensure_dynamic_smem((const void*)attend_few_kernel<P>, (int)sizeof(FewShared<P>));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sms * FEW_CTAS);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = sizeof(FewShared<P>);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attend_few_kernel<P>, a);
+}
+
+}  // namespace
+
+size_t attend_few_workspace(int p, int sms) {
+  const size_t ctas = (size_t)sms * FEW_CTAS;
+  return ctas * (2 * FEW_ROWS * (p * sizeof(float) + sizeof(float2)) + sizeof(int4));
+}
+
+cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream) {
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  cudaError_t e;
+  switch (a.c.p / 64) {
+    case 1: e = launch<64>(a, sms, stream); break;
+    case 2: e = launch<128>(a, sms, stream); break;
+    case 3: e = launch<192>(a, sms, stream); break;
+    default: e = launch<256>(a, sms, stream); break;
+  }
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sms * FEW_CTAS - 1, FEW_ROWS / 4);
+  cfg.blockDim = dim3(128);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, join_kernel<FEW_ROWS>, a, a.pl.small);
+}
+
+}  // namespace admmq

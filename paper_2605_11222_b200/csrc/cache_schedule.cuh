@@ -1,0 +1,108 @@
+// How the kernels that attend over the cache share out their work, and how partial results are joined.
+//
+// Work is counted in units of a fixed number of positions.  A tile of packed rows of one request has, for every key head,
+// the units that its rows see; all of them, tile after tile and head after head, are one line of T units, of which CTA c of
+// G takes [c T / G, (c + 1) T / G): every CTA has the same to do, however long the requests are, and the device finds its
+// part from the lengths when it runs.  A piece is what a CTA has of one (tile, head).  Pieces that are whole write the
+// result; of others the CTA leaves the unnormalised sum, the maximum and the sum of weights (slot 1 where it begins the
+// (tile, head), slot 0 where it goes on with one), and the join kernel adds them up in the order of the CTAs.
+#pragma once
+#include "cache.h"
+
+namespace admmq {
+
+// Positions that the rows of a tile see: [lo, hi); hi = 0 where the request takes no part.
+struct Span {
+  int at;                              // position of the request's first row, -1: none
+  int lo, hi;
+};
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const int4& tile, int tile_rows) {
+  Span s = {-1, 0, 0};
+  const long long at = first_position(a.pl, tile.x, tile.w, a.status);
+  if (at < 0) return s;
+  const int first = tile.y / a.pl.group, last = (min(tile.y + tile_rows, tile.w * a.pl.group) - 1) / a.pl.group;
+  s.at = (int)at;
+  s.hi = s.at + last + 1;
+  s.lo = a.window > 0 ? max(0, s.at + first - a.window + 1) : 0;
+  return s;
+}
+template <int UNIT>
+__device__ __forceinline__ int units_of(const Span& s) {
+  return s.hi > 0 ? (s.hi + UNIT - 1) / UNIT - s.lo / UNIT : 1;     // (one without positions writes the empty rows)
+}
+
+// Prefix sums of the tiles' units by segments of tiles, one segment a thread.
+template <int THREADS>
+struct Schedule {
+  long long sums[THREADS + 1];
+  long long warp_sums[THREADS / 32];
+  int per;
+};
+// All threads; returns the number of units (of one head).
+template <int THREADS, int UNIT, int ROWS>
+__device__ __forceinline__ long long make_schedule(const AttendArgs& a, const int4* tiles, int n, Schedule<THREADS>& s) {
+  const int per = (n + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  long long mine = 0;
+  for (int t = tid * per; t < min(n, (tid + 1) * per); ++t) mine += units_of<UNIT>(span_of(a, __ldg(tiles + t), ROWS));
+  long long run = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += up;
+  }
+  if (lane == 31) s.warp_sums[warp] = run;
+  if (tid == 0) s.per = per;
+  __syncthreads();
+  long long base = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) base += w < warp ? s.warp_sums[w] : 0;
+  s.sums[tid] = base + run - mine;
+  if (tid == THREADS - 1) s.sums[THREADS] = base + run;
+  __syncthreads();
+  return s.sums[THREADS];
+}
+// The piece that holds unit u of the line.
+struct Piece {
+  int tile, head;
+  int4 job;
+  Span span;
+  long long begin, end;                // the (tile, head)'s part of the line
+};
+template <int THREADS, int UNIT, int ROWS>
+__device__ __forceinline__ Piece find_piece(const AttendArgs& a, const int4* tiles, int n, const Schedule<THREADS>& s, long long u) {
+  const int heads = a.c.heads;
+  int lo = 0, hi = THREADS;            // segment: the last one with sums * heads <= u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (s.sums[mid] * heads <= u) lo = mid;
+    else hi = mid;
+  }
+  long long at = s.sums[lo] * heads;
+  Piece p;
+  int t = lo * s.per;
+  for (;; ++t) {                       // (ends within the segment: u is below the line's end)
+    p.job = __ldg(tiles + t);
+    p.span = span_of(a, p.job, ROWS);
+    const long long units = units_of<UNIT>(p.span);
+    if (u < at + units * heads || t + 1 >= n) {
+      p.head = (int)((u - at) / units);
+      p.begin = at + p.head * units;
+      p.end = p.begin + units;
+      break;
+    }
+    at += units * heads;
+  }
+  p.tile = t;
+  return p;
+}
+// CTAs that get work: at least `least` units each.
+__device__ __forceinline__ int active_ctas(long long total, int least) {
+  const long long most = (total + least - 1) / least;
+  return (int)(most < (long long)gridDim.x ? most : (long long)gridDim.x);
+}
+__device__ __forceinline__ long long line_at(long long total, int c, int ctas) { return total * c / ctas; }
+__device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
+  return (int)(((u + 1) * ctas + total - 1) / total) - 1;
+}
+
+}  // namespace admmq

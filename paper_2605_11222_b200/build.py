@@ -15,7 +15,7 @@ BIND = os.path.join(HERE, "_adapt.so")
 BIND_FOR = os.path.join(OBJ, "_adapt.for")     # the Python and the torch that _adapt.so was built for
 SOURCES = ["api.cu", "elem.cu", "gemm_simt.cu", "gemm_tc.cu", "tridiag.cu", "tridiag_blocked.cu", "local_search.cu", "pair_swap.cu",
            "objective_static.cu", "adapt_api.cu", "linear_small.cu", "shrink_tc.cu", "linear_tc.cu", "linear_pair.cu", "adapter_grad.cu", "checkpoint8.cu",
-           "qk_rope.cu", "cache_api.cu", "cache_store.cu", "cache_attend.cu"]
+           "qk_rope.cu", "cache_api.cu", "cache_store.cu", "cache_attend.cu", "cache_attend_tc.cu", "cache_join.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

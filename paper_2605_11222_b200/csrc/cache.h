@@ -57,6 +57,23 @@ __device__ __forceinline__ long long block_index(const CacheView& c, const PlanV
   return (long long)page * c.heads * c.bpp + b % c.bpp;
 }
 
+// Codes of bytes 0, 1 (HIGH: 2, 3) of a word as two fp16 numbers.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t two_codes(uint32_t w) {
+  const uint32_t x = __byte_perm(w, 0x64646464u, HIGH ? 0x4342 : 0x4140);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 struct StoreArgs {
   CacheView c;
   PlanView pl;
@@ -83,7 +100,9 @@ struct AttendArgs {
   int4* joins;                       // [ctas]: (tile, head, last CTA, -), tile -1: nothing
 };
 constexpr int FEW_CTAS = 2;          // of an SM
+__host__ __device__ constexpr int many_rows(int p) { return p <= 128 ? MANY_ROWS : MANY_ROWS / 2; }
 cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream);
-size_t attend_few_workspace(int p, int sms);
+cudaError_t launch_cache_attend_many(const AttendArgs& a, cudaStream_t stream);
+cudaError_t launch_cache_join(const AttendArgs& a, bool many, int sms, cudaStream_t stream);
 
 }  // namespace admmq

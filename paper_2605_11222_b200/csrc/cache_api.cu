@@ -6,6 +6,7 @@ namespace {
 
 constexpr int MAX_HEADS = 4096;
 constexpr long long MAX_POSITIONS = 1LL << 30;
+constexpr int MOST_FEW = 48;           // packed rows of a request up to which they are a few
 
 bool aligned(const void* p, size_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 admmq_status from(cudaError_t e) { return e == cudaSuccess ? ADMMQ_OK : ADMMQ_ERR_CUDA; }
@@ -34,7 +35,7 @@ admmq_status view_cache(const admmq_cache* c, CacheView* v) {
 // Blocks that `rows` rows touch at most, tiles of packed rows.
 long long blocks_of(long long rows) { return rows > 0 ? (rows + 2 * CBLOCK - 2) / CBLOCK : 0; }
 long long tiles_of(long long packed, int rows) { return (packed + rows - 1) / rows; }
-bool is_few(long long) { return true; }
+bool is_few(long long packed) { return packed <= MOST_FEW; }
 long long round4(long long n) { return (n + 3) & ~3LL; }
 struct IndexSizes {
   long long rows, blocks, small, big;
@@ -91,7 +92,14 @@ admmq_status store(bool write, const admmq_cache* cache, const admmq_cache_plan*
   return from(write ? launch_cache_write(a, dtype == ADMMQ_BF16, stream) : launch_cache_read(a, dtype == ADMMQ_BF16, stream));
 }
 
-size_t workspace_of(const CacheView& c, const PlanView& p, int sms) { return p.n_small ? attend_few_workspace(c.p, sms) : 0; }
+// Workspace of one kind of tiles: for every CTA what is to be joined, and two partial results.
+size_t part_bytes(const CacheView& c, bool many, int sms) {
+  const size_t ctas = (size_t)sms * (many ? 1 : FEW_CTAS), rows = many ? many_rows(c.p) : FEW_ROWS;
+  return ctas * (sizeof(int4) + 2 * rows * (c.p * sizeof(float) + sizeof(float2)));
+}
+size_t workspace_of(const CacheView& c, const PlanView& p, int sms) {
+  return (p.n_small ? part_bytes(c, false, sms) : 0) + (p.n_big ? part_bytes(c, true, sms) : 0);
+}
 
 }  // namespace
 }  // namespace admmq
@@ -196,12 +204,15 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
   a.window = window;
   a.status = d_status;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (a.pl.n_small) {
-    const size_t ctas = (size_t)sms * FEW_CTAS;
-    a.joins = (int4*)d_workspace;
+  char* at = (char*)d_workspace;
+  for (int many = 0; many < 2; ++many) {
+    if (!(many ? a.pl.n_big : a.pl.n_small)) continue;
+    const size_t ctas = (size_t)sms * (many ? 1 : FEW_CTAS), rows = many ? many_rows(a.c.p) : FEW_ROWS;
+    a.joins = (int4*)at;
     a.part = (float*)(a.joins + ctas);
-    a.part_ml = (float2*)(a.part + ctas * 2 * FEW_ROWS * a.c.p);
-    const cudaError_t e = launch_cache_attend_few(a, stream);
+    a.part_ml = (float2*)(a.part + ctas * 2 * rows * a.c.p);
+    at += part_bytes(a.c, many, sms);
+    const cudaError_t e = many ? launch_cache_attend_many(a, stream) : launch_cache_attend_few(a, stream);
     if (e != cudaSuccess) return ADMMQ_ERR_CUDA;
   }
   return ADMMQ_OK;

@@ -17,7 +17,7 @@
 namespace admmq {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS;
+constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 4;
 constexpr float LN2 = 0.693147180559945309f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
@@ -26,23 +26,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
-// Codes of bytes 0, 1 (HIGH: 2, 3) of a word as two fp16 numbers.
-template <bool HIGH>
-__device__ __forceinline__ uint32_t two_codes(uint32_t w) {
-  const uint32_t x = __byte_perm(w, 0x64646464u, HIGH ? 0x4342 : 0x4140);
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&x), __half2half2(__ushort_as_half(0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 template <int P>
 struct FewShared {
   Schedule<THREADS> schedule;
@@ -68,7 +51,8 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
   pdl_launch();
   pdl_wait();
 
-  const long long units = make_schedule<THREADS, UNIT, FEW_ROWS>(a, a.pl.small, a.pl.n_small, sh.schedule);
+  const auto job = [&](int tile) { return __ldg(a.pl.small + tile); };
+  const long long units = make_schedule<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule);
   const long long total = units * heads;
   const int ctas = active_ctas(total, LEAST_UNITS), cta = blockIdx.x;
   if (cta >= ctas) {
@@ -79,8 +63,10 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
   int4 join = make_int4(-1, 0, 0, 0);
 
   for (long long u = line_at(total, cta, ctas); u < line_end;) {
-    const Piece pc = find_piece<THREADS, UNIT, FEW_ROWS>(a, a.pl.small, a.pl.n_small, sh.schedule, u);
+    const Piece pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
     const long long stop = min(line_end, pc.end);
+    u = max(u, pc.begin);
+    if (u >= stop) break;
     const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
     if (u == pc.begin && stop < pc.end) join = make_int4(pc.tile, pc.head, cta_of(pc.end - 1, total, ctas), 0);
 
@@ -333,56 +319,6 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
   if (tid == 0) a.joins[cta] = join;
 }
 
-// Adds up the partial results of a (tile, head) in the order of their CTAs.  A warp a row.
-template <int ROWS>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttendArgs a, const int4* tiles) {
-  pdl_launch();
-  pdl_wait();
-  const int first = blockIdx.x, lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5), p = a.c.p;
-  const int4 join = a.joins[first];
-  if (join.x < 0) return;
-  const int4 job = __ldg(tiles + join.x);
-  const int group = a.pl.group, nr = min(ROWS, job.w * group - job.y);
-  if (r >= nr) return;
-  const int last = join.z;
-  // slot of CTA c: 1 where the (tile, head) begins, 0 after
-  float m = -INFINITY;
-  for (int c = first + lane; c <= last; c += 32) m = fmaxf(m, a.part_ml[(2 * c + (c == first)) * ROWS + r].x);
-  m = warp_max(m);
-  const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
-  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-  const int at = 4 * lane;
-#pragma unroll 4
-  for (int c = first; c <= last; ++c) {
-    const int row = (2 * c + (c == first)) * ROWS + r;
-    const float2 ml = a.part_ml[row];
-    const float k = exp2_fast(ml.x - ref);
-    l = fmaf(ml.y, k, l);
-    const float* src = a.part + (long long)row * p + at;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (at + 128 * i < a.c.d) {
-        const float4 x = *reinterpret_cast<const float4*>(src + 128 * i);
-        acc[i].x = fmaf(x.x, k, acc[i].x);
-        acc[i].y = fmaf(x.y, k, acc[i].y);
-        acc[i].z = fmaf(x.z, k, acc[i].z);
-        acc[i].w = fmaf(x.w, k, acc[i].w);
-      }
-    }
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int pr = job.y + r, head = join.y * group + pr % group;
-  const long long row = job.z + pr / group;
-  bf16* dst = a.out + row * a.out_row + head * a.out_head + at;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (at + 128 * i < a.c.d)
-      *reinterpret_cast<uint2*>(dst + 128 * i) =
-          make_uint2(float2_to_bf16x2(acc[i].x * inv, acc[i].y * inv), float2_to_bf16x2(acc[i].z * inv, acc[i].w * inv));
-  if (lane == 0 && a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
-}
-
 template <int P>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
   const cudaError_t e = ensure_dynamic_smem((const void*)attend_few_kernel<P>, (int)sizeof(FewShared<P>));
@@ -402,11 +338,6 @@ cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
 
 }  // namespace
 
-size_t attend_few_workspace(int p, int sms) {
-  const size_t ctas = (size_t)sms * FEW_CTAS;
-  return ctas * (2 * FEW_ROWS * (p * sizeof(float) + sizeof(float2)) + sizeof(int4));
-}
-
 cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream) {
   const int sms = device_sms();
   if (sms <= 0) return cudaErrorInvalidDevice;
@@ -417,17 +348,7 @@ cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream) {
     case 3: e = launch<192>(a, sms, stream); break;
     default: e = launch<256>(a, sms, stream); break;
   }
-  if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms * FEW_CTAS - 1, FEW_ROWS / 4);
-  cfg.blockDim = dim3(128);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join_kernel<FEW_ROWS>, a, a.pl.small);
+  return e == cudaSuccess ? launch_cache_join(a, false, sms, stream) : e;
 }
 
 }  // namespace admmq

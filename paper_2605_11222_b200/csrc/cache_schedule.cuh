@@ -3,7 +3,8 @@
 // Work is counted in units of a fixed number of positions.  A tile of packed rows of one request has, for every key head,
 // the units that its rows see; all of them, tile after tile and head after head, are one line of T units, of which CTA c of
 // G takes [c T / G, (c + 1) T / G): every CTA has the same to do, however long the requests are, and the device finds its
-// part from the lengths when it runs.  A piece is what a CTA has of one (tile, head).  Pieces that are whole write the
+// part from the lengths when it runs.  A (tile, head) counts `EXTRA` units more than it has, ahead of them, for what a piece
+// costs whatever its length.  A piece is what a CTA has of one (tile, head).  Pieces that are whole write the
 // result; of others the CTA leaves the unnormalised sum, the maximum and the sum of weights (slot 1 where it begins the
 // (tile, head), slot 0 where it goes on with one), and the join kernel adds them up in the order of the CTAs.
 #pragma once
@@ -26,24 +27,35 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const int4& tile, i
   s.lo = a.window > 0 ? max(0, s.at + first - a.window + 1) : 0;
   return s;
 }
+// Its units: one where the request takes no part (the rows are written all the same), none for a tile without rows (a half
+// of one that the request does not fill).
 template <int UNIT>
-__device__ __forceinline__ int units_of(const Span& s) {
-  return s.hi > 0 ? (s.hi + UNIT - 1) / UNIT - s.lo / UNIT : 1;     // (one without positions writes the empty rows)
+__device__ __forceinline__ int units_of(const Span& s, const int4& tile, int group) {
+  if (tile.y >= tile.w * group) return 0;
+  return s.hi > 0 ? (s.hi + UNIT - 1) / UNIT - s.lo / UNIT : 1;
+}
+template <int UNIT>
+__device__ __forceinline__ int units_of(const AttendArgs& a, const int4& tile, int tile_rows) {
+  return units_of<UNIT>(span_of(a, tile, tile_rows), tile, a.pl.group);
 }
 
-// Prefix sums of the tiles' units by segments of tiles, one segment a thread.
+// job(t): tile t, as the plan's tiles.  Prefix sums of the tiles' units by segments of tiles, one segment a thread.
 template <int THREADS>
 struct Schedule {
   long long sums[THREADS + 1];
   long long warp_sums[THREADS / 32];
   int per;
 };
-// All threads; returns the number of units (of one head).
-template <int THREADS, int UNIT, int ROWS>
-__device__ __forceinline__ long long make_schedule(const AttendArgs& a, const int4* tiles, int n, Schedule<THREADS>& s) {
+// All threads; returns the length of the line (of one head).
+template <int UNIT, int EXTRA>
+__device__ __forceinline__ int cost_of(int units) {
+  return units > 0 ? units + EXTRA : 0;
+}
+template <int THREADS, int UNIT, int ROWS, int EXTRA, class Job>
+__device__ __forceinline__ long long make_schedule(const AttendArgs& a, const Job& job, int n, Schedule<THREADS>& s) {
   const int per = (n + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   long long mine = 0;
-  for (int t = tid * per; t < min(n, (tid + 1) * per); ++t) mine += units_of<UNIT>(span_of(a, __ldg(tiles + t), ROWS));
+  for (int t = tid * per; t < min(n, (tid + 1) * per); ++t) mine += cost_of<UNIT, EXTRA>(units_of<UNIT>(a, job(t), ROWS));
   long long run = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -66,10 +78,10 @@ struct Piece {
   int tile, head;
   int4 job;
   Span span;
-  long long begin, end;                // the (tile, head)'s part of the line
+  long long begin, end;                // the (tile, head)'s units in the line (u may be before: of the extra ones)
 };
-template <int THREADS, int UNIT, int ROWS>
-__device__ __forceinline__ Piece find_piece(const AttendArgs& a, const int4* tiles, int n, const Schedule<THREADS>& s, long long u) {
+template <int THREADS, int UNIT, int ROWS, int EXTRA, class Job>
+__device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job, int n, const Schedule<THREADS>& s, long long u) {
   const int heads = a.c.heads;
   int lo = 0, hi = THREADS;            // segment: the last one with sums * heads <= u
   while (hi - lo > 1) {
@@ -81,16 +93,16 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, const int4* til
   Piece p;
   int t = lo * s.per;
   for (;; ++t) {                       // (ends within the segment: u is below the line's end)
-    p.job = __ldg(tiles + t);
+    p.job = job(t);
     p.span = span_of(a, p.job, ROWS);
-    const long long units = units_of<UNIT>(p.span);
-    if (u < at + units * heads || t + 1 >= n) {
-      p.head = (int)((u - at) / units);
-      p.begin = at + p.head * units;
-      p.end = p.begin + units;
+    const long long cost = cost_of<UNIT, EXTRA>(units_of<UNIT>(p.span, p.job, a.pl.group));
+    if (u < at + cost * heads) {
+      p.head = (int)((u - at) / cost);
+      p.begin = at + p.head * cost + EXTRA;
+      p.end = at + (p.head + 1) * cost;
       break;
     }
-    at += units * heads;
+    at += cost * heads;
   }
   p.tile = t;
   return p;

@@ -19,7 +19,8 @@ admmq_status check_sizes(int n_pages, int kv_heads, int head_dim, int page_size)
   if (n_pages < 1 || kv_heads < 1 || kv_heads > MAX_HEADS) return ADMMQ_ERR_SHAPE;
   if (head_dim < 16 || head_dim > ADMMQ_CACHE_MAX_HEAD || head_dim % 16) return ADMMQ_ERR_SHAPE;
   if (page_size < CBLOCK || page_size > ADMMQ_CACHE_MAX_PAGE || page_size & (page_size - 1)) return ADMMQ_ERR_SHAPE;
-  return ADMMQ_OK;
+  // (blocks are counted in 32 bits; so many do not fit a device)
+  return (long long)n_pages * kv_heads * (page_size / CBLOCK) > 0x7fffffffLL ? ADMMQ_ERR_SHAPE : ADMMQ_OK;
 }
 admmq_status view_cache(const admmq_cache* c, CacheView* v) {
   if (!c || c->struct_size != sizeof(admmq_cache)) return ADMMQ_ERR_INVALID_ARG;

@@ -5,15 +5,17 @@
 // cores while the other's softmax runs (heads wider than 128: one track of 128 rows).  Positions come 128 (64) at a time.
 // Both products take fp16 operands: queries times a power of two of their row, codes as they are, and weights
 //   w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m')
-// with the value scale s_b of the block in the exponent, so that they stay below 2^8 whatever the scales are; the key scale
-// multiplies the finished score.  The sum of weights takes w_j / s_b.  The accumulators' reference m' is raised only when a
-// weight would pass 2^8, which is rare, so that the accumulator is hardly ever touched between its products.
+// with the value scale s_b of the block in the exponent, so that they fit fp16 whatever the scales are; the key scale
+// multiplies the finished score.  The sum of weights takes w_j / s_b.  The reference m' is a row's maximum over the first
+// step; it is raised only after a weight has passed 2^8, which is rare, so that the accumulator is hardly ever touched
+// between its products, and a row's weights need not wait for its maximum.
 //   warps 0-7    softmax, a row a thread: scores from tensor memory into registers, weights back over them (the first
 //                operand of the second product), the accumulator's occasional scaling, queries in and results out
 //   warps 8-11   codes: from memory into registers a tile ahead, expanded into the swizzled operand tiles.  The order of
 //                positions inside a product is free, so that values, which the cache keeps as words of four tokens, need no
 //                transposition: position 16 b + k of the operand is token (0 1 8 9 2 3 10 11 4 5 12 13 6 7 14 15)[k] of block b
 //   warp 12      issues the products; tensor memory
+//   warp 13      finds the CTA's pieces of the work, ahead of the others
 // Work is shared out in equal parts (cache_schedule.cuh), a CTA an SM.
 // Bound: exponentials (16 a cycle and SM: 2048 cycles for 256 x 128) and the tensor cores (2048 as well), overlapped.
 // Waits are bounded as in the other tensor-core kernels.  Products of a CTA run in the order of their issue; scores of the
@@ -25,12 +27,13 @@
 namespace admmq {
 namespace {
 
-constexpr int ROWS = 128, SOFT_WARPS = 8, CODE_WARPS = 4, WARPS = 16, THREADS = 32 * WARPS, MMA_WARP = SOFT_WARPS + CODE_WARPS;
-constexpr int SOFT_REGS = 184, CODE_REGS = 104, MMA_REGS = 40;     // of 128 each at launch
+constexpr int ROWS = 128, SOFT_WARPS = 8, CODE_WARPS = 4, WARPS = 16, THREADS = 32 * WARPS, MMA_WARP = SOFT_WARPS + CODE_WARPS, PLAN_WARP = MMA_WARP + 1;
+constexpr int SOFT_REGS = 152, CODE_REGS = 112, MMA_REGS = 96;     // of 128 each at launch
 static_assert(2 * SOFT_REGS + CODE_REGS + MMA_REGS <= 4 * 128, "registers");
-constexpr int STAGES = 2, SCALE_SLOTS = 4;
+constexpr int STAGES = 2, SCALE_SLOTS = 4, PIECE_SLOTS = 4;
 constexpr int EXTRA = 3;                             // a piece's start and end, in steps
-constexpr float LIMIT = 8.0f;                        // weights stay below 2^LIMIT
+// Weights above 2^LIMIT raise the reference for the steps that follow; fp16 holds them up to 2^HARD_LIMIT.
+constexpr float LIMIT = 8.0f, HARD_LIMIT = 15.0f;
 constexpr float LN2 = 0.693147180559945309f;
 
 template <int P>
@@ -59,17 +62,12 @@ __device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, 
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
-  uint32_t* u = reinterpret_cast<uint32_t*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
-        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
-        "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
-        "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
-      : "r"(taddr)
-      : "memory");
+// Values of a load are there after the wait: named in it, so that no use of them moves ahead.
+__device__ __forceinline__ void tc_ld16_wait(uint32_t (&u)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
+                 "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
+               :: "memory");
 }
 __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* u) {
   asm volatile(
@@ -79,6 +77,13 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* u) {
       "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]),
       "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]),
       "r"(u[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&u)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+      ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
+      "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -92,13 +97,38 @@ __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// Bounded wait of a whole warp with one answer for all its lanes.  (Inlined: setmaxnreg asks for a kernel without calls.)
+// Bounded wait of a whole warp with one answer for all its lanes.  A try sleeps for up to `NAP` ns: polled, the barriers took
+// a third of the issue slots.  (Inlined: setmaxnreg asks for a kernel without calls.)
 struct WarpWait {
   volatile int* abort_flag;
   int* status;
   long long limit;
+  static constexpr uint32_t NAP = 4000;
+  __device__ __forceinline__ static bool nap(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        "selp.b32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(NAP)
+        : "memory");
+    return done != 0;
+  }
   __device__ __forceinline__ bool all(uint32_t bar, uint32_t parity) const {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, limit)) != 0;
+    bool ok = nap(bar, parity);
+    if (!ok) {
+      const long long t0 = clock64();
+      do {
+        ok = nap(bar, parity);
+        if (!ok && (*abort_flag || clock64() - t0 > limit)) {
+          *abort_flag = 1;
+          raise_status(status, ST_TIMEOUT);
+          break;
+        }
+      } while (!ok);
+    }
+    return __all_sync(0xffffffffu, ok) != 0;
   }
 };
 
@@ -116,6 +146,14 @@ __device__ __forceinline__ int4 job_of(const AttendArgs& a, int tile) {
   job.y += tile % PER * ROWS;
   return job;
 }
+// A piece as the roles take it from shared memory.
+struct PieceJob {
+  int steps;                                         // 0: there are no more
+  int pos;                                           // position of its first step
+  int head, request, row0, first_row, packed;        // row0: packed row of the tile's first; packed: of the request in all
+  int at, hi;                                        // position of the request's first row; end of what the tile sees
+  int part;                                          // where its partial result goes; -1: it is whole
+};
 
 template <int P>
 __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ ManyArgs A) {
@@ -125,11 +163,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   extern __shared__ uint8_t smem_raw[];
   __shared__ Schedule<THREADS> schedule;
   // full: a step's codes are expanded; empty: its products have read them; scores complete; weights in place (and the
-  // scores' buffer read); accumulator complete; queries in place; scales in place.  Waits go by parity, so a waiter has to
-  // know that the phase before is over and that the one after cannot be: the scales have a barrier a slot because the keys'
-  // may be a phase on before a slow warp of the softmax has looked.
-  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 + 2 + 2 + 2 + 1];
+  // scores' buffer read); accumulator complete; queries in place; scales in place; pieces.  Waits go by parity, so a waiter
+  // has to know that the phase before is over and that the one after cannot be: the scales have a barrier a slot because the
+  // keys' may be a phase on before a slow warp of the softmax has looked.
+  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 * PIECE_SLOTS + 2 + 2 + 2 + 2 + 1];
   __shared__ float4 scales[SCALE_SLOTS][BLOCKS];     // key scale, log2 of the value scale, its reciprocal
+  __shared__ PieceJob pieces[PIECE_SLOTS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
 
@@ -140,7 +179,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   const WarpWait wait = {&abort_s, a.status, A.wait_limit};
   const uint32_t k_full = smem_u32(&bars[0]), k_empty = k_full + 8 * STAGES, v_full = k_empty + 8 * STAGES, v_empty = v_full + 8 * STAGES;
   const uint32_t s_full = v_empty + 8 * STAGES, w_full = s_full + 16, o_full = w_full + 16, q_full = o_full + 16, drain_bar = q_full + 16,
-                 sc_full = drain_bar + 8;
+                 sc_full = drain_bar + 8, p_full = sc_full + 8 * SCALE_SLOTS, p_empty = p_full + 8 * PIECE_SLOTS;
 
   if (threadIdx.x == 0) {
     abort_s = 0;
@@ -158,6 +197,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     }
     mbar_init(drain_bar, 1);
     for (int s = 0; s < SCALE_SLOTS; ++s) mbar_init(sc_full + 8 * s, 1);
+    for (int s = 0; s < PIECE_SLOTS; ++s) {
+      mbar_init(p_full + 8 * s, 1);
+      mbar_init(p_empty + 8 * s, TRACKS * ROWS / 32 + CODE_WARPS + 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) {
@@ -173,9 +216,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int ctas = active_ctas(total, 1), cta = blockIdx.x;
-  const long long line_begin = cta < ctas ? line_at(total, cta, ctas) : 0, line_end = cta < ctas ? line_at(total, cta + 1, ctas) : 0;
-  const auto piece = [&](long long u) { return find_piece<THREADS, TN, TILE, EXTRA>(a, job, n_tiles, schedule, u); };
+  // piece n of the CTA, by all lanes of a warp; false: a wait ran out
+  const auto take = [&](uint32_t n, PieceJob& p) {
+    if (!wait.all(p_full + 8 * (n % PIECE_SLOTS), n / PIECE_SLOTS & 1u)) return false;
+    p = pieces[n % PIECE_SLOTS];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(p_empty + 8 * (n % PIECE_SLOTS));
+    return true;
+  };
 
   if (warp < SOFT_WARPS) {
     more_registers<SOFT_REGS>();
@@ -184,147 +232,220 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
       const uint32_t o_col = lanes + C::O_COL + x * P;
       const int group = a.pl.group, d = a.c.d;
-      int4 join = make_int4(-1, 0, 0, 0);
-      uint32_t it = 0, n_piece = 0;                  // steps and pieces so far
-      bool ok = true;
-      for (long long u = line_begin; ok && u < line_end; ++n_piece) {
-        const Piece pc = piece(u);
-        const long long stop = min(line_end, pc.end);
-        u = max(u, pc.begin);
-        if (u >= stop) break;
-        const int steps = (int)(stop - u), pr = pc.job.y + x * ROWS + r, packed = pc.job.w * group;
-        if (u == pc.begin && stop < pc.end) join = make_int4(pc.tile, pc.head, cta_of(pc.end - 1, total, ctas), 0);
-        const int token = pr / group, head = pc.head * group + pr % group;
-        const bool mine = pr < packed;
-
-        // ---- the row's query: times a power of two, as fp16
-        float row_scale;
-        {
-          const bf16* src = a.q + (long long)(pc.job.z + token) * a.q_row + head * a.q_head;
-          float top = 0.0f;
-          bool finite = true;
-          auto chunk = [&](int c) { return mine && 8 * c < d ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0); };
-#pragma unroll 8
-          for (int c = 0; c < P / 8; ++c) {
-            const uint4 q = chunk(c);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+      constexpr bool AHEAD = P <= 128;               // a query is fetched ahead (64 registers) while a result leaves
+      uint4 raw[AHEAD ? P / 8 : 1];
+      auto query_at = [&](const PieceJob& p) {
+        const int pr = p.row0 + x * ROWS + r;
+        return a.q + (long long)(p.first_row + pr / group) * a.q_row + (p.head * group + pr % group) * a.q_head;
+      };
+      auto chunk = [&](const PieceJob& p, const bf16* src, int c) {
+        return p.row0 + x * ROWS + r < p.packed && 8 * c < d ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
+      };
+      auto fetch_query = [&](const PieceJob& p) {
+        if (AHEAD) {
+          const bf16* src = query_at(p);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = bf16x2_to_float2(w[e]);
-              top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-              finite &= isfinite(f.x) && isfinite(f.y);
-            }
-          }
-          float inv;
-          const float up = pow2_scale_for(top, &inv);
-          row_scale = finite ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
-          uint8_t* dst = tiles_at + x * C::Q_BYTES + r * 128;
-#pragma unroll 8
-          for (int c = 0; c < P / 8; ++c) {
-            const uint4 q = chunk(c);                // (from the L1 cache)
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = bf16x2_to_float2(w[e]);
-              h[e] = pack_f16(f.x * up, f.y * up);
-            }
-            *reinterpret_cast<uint4*>(dst + c / 8 * (ROWS * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-          }
-          fence_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(q_full + 8 * x);
+          for (int c = 0; c < P / 8; ++c) raw[AHEAD ? c : 0] = chunk(p, src, c);
         }
+      };
+      // The row's query: times a power of two, as fp16, into its operand tile.  Returns the factor that takes it to base-2
+      // exponents.
+      auto place_query = [&](const PieceJob& p) {
+        const bf16* src = query_at(p);
+        float top = 0.0f;
+        bool finite = true;
+#pragma unroll (AHEAD ? 16 : 8)
+        for (int c = 0; c < P / 8; ++c) {
+          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, src, c);
+          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = bf16x2_to_float2(w[e]);
+            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+            finite &= isfinite(f.x) && isfinite(f.y);
+          }
+        }
+        float inv;
+        const float up = pow2_scale_for(top, &inv);
+        uint8_t* dst = tiles_at + x * C::Q_BYTES + r * 128;
+#pragma unroll (AHEAD ? 16 : 8)
+        for (int c = 0; c < P / 8; ++c) {
+          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, src, c);
+          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = bf16x2_to_float2(w[e]);
+            h[e] = pack_f16(f.x * up, f.y * up);
+          }
+          *reinterpret_cast<uint4*>(dst + c / 8 * (ROWS * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full + 8 * x);
+        return finite ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
+      };
 
-        const int here = pc.span.at + token;
+      PieceJob pc;
+      bool ok = take(0, pc);
+      uint32_t it = 0;                               // steps so far
+      float row_scale = 0.0f;
+      if (ok && pc.steps > 0) {
+        fetch_query(pc);
+        row_scale = place_query(pc);
+      }
+      for (uint32_t n = 1; ok && pc.steps > 0; ++n) {
+        const int here = pc.at + (pc.row0 + x * ROWS + r) / group;
         // positions that every row of the track sees: up to its first row's own, from its last row's window on
-        const int track_first = pc.job.y + x * ROWS;
-        const int all_to = pc.span.at + track_first / group;
-        const int all_from = a.window > 0 ? pc.span.at + (min(track_first + ROWS, packed) - 1) / group - a.window + 1 : 0;
-        int pos = ((int)(u - pc.begin) + pc.span.lo / TN) * TN;
-        float ref = 0.0f, l = 0.0f;
+        const int all_to = pc.at + (pc.row0 + x * ROWS) / group;
+        const int all_from = a.window > 0 ? pc.at + (min(pc.row0 + x * ROWS + ROWS, pc.packed) - 1) / group - a.window + 1 : 0;
+        const uint32_t begin = it, end = it + pc.steps;
+        int pos = pc.pos;
+        float ref = 0.0f, l = 0.0f, raise = 0.0f;
         bool empty = true;                           // nothing seen so far
-        for (int j = 0; j < steps; ++j, ++it, pos += TN) {
+        for (; it < end; ++it, pos += TN) {
           const int sb = TRACKS == 2 ? x : (int)(it & 1u);                         // score buffer
-          const uint32_t phase = TRACKS == 2 ? it & 1u : it >> 1 & 1u;
-          ok = wait.all(sc_full + 8 * (it % SCALE_SLOTS), it / SCALE_SLOTS & 1u) && wait.all(s_full + 8 * sb, phase);
+          ok = wait.all(sc_full + 8 * (it % SCALE_SLOTS), it / SCALE_SLOTS & 1u) &&
+               wait.all(s_full + 8 * sb, TRACKS == 2 ? it & 1u : it >> 1 & 1u);
           if (!ok) break;
           tc_fence_after();
-          float z[TN];
           const uint32_t s_col = lanes + C::S_COL + sb * TN;
-#pragma unroll
-          for (int c = 0; c < TN / 32; ++c) tc_ld32(s_col + 32 * c, z + 32 * c);
-          tc_ld_wait();
           const float4* sc = scales[it % SCALE_SLOTS];
-          float2* z2 = reinterpret_cast<float2*>(z);
-#pragma unroll
-          for (int b = 0; b < BLOCKS; ++b) {
-            const float4 s = sc[b];
-            const float k = row_scale * s.x, c = s.y - ref;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z2[8 * b + e] = __ffma2_rn(z2[8 * b + e], make_float2(k, k), make_float2(c, c));
-          }
           const bool whole = pos + TN - 1 <= all_to && pos >= all_from;
-          if (!whole) {
-            const int last = here - pos, first = a.window > 0 ? here - a.window + 1 - pos : 0;
+          // exponents of the 16 positions of block b from their scores
+          auto exponents = [&](uint32_t (&u)[16], const float4& s, int b) {
+            float2* z2 = reinterpret_cast<float2*>(u);
+            const float k = row_scale * s.x, o = s.y - ref;
 #pragma unroll
-            for (int e = 0; e < TN; ++e)
-              if (e > last || e < first) z[e] = -INFINITY;
-          }
-          float most = z[0];
+            for (int e = 0; e < 8; ++e) z2[e] = __ffma2_rn(z2[e], make_float2(k, k), make_float2(o, o));
+            if (!whole) {
+              const int last = here - pos - 16 * b, first = a.window > 0 ? here - a.window + 1 - pos - 16 * b : 0;
 #pragma unroll
-          for (int e = 1; e < TN; ++e) most = fmaxf(most, z[e]);
-          const bool raise = empty ? most > -INFINITY : most > LIMIT;
-          if (__any_sync(0xffffffffu, raise)) {
-            const float by = raise ? most : 0.0f, f = raise ? (empty ? 0.0f : exp2_fast(-most)) : 1.0f;
-            ref += by;
-            l *= f;
+              for (int e = 0; e < 16; ++e)
+                if (e > last || e < first) u[e] = 0xff800000u;
+            }
+          };
+          auto largest = [](const uint32_t (&u)[16], float (&tops)[4]) {
 #pragma unroll
-            for (int e = 0; e < TN / 2; ++e) z2[e] = __fadd2_rn(z2[e], make_float2(-by, -by));
-            empty = empty && !raise;
-            if (j > 0) {
-              ok = wait.all(o_full + 8 * x, (it - 1) & 1u);
-              if (!ok) break;
-              tc_fence_after();
+            for (int e = 0; e < 16; e += 8)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(u[e + i])), __uint_as_float(u[e + 4 + i]));
+          };
+          auto scale_accumulator = [&](float f) {    // of the products before this step
+            if (!wait.all(o_full + 8 * x, (it - 1) & 1u)) return false;
+            tc_fence_after();
 #pragma unroll 1
-              for (int c = 0; c < P; c += 32) {
-                float o[32];
-                tc_ld32(o_col + c, o);
-                tc_ld_wait();
+            for (int c = 0; c < P; c += 16) {
+              uint32_t o[16];
+              tc_ld16(o_col + c, o);
+              tc_ld16_wait(o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] *= f;
-                tc_st32(o_col + c, reinterpret_cast<const uint32_t*>(o));
-              }
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tc_st16(o_col + c, o);
+            }
+            return true;
+          };
+          if (__any_sync(0xffffffffu, raise > 0.0f)) {   // the step before asked for a higher reference
+            const float f = exp2_fast(-raise);
+            ok = scale_accumulator(f);
+            if (!ok) break;
+            ref += raise;
+            l *= f;
+          }
+          if (__any_sync(0xffffffffu, empty)) {          // rows that have seen nothing: their reference is the first maximum
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 2
+            for (int b = 0; b < BLOCKS; ++b) {
+              uint32_t z[16];
+              tc_ld16(s_col + 16 * b, z);
+              tc_ld16_wait(z);
+              exponents(z, sc[b], b);
+              largest(z, tops);
+            }
+            const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            if (empty && most > -INFINITY) {
+              ref = most;
+              empty = false;
             }
           }
-          // ---- weights, in the order of the values' operand
+          // ---- weights, 64 positions at a time, in the order of the values' operand, over the scores that they come from
+          raise = 0.0f;
 #pragma unroll
-          for (int c = 0; c < TN / 64; ++c) {
+          for (int h = 0; h < TN / 64; ++h) {
             uint32_t w[32];
+            float add;
+            for (int tries = 0;; ++tries) {
+              float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+              add = 0.0f;
+              // A block's exponentials are on their way while the one before is summed and packed.
+              uint32_t z[3][16];
+              float inv_s[2];
+              tc_ld16(s_col + 64 * h, z[0]);
+              tc_ld16_wait(z[0]);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              float* y = z + 64 * c + 16 * b;
-              const float2* y2 = reinterpret_cast<const float2*>(y);
+              for (int b = 0; b <= 4; ++b) {
+                if (b < 4) {
+                  uint32_t(&u)[16] = z[b % 3];
+                  if (b + 1 < 4) tc_ld16(s_col + 64 * h + 16 * (b + 1), z[(b + 1) % 3]);
+                  const float4 s = sc[4 * h + b];
+                  inv_s[b & 1] = s.z;
+                  exponents(u, s, 4 * h + b);
+                  largest(u, tops);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) y[e] = exp2_fast(y[e]);
-              float2 s = make_float2(0.f, 0.f);
+                  for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(exp2_fast(__uint_as_float(u[e])));
+                }
+                if (b > 0) {
+                  const int c = b - 1;
+                  const float2* y = reinterpret_cast<const float2*>(z[c % 3]);
+                  const float2 t = __fadd2_rn(__fadd2_rn(__fadd2_rn(y[0], y[1]), __fadd2_rn(y[2], y[3])),
+                                              __fadd2_rn(__fadd2_rn(y[4], y[5]), __fadd2_rn(y[6], y[7])));
+                  const float sum = t.x + t.y;
+                  // (a block that the row sees nothing of adds nothing, even with a scale of NaN)
+                  add = sum == 0.0f ? add : fmaf(sum, inv_s[c & 1], add);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) s = __fadd2_rn(s, y2[e]);
-              const float sum = s.x + s.y;
-              // (a block that the row sees nothing of adds nothing, even with a scale of NaN)
-              l = sum == 0.0f ? l : fmaf(sum, sc[4 * c + b].z, l);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                w[8 * b + 2 * e] = pack_f16(y2[e].x, y2[e].y);
-                w[8 * b + 2 * e + 1] = pack_f16(y2[4 + e].x, y2[4 + e].y);
+                  for (int e = 0; e < 4; ++e) {
+                    w[8 * c + 2 * e] = pack_f16(y[e].x, y[e].y);
+                    w[8 * c + 2 * e + 1] = pack_f16(y[4 + e].x, y[4 + e].y);
+                  }
+                }
+                if (b + 1 < 4) tc_ld16_wait(z[(b + 1) % 3]);
               }
+              const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+              raise = fmaxf(raise, most > LIMIT ? most : 0.0f);
+              // (where scores are so large that a reference rounds to another number it may never fit)
+              if (!__any_sync(0xffffffffu, most > HARD_LIMIT) || tries == 4) break;
+              // some weight would not fit fp16: the reference is raised at once, what there is so far is scaled
+              const float f = exp2_fast(-raise);
+              if (it > begin) {
+                ok = scale_accumulator(f);
+                if (!ok) break;
+              }
+              const __half2 f2 = __float2half2_rn(f);
+#pragma unroll 1
+              for (int c = 0; c < 32 * h; c += 16) {
+                uint32_t o[16];
+                tc_ld16(s_col + c, o);
+                tc_ld16_wait(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&o[e]), f2);
+                  o[e] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+                tc_st16(s_col + c, o);
+              }
+              ref += raise;
+              l *= f;
+              raise = 0.0f;
             }
-            tc_st32(s_col + 32 * c, w);
+            if (!ok) break;
+            l += add;
+            tc_st32(s_col + 32 * h, w);
           }
+          if (!ok) break;
           tc_st_wait();
           // One track's scores are issued ahead of the products before: the last but one has to be known to be over before
           // the last is waited for, and asked for while the last cannot be.
-          if (TRACKS == 1 && j > 0 && j == steps - 1) {
+          if (TRACKS == 1 && it > begin && it + 1 == end) {
             ok = wait.all(o_full + 8 * x, (it - 1) & 1u);
             if (!ok) break;
           }
@@ -334,33 +455,38 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         }
         if (!ok) break;
 
-        // ---- result
+        // ---- result; the next piece's query is fetched meanwhile (its tile's scores are complete)
+        PieceJob next;
+        ok = take(n, next);
+        if (!ok) break;
+        fetch_query(next);                           // (nothing where there is none: its rows are 0)
         ok = wait.all(o_full + 8 * x, (it - 1) & 1u);
         if (!ok) break;
         tc_fence_after();
-        const bool complete = u == pc.begin && stop == pc.end;
+        const int pr = pc.row0 + x * ROWS + r;
+        const bool mine = pr < pc.packed, complete = pc.part < 0;
         const float inv = !complete ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-        const long long row = pc.job.z + token;
-        const int slot = (2 * cta + (u == pc.begin ? 1 : 0)) * TILE + x * ROWS + r;
+        const long long row = pc.first_row + pr / group;
+        const int head = pc.head * group + pr % group;
+        const long long slot = (long long)pc.part * TILE + x * ROWS + r;
+        bf16* const out = a.out + row * a.out_row + head * a.out_head;
 #pragma unroll 1
-        for (int c = 0; c < P; c += 32) {
-          float o[32];
-          tc_ld32(o_col + c, o);
-          tc_ld_wait();
-          if (mine) {
-            if (complete) {
-              uint4* dst = reinterpret_cast<uint4*>(a.out + row * a.out_row + head * a.out_head + c);
+        for (int c = 0; c < P; c += 16) {
+          uint32_t o[16];
+          tc_ld16(o_col + c, o);
+          tc_ld16_wait(o);
+          if (!mine || c >= d) continue;             // (head_dim is a multiple of 16)
+          const float* f = reinterpret_cast<const float*>(o);
+          if (complete) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (c + 8 * i < d)
-                  dst[i] = make_uint4(float2_to_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), float2_to_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                                      float2_to_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), float2_to_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-            } else {
-              float4* dst = reinterpret_cast<float4*>(a.part + (long long)slot * P + c);
+            for (int i = 0; i < 2; ++i)
+              *reinterpret_cast<uint4*>(out + c + 8 * i) =
+                  make_uint4(float2_to_bf16x2(f[8 * i] * inv, f[8 * i + 1] * inv), float2_to_bf16x2(f[8 * i + 2] * inv, f[8 * i + 3] * inv),
+                             float2_to_bf16x2(f[8 * i + 4] * inv, f[8 * i + 5] * inv), float2_to_bf16x2(f[8 * i + 6] * inv, f[8 * i + 7] * inv));
+          } else {
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (c + 4 * i < d) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-            }
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<float4*>(a.part + slot * P + c + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
           }
         }
         tc_fence_before();
@@ -369,127 +495,142 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           if (!complete) a.part_ml[slot] = make_float2(top, l);
           else if (a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : top * LN2 + logf(l);
         }
-        u = stop;
+        if (next.steps > 0) row_scale = place_query(next);
+        pc = next;
       }
-      if (threadIdx.x == 0) a.joins[cta] = join;
     }
   } else if (warp < MMA_WARP) {
-    fewer_registers<CODE_REGS>();
+    if (CODE_REGS < 128) fewer_registers<CODE_REGS>();
     const int w = warp - SOFT_WARPS, tid = threadIdx.x - 32 * SOFT_WARPS;
-    constexpr int K_EACH = TN * P / 16 / (32 * CODE_WARPS), V_EACH = K_EACH / 2;   // 16-byte chunks of keys, 32 of values
-    // the step that is fetched next
-    long long u = line_begin;
-    Piece pc;
-    int left = 0, blk0 = 0;
-    auto places = [&](float4* scale, bool& more) -> long long {  // byte offset of the lane's block (lanes 0 .. BLOCKS - 1), -1: none
-      more = false;
+    // Three steps are under way: one is expanded, the codes of the next are on their way, and the pages of the one after
+    // are looked up.  Lanes 0 .. BLOCKS - 1 hold a block each.
+    struct Look {                                    // a step whose pages have been asked for
+      int page, block, heads_before;                 // page -1: none;  block of the page;  head * blocks of a page
+      bool more;                                     // is there such a step?
+    };
+    struct Found {                                   // a step whose codes can be asked for
+      int at;                                        // block of the cache, -1: none (block 0 is read for it, unused)
+      float2 scale;
+      bool more;
+    };
+    PieceJob pc;
+    uint32_t n_piece = 0;
+    int left = 0;
+    bool ended = false;                              // no more pieces, or a wait ran out
+    auto look = [&]() {
+      Look n = {-1, 0, 0, false};
       if (left == 0) {
-        if (u >= line_end) return -1;
-        pc = piece(u);
-        const long long stop = min(line_end, pc.end);
-        u = max(u, pc.begin);
-        if (u >= stop) return -1;
-        left = (int)(stop - u);
-        blk0 = ((int)(u - pc.begin) + pc.span.lo / TN) * BLOCKS;
-        u = stop;
+        ended = ended || !take(n_piece++, pc) || pc.steps == 0;
+        if (ended) return n;
+        left = pc.steps;
       }
-      more = true;
-      long long at = -1;
-      *scale = make_float4(0.f, -INFINITY, 0.f, 0.f);
-      const int b = blk0 + lane;
-      if (lane < BLOCKS && b < (pc.span.hi + CBLOCK - 1) / CBLOCK) {
-        at = block_index(a.c, a.pl, pc.job.x, b, a.status);
-        if (at >= 0) {
-          at += (long long)pc.head * a.c.bpp;
-          const float2 s = __ldg(a.c.scale + at);
-          const float vs = s.y == 0.0f ? 1.0f : s.y;
-          *scale = make_float4(s.x, __log2f(vs), __fdividef(1.0f, vs), 0.f);
-          at *= a.c.block_bytes;
-        }
+      n.more = true;
+      const int b = pc.pos / CBLOCK + lane;
+      if (lane < BLOCKS && b < (pc.hi + CBLOCK - 1) / CBLOCK) {
+        n.page = a.pl.tables[(long long)pc.request * a.pl.max_pages + b / a.c.bpp];
+        n.block = b % a.c.bpp;
+        if (n.page < 0) n.page = 0x7fffffff;         // (-1 is "none", not a page that does not exist)
       }
+      n.heads_before = pc.head * a.c.bpp;
       --left;
-      blk0 += BLOCKS;
-      return at;
+      pc.pos += TN;
+      return n;
     };
-    uint4 kr[K_EACH], vr[2 * V_EACH];
-    // key chunk e of this thread: token, quarter of a 64-value column, column
-    auto fetch_k = [&](long long place) {
-#pragma unroll
-      for (int e = 0; e < K_EACH; ++e) {
-        const int i = e * 32 * CODE_WARPS + tid, token = i / 4 % TN, h = i / (4 * TN);
-        const long long at = __shfl_sync(0xffffffffu, place, token / CBLOCK);
-        kr[e] = at >= 0 ? ldg_stream(a.c.codes + at + h * 1024 + token % CBLOCK * 64 + (i & 3) * 16) : make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+    auto find = [&](const Look& n) {
+      Found f = {-1, make_float2(0.f, 0.f), n.more};
+      if (n.page >= a.c.n_pages) raise_status(a.status, ADMMQ_ERR_SHAPE);
+      else if (n.page >= 0) {
+        f.at = n.page * (a.c.heads * a.c.bpp) + n.heads_before + n.block;
+        f.scale = __ldg(a.c.scale + f.at);
       }
+      return f;
     };
-    // value chunk e: two blocks by lane, g, and pairs of t; 32-value column
+    // Keys: chunk (h, i) of this thread is quarter kq of the 64 values from 64 h on of token kt + 32 i.  Values: chunk e is
+    // what lane (vg, 2 vu) and its neighbour hold (32 bytes) of a block and 32 columns; a warp takes two blocks.
+    constexpr int KH = P / 64, KI = TN / 32, PAIRS = BLOCKS / 2, VE = P / 32 * PAIRS / CODE_WARPS;
+    uint4 kr[KH][KI], vr[VE][2];
+    const int kq = tid & 3, kt = tid >> 2;
     const int vu = lane & 1, vb = lane >> 1 & 1, vg = (lane >> 2 & 1) | (lane >> 3) << 1;
-    auto fetch_v = [&](long long place) {
+    const int vblk = 2 * (w % PAIRS) + vb, vc = w / PAIRS;            // (columns 32 (vc + CODE_WARPS / PAIRS e))
+    const uint32_t k_src = kt % CBLOCK * 64 + kq * 16, v_src = 16 * P + vc * 512 + vg * 64 + vu * 32;
+    const uint32_t k_dst = kt * 128 + ((2 * kq) ^ (kt & 7)) * 16;      // (the neighbouring chunk: address ^ 16)
+    const uint32_t v_dst = vblk / 4 * (P * 128) + (32 * vc + 4 * vg) * 128;
+    auto fetch_k = [&](int at) {
 #pragma unroll
-      for (int e = 0; e < V_EACH; ++e) {
-        const int i = e * CODE_WARPS + w, pair = i % (BLOCKS / 2), c = i / (BLOCKS / 2);
-        const long long at = __shfl_sync(0xffffffffu, place, 2 * pair + vb);
-        const uint8_t* p = a.c.codes + at + 16 * P + c * 512 + vg * 64 + vu * 32;
-        const uint4 none = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-        vr[2 * e] = at >= 0 ? ldg_stream(p) : none;
-        vr[2 * e + 1] = at >= 0 ? ldg_stream(p + 16) : none;
+      for (int i = 0; i < KI; ++i) {
+        const int b = max(0, __shfl_sync(0xffffffffu, at, kt / CBLOCK + 2 * i));
+        const uint8_t* src = a.c.codes + (size_t)(uint32_t)b * (uint32_t)(32 * P) + k_src;
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kr[h][i] = ldg_stream(src + h * 1024);
       }
     };
-    float4 scale, next_scale;
-    bool more, next_more;                            // is there a step?
-    if (!A.hold_loads) {
-      long long place = places(&scale, more);
-      fetch_k(place);
-      fetch_v(place);
-      for (uint32_t it = 0; more; ++it, more = next_more) {
-        const uint32_t s = it % STAGES, ph = it / STAGES & 1u;
-        place = places(&next_scale, next_more);
-        if (!wait.all(k_empty + 8 * s, ph ^ 1u)) break;
-        uint8_t* kt = tiles_at + TRACKS * C::Q_BYTES + s * C::T_BYTES;
+    auto fetch_v = [&](int at) {
+      const int b = max(0, __shfl_sync(0xffffffffu, at, vblk));
+      const uint8_t* src = a.c.codes + (size_t)(uint32_t)b * (uint32_t)(32 * P) + v_src;
 #pragma unroll
-        for (int e = 0; e < K_EACH; ++e) {
-          const int i = e * 32 * CODE_WARPS + tid, token = i / 4 % TN, h = i / (4 * TN), q = i & 3;
-          uint8_t* dst = kt + h * (TN * 128) + token * 128;
-          const uint4 c = kr[e];
-          *reinterpret_cast<uint4*>(dst + (((2 * q) ^ (token & 7)) << 4)) =
-              make_uint4(two_codes<false>(c.x), two_codes<true>(c.x), two_codes<false>(c.y), two_codes<true>(c.y));
-          *reinterpret_cast<uint4*>(dst + (((2 * q + 1) ^ (token & 7)) << 4)) =
-              make_uint4(two_codes<false>(c.z), two_codes<true>(c.z), two_codes<false>(c.w), two_codes<true>(c.w));
+      for (int e = 0; e < VE; ++e) {
+        vr[e][0] = ldg_stream(src + e * (CODE_WARPS / PAIRS * 512));
+        vr[e][1] = ldg_stream(src + e * (CODE_WARPS / PAIRS * 512) + 16);
+      }
+    };
+    if (!A.hold_loads) {
+      Found now = find(look()), next;
+      fetch_k(now.at);
+      fetch_v(now.at);
+      Look ahead = look();
+      for (uint32_t it = 0; now.more; ++it) {
+        const uint32_t s = it % STAGES, ph = it / STAGES & 1u;
+        next = find(ahead);
+        ahead = look();
+        if (!wait.all(k_empty + 8 * s, ph ^ 1u)) break;
+        uint8_t* const to_k = tiles_at + TRACKS * C::Q_BYTES + s * C::T_BYTES;
+#pragma unroll
+        for (int h = 0; h < KH; ++h)
+#pragma unroll
+          for (int i = 0; i < KI; ++i) {
+            const uint4 c = kr[h][i];
+            uint8_t* dst = to_k + h * (TN * 128) + i * 4096;
+            *reinterpret_cast<uint4*>(dst + k_dst) =
+                make_uint4(two_codes<false>(c.x), two_codes<true>(c.x), two_codes<false>(c.y), two_codes<true>(c.y));
+            *reinterpret_cast<uint4*>(dst + (k_dst ^ 16)) =
+                make_uint4(two_codes<false>(c.z), two_codes<true>(c.z), two_codes<false>(c.w), two_codes<true>(c.w));
+          }
+        if (w == 0 && lane < BLOCKS) {
+          const float vs = now.scale.y == 0.0f ? 1.0f : now.scale.y;
+          scales[it % SCALE_SLOTS][lane] = now.at >= 0 ? make_float4(now.scale.x, __log2f(vs), __fdividef(1.0f, vs), 0.f)
+                                                       : make_float4(0.f, -INFINITY, 0.f, 0.f);
         }
-        if (w == 0 && lane < BLOCKS) scales[it % SCALE_SLOTS][lane] = scale;
         fence_async();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(k_full + 8 * s);
           if (w == 0) mbar_arrive(sc_full + 8 * (it % SCALE_SLOTS));
         }
-        fetch_k(place);
+        fetch_k(next.at);
         if (!wait.all(v_empty + 8 * s, ph ^ 1u)) break;
-        uint8_t* vt = tiles_at + TRACKS * C::Q_BYTES + (STAGES + s) * C::T_BYTES;
+        uint8_t* const to_v = tiles_at + TRACKS * C::Q_BYTES + (STAGES + s) * C::T_BYTES;
 #pragma unroll
-        for (int e = 0; e < V_EACH; ++e) {
-          const int i = e * CODE_WARPS + w, blk = 2 * (i % (BLOCKS / 2)) + vb, c = i / (BLOCKS / 2);
-          const uint4 lo = vr[2 * e], hi = vr[2 * e + 1];
-          const uint32_t l4[4] = {lo.x, lo.y, lo.z, lo.w}, h4[4] = {hi.x, hi.y, hi.z, hi.w};
+        for (int e = 0; e < VE; ++e) {
+          const uint32_t lo[4] = {vr[e][0].x, vr[e][0].y, vr[e][0].z, vr[e][0].w}, hi[4] = {vr[e][1].x, vr[e][1].y, vr[e][1].z, vr[e][1].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int row = 32 * c + 4 * vg + k;
-            *reinterpret_cast<uint4*>(vt + blk / 4 * (P * 128) + row * 128 + (((2 * (blk & 3) + vu) ^ (row & 7)) << 4)) =
-                make_uint4(two_codes<false>(l4[k]), two_codes<true>(l4[k]), two_codes<false>(h4[k]), two_codes<true>(h4[k]));
-          }
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<uint4*>(to_v + e * (CODE_WARPS / PAIRS * 4096) + v_dst + k * 128 +
+                                      (((2 * (vblk & 3) + vu) ^ ((4 * vg + k) & 7)) << 4)) =
+                make_uint4(two_codes<false>(lo[k]), two_codes<true>(lo[k]), two_codes<false>(hi[k]), two_codes<true>(hi[k]));
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(v_full + 8 * s);
-        fetch_v(place);
-        scale = next_scale;
+        fetch_v(next.at);
+        now = next;
       }
     }
   } else {
     fewer_registers<MMA_REGS>();
     if (warp == MMA_WARP) {
-      uint32_t it = 0, n_piece = 0;
+      uint32_t it = 0;
       bool ok = true;
-      // scores of step i (of the line) of track x
+      // scores of step i (of the CTA's) of track x
       auto scores = [&](uint32_t i, int x) {
         const uint64_t qd = make_kmajor_sw128_desc(q_at + x * C::Q_BYTES), kd = make_kmajor_sw128_desc(k_at + i % STAGES * C::T_BYTES);
         const int sb = TRACKS == 2 ? x : (int)(i & 1u);
@@ -503,16 +644,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         }
         __syncwarp();
       };
-      for (long long u = line_begin; ok && u < line_end; ++n_piece) {
-        const Piece pc = piece(u);
-        const long long stop = min(line_end, pc.end);
-        u = max(u, pc.begin);
-        if (u >= stop) break;
-        const int steps = (int)(stop - u);
-        u = stop;
+      PieceJob pc;
+      for (uint32_t n = 0; ok; ++n) {
+        ok = take(n, pc);
+        if (!ok || pc.steps == 0) break;
+        const int steps = pc.steps;
         ok = wait.all(k_full + 8 * (it % STAGES), it / STAGES & 1u);
         for (int x = 0; x < TRACKS && ok; ++x) {
-          ok = wait.all(q_full + 8 * x, n_piece & 1u);
+          ok = wait.all(q_full + 8 * x, n & 1u);
           if (!ok) break;
           tc_fence_after();
           scores(it, x);
@@ -549,6 +688,41 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           }
         }
       }
+    } else if (warp == PLAN_WARP) {
+      const int ctas = active_ctas(total, 1), cta = blockIdx.x;
+      long long u = cta < ctas ? line_at(total, cta, ctas) : 0;
+      const long long line_end = cta < ctas ? line_at(total, cta + 1, ctas) : 0;
+      int4 join = make_int4(-1, 0, 0, 0);
+      for (uint32_t n = 0;; ++n) {
+        PieceJob p = {};
+        if (u < line_end) {
+          const Piece f = find_piece<THREADS, TN, TILE, EXTRA>(a, job, n_tiles, schedule, u);
+          const long long stop = min(line_end, f.end);
+          u = max(u, f.begin);
+          if (u < stop) {
+            p.steps = (int)(stop - u);
+            p.pos = ((int)(u - f.begin) + f.span.lo / TN) * TN;
+            p.head = f.head;
+            p.request = f.job.x;
+            p.row0 = f.job.y;
+            p.first_row = f.job.z;
+            p.packed = f.job.w * a.pl.group;
+            p.at = f.span.at;
+            p.hi = f.span.hi;
+            p.part = u == f.begin && stop == f.end ? -1 : 2 * cta + (u == f.begin ? 1 : 0);
+            if (u == f.begin && stop < f.end) join = make_int4(f.tile, f.head, cta_of(f.end - 1, total, ctas), 0);
+            u = stop;
+          }
+        }
+        if (!wait.all(p_empty + 8 * (n % PIECE_SLOTS), (n / PIECE_SLOTS & 1u) ^ 1u)) break;
+        if (lane == 0) {
+          pieces[n % PIECE_SLOTS] = p;
+          mbar_arrive(p_full + 8 * (n % PIECE_SLOTS));
+        }
+        __syncwarp();
+        if (p.steps == 0) break;
+      }
+      if (lane == 0) a.joins[cta] = join;
     }
   }
   __syncthreads();

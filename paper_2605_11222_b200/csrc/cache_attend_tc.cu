@@ -27,9 +27,9 @@
 namespace admmq {
 namespace {
 
-constexpr int ROWS = 128, SOFT_WARPS = 8, CODE_WARPS = 4, WARPS = 16, THREADS = 32 * WARPS, MMA_WARP = SOFT_WARPS + CODE_WARPS, PLAN_WARP = MMA_WARP + 1;
-constexpr int SOFT_REGS = 152, CODE_REGS = 112, MMA_REGS = 96;     // of 128 each at launch
-static_assert(2 * SOFT_REGS + CODE_REGS + MMA_REGS <= 4 * 128, "registers");
+constexpr int ROWS = 128, SOFT_WARPS = 16, CODE_WARPS = 4, WARPS = 24, THREADS = 32 * WARPS, MMA_WARP = SOFT_WARPS + CODE_WARPS, PLAN_WARP = MMA_WARP + 1;
+constexpr int SOFT_REGS = 88, CODE_REGS = 88, MMA_REGS = 40;      // of 80 each at launch
+static_assert(4 * SOFT_REGS + CODE_REGS + MMA_REGS <= 6 * 80, "registers");
 constexpr int STAGES = 2, SCALE_SLOTS = 4, PIECE_SLOTS = 4;
 constexpr int EXTRA = 3;                             // a piece's start and end, in steps
 // Weights above 2^LIMIT raise the reference for the steps that follow; fp16 holds them up to 2^HARD_LIMIT.
@@ -69,15 +69,21 @@ __device__ __forceinline__ void tc_ld16_wait(uint32_t (&u)[16]) {
                  "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
                :: "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* u) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-      ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
-      "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]),
-      "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]),
-      "r"(u[31]), "r"(taddr)
-      : "memory");
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t (&u)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tc_ld8_wait(uint32_t (&u)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7])
+               :: "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&u)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]),
+               "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(taddr)
+               : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&u)[16]) {
   asm volatile(
@@ -97,40 +103,21 @@ __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// Bounded wait of a whole warp with one answer for all its lanes.  A try sleeps for up to `NAP` ns: polled, the barriers took
-// a third of the issue slots.  (Inlined: setmaxnreg asks for a kernel without calls.)
+// Bounded wait of a whole warp with one answer for all its lanes.  (Inlined: setmaxnreg asks for a kernel without calls.)
 struct WarpWait {
   volatile int* abort_flag;
   int* status;
   long long limit;
-  static constexpr uint32_t NAP = 4000;
-  __device__ __forceinline__ static bool nap(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-        "selp.b32 %0, 1, 0, p;\n}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(NAP)
-        : "memory");
-    return done != 0;
-  }
   __device__ __forceinline__ bool all(uint32_t bar, uint32_t parity) const {
-    bool ok = nap(bar, parity);
-    if (!ok) {
-      const long long t0 = clock64();
-      do {
-        ok = nap(bar, parity);
-        if (!ok && (*abort_flag || clock64() - t0 > limit)) {
-          *abort_flag = 1;
-          raise_status(status, ST_TIMEOUT);
-          break;
-        }
-      } while (!ok);
-    }
-    return __all_sync(0xffffffffu, ok) != 0;
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, limit)) != 0;
   }
 };
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 
 struct ManyArgs {
   AttendArgs a;
@@ -166,9 +153,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   // scores' buffer read); accumulator complete; queries in place; scales in place; pieces.  Waits go by parity, so a waiter
   // has to know that the phase before is over and that the one after cannot be: the scales have a barrier a slot because the
   // keys' may be a phase on before a slow warp of the softmax has looked.
-  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 * PIECE_SLOTS + 2 + 2 + 2 + 2 + 1];
+  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 * PIECE_SLOTS + 2 + 2 + 2 + 2 + 1 + 2 * ROWS / 32];
   __shared__ float4 scales[SCALE_SLOTS][BLOCKS];     // key scale, log2 of the value scale, its reciprocal
   __shared__ PieceJob pieces[PIECE_SLOTS];
+  __shared__ float swapped[2][2][2 * ROWS];          // between the two threads of a row
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
 
@@ -179,7 +167,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   const WarpWait wait = {&abort_s, a.status, A.wait_limit};
   const uint32_t k_full = smem_u32(&bars[0]), k_empty = k_full + 8 * STAGES, v_full = k_empty + 8 * STAGES, v_empty = v_full + 8 * STAGES;
   const uint32_t s_full = v_empty + 8 * STAGES, w_full = s_full + 16, o_full = w_full + 16, q_full = o_full + 16, drain_bar = q_full + 16,
-                 sc_full = drain_bar + 8, p_full = sc_full + 8 * SCALE_SLOTS, p_empty = p_full + 8 * PIECE_SLOTS;
+                 sc_full = drain_bar + 8, p_full = sc_full + 8 * SCALE_SLOTS, p_empty = p_full + 8 * PIECE_SLOTS, pair_bar = p_empty + 8 * PIECE_SLOTS;
 
   if (threadIdx.x == 0) {
     abort_s = 0;
@@ -191,16 +179,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full + 8 * x, 1);
-      mbar_init(w_full + 8 * x, ROWS / 32);
+      mbar_init(w_full + 8 * x, 2 * ROWS / 32);
       mbar_init(o_full + 8 * x, 1);
-      mbar_init(q_full + 8 * x, ROWS / 32);
+      mbar_init(q_full + 8 * x, 2 * ROWS / 32);
     }
     mbar_init(drain_bar, 1);
     for (int s = 0; s < SCALE_SLOTS; ++s) mbar_init(sc_full + 8 * s, 1);
     for (int s = 0; s < PIECE_SLOTS; ++s) {
       mbar_init(p_full + 8 * s, 1);
-      mbar_init(p_empty + 8 * s, TRACKS * ROWS / 32 + CODE_WARPS + 1);
+      mbar_init(p_empty + 8 * s, 2 * TRACKS * ROWS / 32 + CODE_WARPS + 1);
     }
+    for (int s = 0; s < 2 * ROWS / 32; ++s) mbar_init(pair_bar + 8 * s, 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) {
@@ -226,51 +215,62 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   };
 
   if (warp < SOFT_WARPS) {
-    more_registers<SOFT_REGS>();
-    const int x = warp >> 2, r = (warp & 3) * 32 + lane;
+    if (SOFT_REGS > 80) more_registers<SOFT_REGS>();
+    // Two threads to a row, of warps w and w + 4: each has half of a step's positions, of the query and of the result.
+    const int x = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+    constexpr int CW = TN / 2;                       // positions of a thread
     if (x < TRACKS) {
       const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-      const uint32_t o_col = lanes + C::O_COL + x * P;
+      const uint32_t o_col = lanes + C::O_COL + x * P + half * (P / 2);
       const int group = a.pl.group, d = a.c.d;
-      constexpr bool AHEAD = P <= 128;               // a query is fetched ahead (64 registers) while a result leaves
-      uint4 raw[AHEAD ? P / 8 : 1];
-      auto query_at = [&](const PieceJob& p) {
-        const int pr = p.row0 + x * ROWS + r;
-        return a.q + (long long)(p.first_row + pr / group) * a.q_row + (p.head * group + pr % group) * a.q_head;
+      // A value of each of a row's threads to the other; false: a wait ran out.
+      uint32_t swaps = 0;
+      auto swap = [&](float mine, float& other) {
+        const uint32_t bar = pair_bar + 8 * (4 * x + (warp & 3)), side = swaps & 1u;
+        swapped[side][half][x * ROWS + r] = mine;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+        if (!wait.all(bar, side)) return false;
+        other = swapped[side][half ^ 1][x * ROWS + r];
+        ++swaps;
+        return true;
       };
-      auto chunk = [&](const PieceJob& p, const bf16* src, int c) {
-        return p.row0 + x * ROWS + r < p.packed && 8 * c < d ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
+      constexpr int QC = P / 16;                     // 16-byte chunks of half a query
+      constexpr bool AHEAD = P <= 128;               // it is fetched ahead (32 registers) while a result leaves
+      uint4 raw[AHEAD ? QC : 1];
+      auto chunk = [&](const PieceJob& p, int c) {
+        const int pr = p.row0 + x * ROWS + r, at = half * QC + c;
+        const bf16* src = a.q + (long long)(p.first_row + pr / group) * a.q_row + (p.head * group + pr % group) * a.q_head;
+        return pr < p.packed && 8 * at < d ? __ldg(reinterpret_cast<const uint4*>(src) + at) : make_uint4(0, 0, 0, 0);
       };
       auto fetch_query = [&](const PieceJob& p) {
         if (AHEAD) {
-          const bf16* src = query_at(p);
 #pragma unroll
-          for (int c = 0; c < P / 8; ++c) raw[AHEAD ? c : 0] = chunk(p, src, c);
+          for (int c = 0; c < QC; ++c) raw[AHEAD ? c : 0] = chunk(p, c);
         }
       };
-      // The row's query: times a power of two, as fp16, into its operand tile.  Returns the factor that takes it to base-2
-      // exponents.
-      auto place_query = [&](const PieceJob& p) {
-        const bf16* src = query_at(p);
-        float top = 0.0f;
-        bool finite = true;
-#pragma unroll (AHEAD ? 16 : 8)
-        for (int c = 0; c < P / 8; ++c) {
-          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, src, c);
+      // The row's query: times a power of two, as fp16, into its operand tile; `factor` takes scores to base-2 exponents.
+      auto place_query = [&](const PieceJob& p, float& factor) {
+        float top = 0.0f, other;
+#pragma unroll (AHEAD ? 8 : 4)
+        for (int c = 0; c < QC; ++c) {
+          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, c);
           const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 f = bf16x2_to_float2(w[e]);
             top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-            finite &= isfinite(f.x) && isfinite(f.y);
+            if (!(isfinite(f.x) && isfinite(f.y))) top = INFINITY;
           }
         }
+        if (!swap(top, other)) return false;
+        top = fmaxf(top, other);
         float inv;
         const float up = pow2_scale_for(top, &inv);
         uint8_t* dst = tiles_at + x * C::Q_BYTES + r * 128;
-#pragma unroll (AHEAD ? 16 : 8)
-        for (int c = 0; c < P / 8; ++c) {
-          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, src, c);
+#pragma unroll (AHEAD ? 8 : 4)
+        for (int c = 0; c < QC; ++c) {
+          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, c);
           const uint32_t w[4] = {q.x, q.y, q.z, q.w};
           uint32_t h[4];
 #pragma unroll
@@ -278,12 +278,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             const float2 f = bf16x2_to_float2(w[e]);
             h[e] = pack_f16(f.x * up, f.y * up);
           }
-          *reinterpret_cast<uint4*>(dst + c / 8 * (ROWS * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          const int at = half * QC + c;
+          *reinterpret_cast<uint4*>(dst + at / 8 * (ROWS * 128) + (((at & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full + 8 * x);
-        return finite ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
+        factor = top < INFINITY ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
+        return true;
       };
 
       PieceJob pc;
@@ -292,50 +294,67 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       float row_scale = 0.0f;
       if (ok && pc.steps > 0) {
         fetch_query(pc);
-        row_scale = place_query(pc);
+        ok = place_query(pc, row_scale);
       }
       for (uint32_t n = 1; ok && pc.steps > 0; ++n) {
-        const int here = pc.at + (pc.row0 + x * ROWS + r) / group;
-        // positions that every row of the track sees: up to its first row's own, from its last row's window on
-        const int all_to = pc.at + (pc.row0 + x * ROWS) / group;
-        const int all_from = a.window > 0 ? pc.at + (min(pc.row0 + x * ROWS + ROWS, pc.packed) - 1) / group - a.window + 1 : 0;
+        // position of the row within the thread's part of the piece's first step, and what every row of the track sees: up
+        // to its first row's own position, from its last row's window on
+        const int shift = pc.pos + half * CW;
+        int here = pc.at + (pc.row0 + x * ROWS + r) / group - shift;
+        int all_to = pc.at + (pc.row0 + x * ROWS) / group - shift;
+        int all_from = a.window > 0 ? pc.at + (min(pc.row0 + x * ROWS + ROWS, pc.packed) - 1) / group - a.window + 1 - shift : -0x40000000;
         const uint32_t begin = it, end = it + pc.steps;
-        int pos = pc.pos;
         float ref = 0.0f, l = 0.0f, raise = 0.0f;
         bool empty = true;                           // nothing seen so far
-        for (; it < end; ++it, pos += TN) {
+        for (; it < end; ++it, here -= TN, all_to -= TN, all_from -= TN) {
           const int sb = TRACKS == 2 ? x : (int)(it & 1u);                         // score buffer
           ok = wait.all(sc_full + 8 * (it % SCALE_SLOTS), it / SCALE_SLOTS & 1u) &&
                wait.all(s_full + 8 * sb, TRACKS == 2 ? it & 1u : it >> 1 & 1u);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t s_col = lanes + C::S_COL + sb * TN;
-          const float4* sc = scales[it % SCALE_SLOTS];
-          const bool whole = pos + TN - 1 <= all_to && pos >= all_from;
+          const uint32_t s_col = lanes + C::S_COL + sb * TN + half * CW;
+          const float4* sc = scales[it % SCALE_SLOTS] + half * (BLOCKS / 2);
+          const bool whole = CW - 1 <= all_to && 0 >= all_from;
           // exponents of the 16 positions of block b from their scores
-          auto exponents = [&](uint32_t (&u)[16], const float4& s, int b) {
+          auto exponents = [&](uint32_t (&u)[16], const float4& s, int b, float reference) {
             float2* z2 = reinterpret_cast<float2*>(u);
-            const float k = row_scale * s.x, o = s.y - ref;
+            const float k = row_scale * s.x, o = s.y - reference;
 #pragma unroll
             for (int e = 0; e < 8; ++e) z2[e] = __ffma2_rn(z2[e], make_float2(k, k), make_float2(o, o));
             if (!whole) {
-              const int last = here - pos - 16 * b, first = a.window > 0 ? here - a.window + 1 - pos - 16 * b : 0;
+              const int last = here - 16 * b, first = a.window > 0 ? here - a.window + 1 - 16 * b : 0;
 #pragma unroll
               for (int e = 0; e < 16; ++e)
                 if (e > last || e < first) u[e] = 0xff800000u;
             }
           };
-          auto largest = [](const uint32_t (&u)[16], float (&tops)[4]) {
-#pragma unroll
-            for (int e = 0; e < 16; e += 8)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(u[e + i])), __uint_as_float(u[e + 4 + i]));
+          auto largest = [](const uint32_t (&u)[16]) {
+            const float* f = reinterpret_cast<const float*>(u);
+            const float a = max3(f[0], f[1], f[2]), b = max3(f[3], f[4], f[5]), c = max3(f[6], f[7], f[8]), d = max3(f[9], f[10], f[11]),
+                        e = max3(f[12], f[13], f[14]);
+            return fmaxf(max3(a, b, f[15]), max3(c, d, e));
           };
-          auto scale_accumulator = [&](float f) {    // of the products before this step
+          auto scale_weights = [&](uint32_t col, int n, float f) {   // those of this step that are there, n columns of them
+            const __half2 f2 = __float2half2_rn(f);
+            tc_st_wait();
+#pragma unroll 1
+            for (int c = 0; c < n; c += 8) {
+              uint32_t o[8];
+              tc_ld8(col + c, o);
+              tc_ld8_wait(o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&o[e]), f2);
+                o[e] = *reinterpret_cast<const uint32_t*>(&v);
+              }
+              tc_st8(col + c, o);
+            }
+          };
+          auto scale_accumulator = [&](float f) {    // the thread's half of it, of the products before this step
             if (!wait.all(o_full + 8 * x, (it - 1) & 1u)) return false;
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < P; c += 16) {
+            for (int c = 0; c < P / 2; c += 16) {
               uint32_t o[16];
               tc_ld16(o_col + c, o);
               tc_ld16_wait(o);
@@ -353,95 +372,77 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             l *= f;
           }
           if (__any_sync(0xffffffffu, empty)) {          // rows that have seen nothing: their reference is the first maximum
-            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 2
-            for (int b = 0; b < BLOCKS; ++b) {
+            float most = -INFINITY, other;
+#pragma unroll 1
+            for (int b = 0; b < CW / 16; ++b) {
               uint32_t z[16];
               tc_ld16(s_col + 16 * b, z);
               tc_ld16_wait(z);
-              exponents(z, sc[b], b);
-              largest(z, tops);
+              exponents(z, sc[b], b, ref);
+              most = fmaxf(most, largest(z));
             }
-            const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-            if (empty && most > -INFINITY) {
-              ref = most;
+            ok = swap(most, other);
+            if (!ok) break;
+            if (empty && fmaxf(most, other) > -INFINITY) {
+              ref = fmaxf(most, other);
               empty = false;
             }
           }
-          // ---- weights, 64 positions at a time, in the order of the values' operand, over the scores that they come from
-          raise = 0.0f;
+          // ---- weights, in the order of the values' operand, over the scores that they come from, block by block.  `up`: how
+          // far a weight that fp16 would not hold has raised the thread's reference in this step.
+          float up = 0.0f, peak = -INFINITY, add = 0.0f;
+          uint32_t z[2][16];
+          tc_ld16(s_col, z[0]);
+          tc_ld16_wait(z[0]);
 #pragma unroll
-          for (int h = 0; h < TN / 64; ++h) {
-            uint32_t w[32];
-            float add;
-            for (int tries = 0;; ++tries) {
-              float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-              add = 0.0f;
-              // A block's exponentials are on their way while the one before is summed and packed.
-              uint32_t z[3][16];
-              float inv_s[2];
-              tc_ld16(s_col + 64 * h, z[0]);
-              tc_ld16_wait(z[0]);
+          for (int b = 0; b < CW / 16; ++b) {
+            uint32_t(&u)[16] = z[b & 1];
+            if (b + 1 < CW / 16) tc_ld16(s_col + 16 * (b + 1), z[(b + 1) & 1]);
+            const float4 s = sc[b];
+            exponents(u, s, b, ref + up);
+            const float top = largest(u);
+            peak = fmaxf(peak, top + up);
+            if (__any_sync(0xffffffffu, top > HARD_LIMIT)) {
+              const float by = top > HARD_LIMIT ? top : 0.0f, f = exp2_fast(-by);
+              scale_weights(s_col, 8 * b, f);
+              add *= f;
+              up += by;
 #pragma unroll
-              for (int b = 0; b <= 4; ++b) {
-                if (b < 4) {
-                  uint32_t(&u)[16] = z[b % 3];
-                  if (b + 1 < 4) tc_ld16(s_col + 64 * h + 16 * (b + 1), z[(b + 1) % 3]);
-                  const float4 s = sc[4 * h + b];
-                  inv_s[b & 1] = s.z;
-                  exponents(u, s, 4 * h + b);
-                  largest(u, tops);
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(exp2_fast(__uint_as_float(u[e])));
-                }
-                if (b > 0) {
-                  const int c = b - 1;
-                  const float2* y = reinterpret_cast<const float2*>(z[c % 3]);
-                  const float2 t = __fadd2_rn(__fadd2_rn(__fadd2_rn(y[0], y[1]), __fadd2_rn(y[2], y[3])),
-                                              __fadd2_rn(__fadd2_rn(y[4], y[5]), __fadd2_rn(y[6], y[7])));
-                  const float sum = t.x + t.y;
-                  // (a block that the row sees nothing of adds nothing, even with a scale of NaN)
-                  add = sum == 0.0f ? add : fmaf(sum, inv_s[c & 1], add);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    w[8 * c + 2 * e] = pack_f16(y[e].x, y[e].y);
-                    w[8 * c + 2 * e + 1] = pack_f16(y[4 + e].x, y[4 + e].y);
-                  }
-                }
-                if (b + 1 < 4) tc_ld16_wait(z[(b + 1) % 3]);
-              }
-              const float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-              raise = fmaxf(raise, most > LIMIT ? most : 0.0f);
-              // (where scores are so large that a reference rounds to another number it may never fit)
-              if (!__any_sync(0xffffffffu, most > HARD_LIMIT) || tries == 4) break;
-              // some weight would not fit fp16: the reference is raised at once, what there is so far is scaled
-              const float f = exp2_fast(-raise);
-              if (it > begin) {
-                ok = scale_accumulator(f);
-                if (!ok) break;
-              }
-              const __half2 f2 = __float2half2_rn(f);
-#pragma unroll 1
-              for (int c = 0; c < 32 * h; c += 16) {
-                uint32_t o[16];
-                tc_ld16(s_col + c, o);
-                tc_ld16_wait(o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&o[e]), f2);
-                  o[e] = *reinterpret_cast<const uint32_t*>(&v);
-                }
-                tc_st16(s_col + c, o);
-              }
-              ref += raise;
-              l *= f;
-              raise = 0.0f;
+              for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - by);
             }
-            if (!ok) break;
-            l += add;
-            tc_st32(s_col + 32 * h, w);
+            float2* y = reinterpret_cast<float2*>(u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = make_float2(exp2_fast(y[e].x), exp2_fast(y[e].y));
+            const float2 t = __fadd2_rn(__fadd2_rn(__fadd2_rn(y[0], y[1]), __fadd2_rn(y[2], y[3])),
+                                        __fadd2_rn(__fadd2_rn(y[4], y[5]), __fadd2_rn(y[6], y[7])));
+            add = fmaf(t.x + t.y, s.z, add);
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              w[2 * e] = pack_f16(y[e].x, y[e].y);
+              w[2 * e + 1] = pack_f16(y[4 + e].x, y[4 + e].y);
+            }
+            if (b + 1 < CW / 16) tc_ld16_wait(z[(b + 1) & 1]);
+            tc_st8(s_col + 8 * b, w);
           }
+          float other;
+          ok = swap(peak, other);
           if (!ok) break;
+          peak = fmaxf(peak, other);
+          raise = peak > LIMIT ? peak : 0.0f;
+          if (__any_sync(0xffffffffu, peak > HARD_LIMIT)) {   // it cannot wait for the next step
+            const float by = peak > HARD_LIMIT ? peak : 0.0f, f = exp2_fast(-by), f_step = exp2_fast(up - by);
+            scale_weights(s_col, CW / 2, f_step);
+            add *= f_step;
+            if (it > begin) {
+              ok = scale_accumulator(f);
+              if (!ok) break;
+            }
+            l *= f;
+            ref += by;
+            raise = peak > HARD_LIMIT ? 0.0f : raise;
+          }
+          l += add;
           tc_st_wait();
           // One track's scores are issued ahead of the products before: the last but one has to be known to be over before
           // the last is waited for, and asked for while the last cannot be.
@@ -460,8 +461,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         ok = take(n, next);
         if (!ok) break;
         fetch_query(next);                           // (nothing where there is none: its rows are 0)
-        ok = wait.all(o_full + 8 * x, (it - 1) & 1u);
+        float other;
+        ok = swap(l, other) && wait.all(o_full + 8 * x, (it - 1) & 1u);
         if (!ok) break;
+        l = half == 0 ? l + other : other + l;       // (one order for both)
         tc_fence_after();
         const int pr = pc.row0 + x * ROWS + r;
         const bool mine = pr < pc.packed, complete = pc.part < 0;
@@ -471,36 +474,37 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         const long long slot = (long long)pc.part * TILE + x * ROWS + r;
         bf16* const out = a.out + row * a.out_row + head * a.out_head;
 #pragma unroll 1
-        for (int c = 0; c < P; c += 16) {
+        for (int i = 0; i < P / 2; i += 16) {
           uint32_t o[16];
-          tc_ld16(o_col + c, o);
+          tc_ld16(o_col + i, o);
           tc_ld16_wait(o);
+          const int c = half * (P / 2) + i;
           if (!mine || c >= d) continue;             // (head_dim is a multiple of 16)
           const float* f = reinterpret_cast<const float*>(o);
           if (complete) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-              *reinterpret_cast<uint4*>(out + c + 8 * i) =
-                  make_uint4(float2_to_bf16x2(f[8 * i] * inv, f[8 * i + 1] * inv), float2_to_bf16x2(f[8 * i + 2] * inv, f[8 * i + 3] * inv),
-                             float2_to_bf16x2(f[8 * i + 4] * inv, f[8 * i + 5] * inv), float2_to_bf16x2(f[8 * i + 6] * inv, f[8 * i + 7] * inv));
+            for (int k = 0; k < 2; ++k)
+              *reinterpret_cast<uint4*>(out + c + 8 * k) =
+                  make_uint4(float2_to_bf16x2(f[8 * k] * inv, f[8 * k + 1] * inv), float2_to_bf16x2(f[8 * k + 2] * inv, f[8 * k + 3] * inv),
+                             float2_to_bf16x2(f[8 * k + 4] * inv, f[8 * k + 5] * inv), float2_to_bf16x2(f[8 * k + 6] * inv, f[8 * k + 7] * inv));
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<float4*>(a.part + slot * P + c + 4 * i) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            for (int k = 0; k < 4; ++k)
+              *reinterpret_cast<float4*>(a.part + slot * P + c + 4 * k) = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
           }
         }
         tc_fence_before();
         const float top = empty ? -INFINITY : ref;
-        if (mine) {
+        if (mine && half == 0) {
           if (!complete) a.part_ml[slot] = make_float2(top, l);
           else if (a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : top * LN2 + logf(l);
         }
-        if (next.steps > 0) row_scale = place_query(next);
+        if (next.steps > 0) ok = place_query(next, row_scale);
         pc = next;
       }
     }
   } else if (warp < MMA_WARP) {
-    if (CODE_REGS < 128) fewer_registers<CODE_REGS>();
+    more_registers<CODE_REGS>();
     const int w = warp - SOFT_WARPS, tid = threadIdx.x - 32 * SOFT_WARPS;
     // Three steps are under way: one is expanded, the codes of the next are on their way, and the pages of the one after
     // are looked up.  Lanes 0 .. BLOCKS - 1 hold a block each.
@@ -597,7 +601,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           }
         if (w == 0 && lane < BLOCKS) {
           const float vs = now.scale.y == 0.0f ? 1.0f : now.scale.y;
-          scales[it % SCALE_SLOTS][lane] = now.at >= 0 ? make_float4(now.scale.x, __log2f(vs), __fdividef(1.0f, vs), 0.f)
+          // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
+          scales[it % SCALE_SLOTS][lane] = now.at >= 0 ? make_float4(now.scale.x, __log2f(vs), vs == vs ? __fdividef(1.0f, vs) : 1.0f, 0.f)
                                                        : make_float4(0.f, -INFINITY, 0.f, 0.f);
         }
         fence_async();
@@ -673,7 +678,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < TN / 16; ++k)
-                tc_mma_f16_ts(tmem + C::O_COL + x * P, tmem + C::S_COL + sb * TN + 8 * k, desc_of(vd, k / 4 * (P * 128) + k % 4 * 32),
+                tc_mma_f16_ts(tmem + C::O_COL + x * P, tmem + C::S_COL + sb * TN + k / (TN / 32) * (TN / 2) + k % (TN / 32) * 8, desc_of(vd, k / 4 * (P * 128) + k % 4 * 32),
                               idesc_f16(P), j > 0 || k > 0);
               tc_commit(o_full + 8 * x);
               if (x == TRACKS - 1) tc_commit(v_empty + 8 * s);

@@ -69,6 +69,25 @@ __device__ __forceinline__ void tc_ld16_wait(uint32_t (&u)[16]) {
                  "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
                :: "memory");
 }
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&u)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]),
+        "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]),
+        "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld32_wait(uint32_t (&u)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
+                 "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
+               :: "memory");
+  asm volatile("" : "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]),
+                    "+r"(u[25]), "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31]));
+}
 __device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t (&u)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
@@ -113,6 +132,28 @@ struct WarpWait {
   }
 };
 
+// Waits, within the limit, for the word with the tag.
+__device__ __forceinline__ bool poll_swap(uint32_t from, uint32_t tag, float& value, const WarpWait& wait) {
+  uint32_t v, t;
+  auto look = [&] {
+    asm volatile("ld.volatile.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v), "=r"(t) : "r"(from) : "memory");
+    return __all_sync(0xffffffffu, t == tag) != 0;
+  };
+  bool ok = look();
+  if (!ok) {
+    const long long t0 = clock64();
+    while (!(ok = look())) {
+      const bool late = *wait.abort_flag || clock64() - t0 > wait.limit;
+      if (__any_sync(0xffffffffu, late)) {
+        *wait.abort_flag = 1;
+        raise_status(wait.status, ST_TIMEOUT);
+        break;
+      }
+    }
+  }
+  value = __uint_as_float(v);
+  return ok;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -153,10 +194,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   // scores' buffer read); accumulator complete; queries in place; scales in place; pieces.  Waits go by parity, so a waiter
   // has to know that the phase before is over and that the one after cannot be: the scales have a barrier a slot because the
   // keys' may be a phase on before a slow warp of the softmax has looked.
-  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 * PIECE_SLOTS + 2 + 2 + 2 + 2 + 1 + 2 * ROWS / 32];
+  __shared__ __align__(8) uint64_t bars[4 * STAGES + SCALE_SLOTS + 2 * PIECE_SLOTS + 2 + 2 + 2 + 2 + 1];
   __shared__ float4 scales[SCALE_SLOTS][BLOCKS];     // key scale, log2 of the value scale, its reciprocal
   __shared__ PieceJob pieces[PIECE_SLOTS];
-  __shared__ float swapped[2][2][2 * ROWS];          // between the two threads of a row
+  __shared__ __align__(8) uint2 swapped[2][2][2 * ROWS];   // between the two threads of a row
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_s;
 
@@ -167,8 +208,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   const WarpWait wait = {&abort_s, a.status, A.wait_limit};
   const uint32_t k_full = smem_u32(&bars[0]), k_empty = k_full + 8 * STAGES, v_full = k_empty + 8 * STAGES, v_empty = v_full + 8 * STAGES;
   const uint32_t s_full = v_empty + 8 * STAGES, w_full = s_full + 16, o_full = w_full + 16, q_full = o_full + 16, drain_bar = q_full + 16,
-                 sc_full = drain_bar + 8, p_full = sc_full + 8 * SCALE_SLOTS, p_empty = p_full + 8 * PIECE_SLOTS, pair_bar = p_empty + 8 * PIECE_SLOTS;
+                 sc_full = drain_bar + 8, p_full = sc_full + 8 * SCALE_SLOTS, p_empty = p_full + 8 * PIECE_SLOTS;
 
+  for (int i = threadIdx.x; i < 8 * ROWS; i += THREADS) swapped[0][0][i] = make_uint2(0u, 0u);
   if (threadIdx.x == 0) {
     abort_s = 0;
     for (int s = 0; s < STAGES; ++s) {
@@ -189,7 +231,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       mbar_init(p_full + 8 * s, 1);
       mbar_init(p_empty + 8 * s, 2 * TRACKS * ROWS / 32 + CODE_WARPS + 1);
     }
-    for (int s = 0; s < 2 * ROWS / 32; ++s) mbar_init(pair_bar + 8 * s, 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) {
@@ -223,17 +264,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
       const uint32_t o_col = lanes + C::O_COL + x * P + half * (P / 2);
       const int group = a.pl.group, d = a.c.d;
-      // A value of each of a row's threads to the other; false: a wait ran out.
+      // A value of each of a row's threads to the other, as a word with the exchange's number beside it; two places in turn,
+      // since the other may be one exchange ahead.  false: the wait ran out.
       uint32_t swaps = 0;
+      const uint32_t swap_at = smem_u32(swapped) + (x * ROWS + r) * 8;
       auto swap = [&](float mine, float& other) {
-        const uint32_t bar = pair_bar + 8 * (4 * x + (warp & 3)), side = swaps & 1u;
-        swapped[side][half][x * ROWS + r] = mine;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
-        if (!wait.all(bar, side)) return false;
-        other = swapped[side][half ^ 1][x * ROWS + r];
         ++swaps;
-        return true;
+        const uint32_t to = swap_at + ((swaps & 1u) * 2 + half) * (2 * ROWS * 8), from = swap_at + ((swaps & 1u) * 2 + (half ^ 1)) * (2 * ROWS * 8);
+        asm volatile("st.volatile.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(__float_as_uint(mine)), "r"(swaps) : "memory");
+        return poll_swap(from, swaps, other, wait);
       };
       constexpr int QC = P / 16;                     // 16-byte chunks of half a query
       constexpr bool AHEAD = P <= 128;               // it is fetched ahead (32 registers) while a result leaves
@@ -315,24 +354,27 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           const uint32_t s_col = lanes + C::S_COL + sb * TN + half * CW;
           const float4* sc = scales[it % SCALE_SLOTS] + half * (BLOCKS / 2);
           const bool whole = CW - 1 <= all_to && 0 >= all_from;
-          // exponents of the 16 positions of block b from their scores
-          auto exponents = [&](uint32_t (&u)[16], const float4& s, int b, float reference) {
+          // exponents of 32 positions from their scores, and the largest
+          auto exponents = [&](uint32_t (&u)[32], int c, float reference) {
             float2* z2 = reinterpret_cast<float2*>(u);
-            const float k = row_scale * s.x, o = s.y - reference;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z2[e] = __ffma2_rn(z2[e], make_float2(k, k), make_float2(o, o));
+            for (int b = 0; b < 2; ++b) {
+              const float2 s = *reinterpret_cast<const float2*>(&sc[2 * c + b]);
+              const float k = row_scale * s.x, o = s.y - reference;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) z2[8 * b + e] = __ffma2_rn(z2[8 * b + e], make_float2(k, k), make_float2(o, o));
+            }
             if (!whole) {
-              const int last = here - 16 * b, first = a.window > 0 ? here - a.window + 1 - 16 * b : 0;
+              const int last = here - 32 * c, first = a.window > 0 ? here - a.window + 1 - 32 * c : 0;
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
+              for (int e = 0; e < 32; ++e)
                 if (e > last || e < first) u[e] = 0xff800000u;
             }
-          };
-          auto largest = [](const uint32_t (&u)[16]) {
             const float* f = reinterpret_cast<const float*>(u);
-            const float a = max3(f[0], f[1], f[2]), b = max3(f[3], f[4], f[5]), c = max3(f[6], f[7], f[8]), d = max3(f[9], f[10], f[11]),
-                        e = max3(f[12], f[13], f[14]);
-            return fmaxf(max3(a, b, f[15]), max3(c, d, e));
+            float tops[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tops[i] = max3(max3(f[i], f[4 + i], f[8 + i]), max3(f[12 + i], f[16 + i], f[20 + i]), fmaxf(f[24 + i], f[28 + i]));
+            return fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
           };
           auto scale_weights = [&](uint32_t col, int n, float f) {   // those of this step that are there, n columns of them
             const __half2 f2 = __float2half2_rn(f);
@@ -374,12 +416,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           if (__any_sync(0xffffffffu, empty)) {          // rows that have seen nothing: their reference is the first maximum
             float most = -INFINITY, other;
 #pragma unroll 1
-            for (int b = 0; b < CW / 16; ++b) {
-              uint32_t z[16];
-              tc_ld16(s_col + 16 * b, z);
-              tc_ld16_wait(z);
-              exponents(z, sc[b], b, ref);
-              most = fmaxf(most, largest(z));
+            for (int c = 0; c < CW / 32; ++c) {
+              uint32_t z[32];
+              tc_ld32(s_col + 32 * c, z);
+              tc_ld32_wait(z);
+              most = fmaxf(most, exponents(z, c, ref));
             }
             ok = swap(most, other);
             if (!ok) break;
@@ -388,43 +429,43 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
               empty = false;
             }
           }
-          // ---- weights, in the order of the values' operand, over the scores that they come from, block by block.  `up`: how
-          // far a weight that fp16 would not hold has raised the thread's reference in this step.
+          // ---- weights, in the order of the values' operand, over the scores that they come from, 32 at a time.  `up`: how
+          // far a weight that fp16 would not hold has raised the thread's reference in this step.  (Loads from tensor memory
+          // that follow stores take as long as these, some 300 cycles; the first weights leave after the last load.)
           float up = 0.0f, peak = -INFINITY, add = 0.0f;
-          uint32_t z[2][16];
-          tc_ld16(s_col, z[0]);
-          tc_ld16_wait(z[0]);
+          uint32_t w[16];
 #pragma unroll
-          for (int b = 0; b < CW / 16; ++b) {
-            uint32_t(&u)[16] = z[b & 1];
-            if (b + 1 < CW / 16) tc_ld16(s_col + 16 * (b + 1), z[(b + 1) & 1]);
-            const float4 s = sc[b];
-            exponents(u, s, b, ref + up);
-            const float top = largest(u);
+          for (int c = 0; c < CW / 32; ++c) {
+            uint32_t u[32];
+            tc_ld32(s_col + 32 * c, u);
+            tc_ld32_wait(u);
+            if (c > 0) tc_st16(s_col + 16 * (c - 1), w);
+            const float top = exponents(u, c, ref + up);
             peak = fmaxf(peak, top + up);
             if (__any_sync(0xffffffffu, top > HARD_LIMIT)) {
               const float by = top > HARD_LIMIT ? top : 0.0f, f = exp2_fast(-by);
-              scale_weights(s_col, 8 * b, f);
+              scale_weights(s_col, 16 * c, f);
               add *= f;
               up += by;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - by);
+              for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - by);
             }
             float2* y = reinterpret_cast<float2*>(u);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = make_float2(exp2_fast(y[e].x), exp2_fast(y[e].y));
-            const float2 t = __fadd2_rn(__fadd2_rn(__fadd2_rn(y[0], y[1]), __fadd2_rn(y[2], y[3])),
-                                        __fadd2_rn(__fadd2_rn(y[4], y[5]), __fadd2_rn(y[6], y[7])));
-            add = fmaf(t.x + t.y, s.z, add);
-            uint32_t w[8];
+            for (int e = 0; e < 16; ++e) y[e] = make_float2(exp2_fast(y[e].x), exp2_fast(y[e].y));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              w[2 * e] = pack_f16(y[e].x, y[e].y);
-              w[2 * e + 1] = pack_f16(y[4 + e].x, y[4 + e].y);
+            for (int b = 0; b < 2; ++b, y += 8) {
+              const float2 t = __fadd2_rn(__fadd2_rn(__fadd2_rn(y[0], y[1]), __fadd2_rn(y[2], y[3])),
+                                          __fadd2_rn(__fadd2_rn(y[4], y[5]), __fadd2_rn(y[6], y[7])));
+              add = fmaf(t.x + t.y, sc[2 * c + b].z, add);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                w[8 * b + 2 * e] = pack_f16(y[e].x, y[e].y);
+                w[8 * b + 2 * e + 1] = pack_f16(y[4 + e].x, y[4 + e].y);
+              }
             }
-            if (b + 1 < CW / 16) tc_ld16_wait(z[(b + 1) & 1]);
-            tc_st8(s_col + 8 * b, w);
           }
+          tc_st16(s_col + CW / 2 - 16, w);
           float other;
           ok = swap(peak, other);
           if (!ok) break;
@@ -671,7 +712,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           }
           for (int x = 0; x < TRACKS; ++x) {
             const int sb = TRACKS == 2 ? x : (int)(it & 1u);
-            ok = wait.all(w_full + 8 * sb, TRACKS == 2 ? it & 1u : it >> 1 & 1u) && wait.all(v_full + 8 * s, it / STAGES & 1u);
+            // (what is there long before the weights is waited for before them)
+            if (x == 0) {
+              ok = wait.all(v_full + 8 * s, it / STAGES & 1u);
+              if (ok && TRACKS == 2 && j + 1 < steps) ok = wait.all(k_full + 8 * ((it + 1) % STAGES), (it + 1) / STAGES & 1u);
+            }
+            ok = ok && wait.all(w_full + 8 * sb, TRACKS == 2 ? it & 1u : it >> 1 & 1u);
             if (!ok) break;
             tc_fence_after();
             const uint64_t vd = make_kmajor_sw128_desc(v_at + s * C::T_BYTES);
@@ -685,9 +731,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             }
             __syncwarp();
             if (TRACKS == 2 && j + 1 < steps) {
-              if (x == 0) ok = wait.all(k_full + 8 * ((it + 1) % STAGES), (it + 1) / STAGES & 1u);
-              if (!ok) break;
-              tc_fence_after();
               scores(it + 1, x);
             }
           }

@@ -43,7 +43,8 @@ struct Cfg {
   static constexpr int BLOCKS = TN / CBLOCK;
   static constexpr int Q_BYTES = ROWS * P * 2;       // a track's
   static constexpr int T_BYTES = TN * P * 2;         // expanded keys or values of a step
-  static constexpr int SMEM = TRACKS * Q_BYTES + 2 * STAGES * T_BYTES + 1024;
+  static constexpr int TILES_BYTES = TRACKS * Q_BYTES + 2 * STAGES * T_BYTES;
+  static constexpr int SMEM = TILES_BYTES + (P == 64 ? SOFT_WARPS * 4096 : 0) + 1024;
   // score buffers: one a track, or two of the only one
   static constexpr int S_COL = 0, O_COL = 2 * TN;
   static_assert(O_COL + TRACKS * P <= 512, "tensor memory");
@@ -274,51 +275,72 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         asm volatile("st.volatile.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(__float_as_uint(mine)), "r"(swaps) : "memory");
         return poll_swap(from, swaps, other, wait);
       };
-      constexpr int QC = P / 16;                     // 16-byte chunks of half a query
-      constexpr bool AHEAD = P <= 128;               // it is fetched ahead (32 registers) while a result leaves
-      uint4 raw[AHEAD ? QC : 1];
-      auto chunk = [&](const PieceJob& p, int c) {
-        const int pr = p.row0 + x * ROWS + r, at = half * QC + c;
-        const bf16* src = a.q + (long long)(p.first_row + pr / group) * a.q_row + (p.head * group + pr % group) * a.q_head;
-        return pr < p.packed && 8 * at < d ? __ldg(reinterpret_cast<const uint4*>(src) + at) : make_uint4(0, 0, 0, 0);
+      // Queries come and results go by warps, a row's 16-byte chunks in neighbouring lanes: a row a lane would touch 32 lines
+      // at a time.  Half a row is QC chunks; instruction i takes rows RI i + lane / QL, QL lanes to a row.
+      constexpr int QC = P / 16, QL = QC & (QC - 1) ? 4 : QC <= 8 ? QC : 8, RI = 32 / QL, QN = QC / QL;   // QN: chunks of a lane
+      constexpr bool AHEAD = P <= 128;               // queries are fetched ahead (32 registers) while a result leaves
+      uint4 raw[AHEAD ? QL : 1];
+      // (row, head) of this lane's row of the piece as one number: -1 where it has none
+      auto place_of = [&](const PieceJob& p) {
+        const int pr = p.row0 + x * ROWS + r;
+        return pr < p.packed ? (long long)(p.first_row + pr / group) << 32 | (uint32_t)(p.head * group + pr % group) : -1LL;
       };
-      auto fetch_query = [&](const PieceJob& p) {
+      auto chunk = [&](long long place, int at) {    // chunk `at` of the row at `place`
+        const bf16* src = a.q + (place >> 32) * a.q_row + (uint32_t)place * a.q_head;
+        return place >= 0 && 8 * at < d ? __ldg(reinterpret_cast<const uint4*>(src) + at) : make_uint4(0, 0, 0, 0);
+      };
+      auto fetch_query = [&](long long place) {
         if (AHEAD) {
 #pragma unroll
-          for (int c = 0; c < QC; ++c) raw[AHEAD ? c : 0] = chunk(p, c);
+          for (int i = 0; i < QL; ++i)
+            raw[AHEAD ? i : 0] = chunk(__shfl_sync(0xffffffffu, place, RI * i + lane / QL), half * QC + lane % QL);
         }
       };
-      // The row's query: times a power of two, as fp16, into its operand tile; `factor` takes scores to base-2 exponents.
-      auto place_query = [&](const PieceJob& p, float& factor) {
-        float top = 0.0f, other;
-#pragma unroll (AHEAD ? 8 : 4)
-        for (int c = 0; c < QC; ++c) {
-          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, c);
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+      // The rows' queries: each times a power of two, as fp16, into the operand tile; `factor` takes a row's scores to base-2
+      // exponents.
+      auto place_query = [&](long long place, float& factor) {
+        float top = 0.0f, other;                     // of this lane's row
+#pragma unroll(AHEAD ? 8 : 2)
+        for (int i = 0; i < QL; ++i) {
+          float t = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = bf16x2_to_float2(w[e]);
-            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-            if (!(isfinite(f.x) && isfinite(f.y))) top = INFINITY;
+          for (int c = 0; c < QN; ++c) {
+            const uint4 q = AHEAD ? raw[AHEAD ? i : 0]
+                                  : chunk(__shfl_sync(0xffffffffu, place, RI * i + lane / QL), half * QC + c * QL + lane % QL);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = bf16x2_to_float2(w[e]);
+              t = fmaxf(t, isfinite(f.x) && isfinite(f.y) ? fmaxf(fabsf(f.x), fabsf(f.y)) : INFINITY);
+            }
           }
+#pragma unroll
+          for (int o = 1; o < QL; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+          t = __shfl_sync(0xffffffffu, t, lane % RI * QL);
+          if (lane / RI == i) top = t;
         }
         if (!swap(top, other)) return false;
         top = fmaxf(top, other);
         float inv;
         const float up = pow2_scale_for(top, &inv);
-        uint8_t* dst = tiles_at + x * C::Q_BYTES + r * 128;
-#pragma unroll (AHEAD ? 8 : 4)
-        for (int c = 0; c < QC; ++c) {
-          const uint4 q = AHEAD ? raw[AHEAD ? c : 0] : chunk(p, c);
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-          uint32_t h[4];
+#pragma unroll(AHEAD ? 8 : 2)
+        for (int i = 0; i < QL; ++i) {
+          const int row = RI * i + lane / QL, tile_row = (warp & 3) * 32 + row;
+          const float by = __shfl_sync(0xffffffffu, up, row);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 f = bf16x2_to_float2(w[e]);
-            h[e] = pack_f16(f.x * up, f.y * up);
+          for (int c = 0; c < QN; ++c) {
+            const int at = half * QC + c * QL + lane % QL;
+            const uint4 q = AHEAD ? raw[AHEAD ? i : 0] : chunk(__shfl_sync(0xffffffffu, place, row), at);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = bf16x2_to_float2(w[e]);
+              h[e] = pack_f16(f.x * by, f.y * by);
+            }
+            *reinterpret_cast<uint4*>(tiles_at + x * C::Q_BYTES + at / 8 * (ROWS * 128) + tile_row * 128 + (((at & 7) ^ (tile_row & 7)) << 4)) =
+                make_uint4(h[0], h[1], h[2], h[3]);
           }
-          const int at = half * QC + c;
-          *reinterpret_cast<uint4*>(dst + at / 8 * (ROWS * 128) + (((at & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
         }
         fence_async();
         __syncwarp();
@@ -331,9 +353,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       bool ok = take(0, pc);
       uint32_t it = 0;                               // steps so far
       float row_scale = 0.0f;
+      long long place = -1;
       if (ok && pc.steps > 0) {
-        fetch_query(pc);
-        ok = place_query(pc, row_scale);
+        place = place_of(pc);
+        fetch_query(place);
+        ok = place_query(place, row_scale);
       }
       for (uint32_t n = 1; ok && pc.steps > 0; ++n) {
         // position of the row within the thread's part of the piece's first step, and what every row of the track sees: up
@@ -353,7 +377,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           tc_fence_after();
           const uint32_t s_col = lanes + C::S_COL + sb * TN + half * CW;
           const float4* sc = scales[it % SCALE_SLOTS] + half * (BLOCKS / 2);
-          const bool whole = CW - 1 <= all_to && 0 >= all_from;
           // exponents of 32 positions from their scores, and the largest
           auto exponents = [&](uint32_t (&u)[32], int c, float reference) {
             float2* z2 = reinterpret_cast<float2*>(u);
@@ -364,11 +387,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
               for (int e = 0; e < 8; ++e) z2[8 * b + e] = __ffma2_rn(z2[8 * b + e], make_float2(k, k), make_float2(o, o));
             }
-            if (!whole) {
-              const int last = here - 32 * c, first = a.window > 0 ? here - a.window + 1 - 32 * c : 0;
+            if (!(32 * c + 31 <= all_to && 32 * c >= all_from)) {
+              // bits of the positions that are seen: first <= e <= last
+              const int last = here - 32 * c, first = a.window > 0 ? last - a.window + 1 : 0;
+              const uint32_t to = last < 0 ? 0u : last >= 31 ? 0xffffffffu : (2u << last) - 1u;
+              const uint32_t from = first <= 0 ? 0xffffffffu : first > 31 ? 0u : 0xffffffffu << first;
+              const uint32_t seen = to & from;
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (e > last || e < first) u[e] = 0xff800000u;
+              for (int e = 0; e < 32; ++e) u[e] = seen >> e & 1u ? u[e] : 0xff800000u;
             }
             const float* f = reinterpret_cast<const float*>(u);
             float tops[4];
@@ -413,22 +439,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             ref += raise;
             l *= f;
           }
-          if (__any_sync(0xffffffffu, empty)) {          // rows that have seen nothing: their reference is the first maximum
-            float most = -INFINITY, other;
-#pragma unroll 1
-            for (int c = 0; c < CW / 32; ++c) {
-              uint32_t z[32];
-              tc_ld32(s_col + 32 * c, z);
-              tc_ld32_wait(z);
-              most = fmaxf(most, exponents(z, c, ref));
-            }
-            ok = swap(most, other);
-            if (!ok) break;
-            if (empty && fmaxf(most, other) > -INFINITY) {
-              ref = fmaxf(most, other);
-              empty = false;
-            }
-          }
           // ---- weights, in the order of the values' operand, over the scores that they come from, 32 at a time.  `up`: how
           // far a weight that fp16 would not hold has raised the thread's reference in this step.  (Loads from tensor memory
           // that follow stores take as long as these, some 300 cycles; the first weights leave after the last load.)
@@ -440,7 +450,20 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             tc_ld32(s_col + 32 * c, u);
             tc_ld32_wait(u);
             if (c > 0) tc_st16(s_col + 16 * (c - 1), w);
-            const float top = exponents(u, c, ref + up);
+            float top = exponents(u, c, ref + up);
+            if (__any_sync(0xffffffffu, empty)) {      // rows that have seen nothing: their reference is the first maximum
+              float other;
+              ok = swap(top, other);
+              if (!ok) break;
+              const float most = fmaxf(top, other);
+              if (empty && most > -INFINITY) {
+                empty = false;
+                ref = most;
+                top -= most;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - most);
+              }
+            }
             peak = fmaxf(peak, top + up);
             if (__any_sync(0xffffffffu, top > HARD_LIMIT)) {
               const float by = top > HARD_LIMIT ? top : 0.0f, f = exp2_fast(-by);
@@ -465,6 +488,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
               }
             }
           }
+          if (!ok) break;
           tc_st16(s_col + CW / 2 - 16, w);
           float other;
           ok = swap(peak, other);
@@ -501,46 +525,65 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         PieceJob next;
         ok = take(n, next);
         if (!ok) break;
-        fetch_query(next);                           // (nothing where there is none: its rows are 0)
+        const long long next_place = place_of(next);
+        fetch_query(next_place);                     // (nothing where there is none: its rows are 0)
         float other;
         ok = swap(l, other) && wait.all(o_full + 8 * x, (it - 1) & 1u);
         if (!ok) break;
         l = half == 0 ? l + other : other + l;       // (one order for both)
         tc_fence_after();
-        const int pr = pc.row0 + x * ROWS + r;
-        const bool mine = pr < pc.packed, complete = pc.part < 0;
-        const float inv = !complete ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-        const long long row = pc.first_row + pr / group;
-        const int head = pc.head * group + pr % group;
+        const bool complete = pc.part < 0;
         const long long slot = (long long)pc.part * TILE + x * ROWS + r;
-        bf16* const out = a.out + row * a.out_row + head * a.out_head;
+        // by way of shared memory, 32 columns of the warp's rows at a time: where the warp puts queries (nothing reads them
+        // now), or beside them where they take too little room
+        const float inv = !complete ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+        uint8_t* const stage = tiles_at + (warp & 3) * 4096 + (P == 64 ? C::TILES_BYTES + (2 * x + half) * 16384 : x * C::Q_BYTES + half * (P / 64 - 1) * 16384);
 #pragma unroll 1
-        for (int i = 0; i < P / 2; i += 16) {
-          uint32_t o[16];
-          tc_ld16(o_col + i, o);
-          tc_ld16_wait(o);
+        for (int i = 0; i < P / 2; i += 32) {
+          uint32_t o[32];
+          tc_ld32(o_col + i, o);
+          tc_ld32_wait(o);
           const int c = half * (P / 2) + i;
-          if (!mine || c >= d) continue;             // (head_dim is a multiple of 16)
+          if (c >= d) continue;
           const float* f = reinterpret_cast<const float*>(o);
+          __syncwarp();
           if (complete) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-              *reinterpret_cast<uint4*>(out + c + 8 * k) =
+            for (int k = 0; k < 4; ++k)
+              *reinterpret_cast<uint4*>(stage + lane * 64 + ((k ^ (lane >> 1 & 3)) << 4)) =
                   make_uint4(float2_to_bf16x2(f[8 * k] * inv, f[8 * k + 1] * inv), float2_to_bf16x2(f[8 * k + 2] * inv, f[8 * k + 3] * inv),
                              float2_to_bf16x2(f[8 * k + 4] * inv, f[8 * k + 5] * inv), float2_to_bf16x2(f[8 * k + 6] * inv, f[8 * k + 7] * inv));
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {            // eight rows at a time, four lanes each
+              const int row = 8 * k + lane / 4, col = c + 8 * (lane & 3);
+              const long long at = __shfl_sync(0xffffffffu, place, row);
+              const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + (((lane & 3) ^ (row >> 1 & 3)) << 4));
+              if (at >= 0 && col < d) *reinterpret_cast<uint4*>(a.out + (at >> 32) * a.out_row + (uint32_t)at * a.out_head + col) = v;
+            }
           } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              *reinterpret_cast<float4*>(a.part + slot * P + c + 4 * k) = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+            for (int k = 0; k < 8; ++k)
+              *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {            // four rows at a time, eight lanes each
+              const int row = 4 * k + lane / 8, col = c + 4 * (lane & 7);
+              const float4 v = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+              if (__shfl_sync(0xffffffffu, place, row) >= 0 && col < d)
+                *reinterpret_cast<float4*>(a.part + (slot - r + (warp & 3) * 32 + row) * P + col) = v;
+            }
           }
         }
         tc_fence_before();
         const float top = empty ? -INFINITY : ref;
-        if (mine && half == 0) {
+        if (place >= 0 && half == 0) {
           if (!complete) a.part_ml[slot] = make_float2(top, l);
-          else if (a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : top * LN2 + logf(l);
+          else if (a.lse) a.lse[(place >> 32) * (a.c.heads * group) + (uint32_t)place] = l == 0.0f ? -INFINITY : top * LN2 + logf(l);
         }
-        if (next.steps > 0) ok = place_query(next, row_scale);
+        place = next_place;
+        __syncwarp();                                // (the staged rows are read before queries go over them)
+        if (next.steps > 0) ok = place_query(place, row_scale);
         pc = next;
       }
     }

@@ -21,7 +21,7 @@ struct CacheView {
   uint8_t* codes;
   float2* scale;
   int n_pages, heads, d, p;          // p = d rounded up to 64
-  int page_shift, bpp;               // log2(page_size), blocks of a page
+  int bpp, bpp_shift;                // blocks of a page, log2 of that
   int block_bytes;                   // 32 p
 };
 // The rows of a call, as the device sees them.
@@ -49,12 +49,12 @@ __device__ __forceinline__ long long first_position(const PlanView& pl, int requ
 }
 // Index of block `b` (16 b = its first position) of a request and head 0; -1 for a page that does not exist.
 __device__ __forceinline__ long long block_index(const CacheView& c, const PlanView& pl, int request, int b, int* status) {
-  const int page = pl.tables[(long long)request * pl.max_pages + b / c.bpp];
+  const int page = pl.tables[(long long)request * pl.max_pages + (b >> c.bpp_shift)];
   if ((unsigned)page >= (unsigned)c.n_pages) {
     raise_status(status, ADMMQ_ERR_SHAPE);
     return -1;
   }
-  return (long long)page * c.heads * c.bpp + b % c.bpp;
+  return (long long)page * c.heads * c.bpp + (b & c.bpp - 1);
 }
 
 // Codes of bytes 0, 1 (HIGH: 2, 3) of a word as two fp16 numbers.
@@ -99,7 +99,8 @@ struct AttendArgs {
   float2* part_ml;                   // [ctas][2][rows]: maximum (base 2) and sum
   int4* joins;                       // [ctas]: (tile, head, last CTA, -), tile -1: nothing
 };
-constexpr int FEW_CTAS = 2;          // of an SM
+// CTAs of an SM that run attention of a few rows
+__host__ __device__ constexpr int few_ctas(int p) { return p <= 128 ? 3 : p <= 192 ? 2 : 1; }
 __host__ __device__ constexpr int many_rows(int p) { return p <= 128 ? MANY_ROWS : MANY_ROWS / 2; }
 cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_cache_attend_many(const AttendArgs& a, cudaStream_t stream);

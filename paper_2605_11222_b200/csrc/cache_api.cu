@@ -29,7 +29,7 @@ admmq_status view_cache(const admmq_cache* c, CacheView* v) {
   if (!aligned(c->d_codes, 16) || !aligned(c->d_scale, 16)) return ADMMQ_ERR_INVALID_ARG;
   const int p = (c->head_dim + 63) / 64 * 64;
   *v = {(uint8_t*)c->d_codes, (float2*)c->d_scale, c->n_pages, c->kv_heads, c->head_dim, p,
-        log2_of(c->page_size), c->page_size / CBLOCK, 2 * CBLOCK * p};
+        c->page_size / CBLOCK, log2_of(c->page_size / CBLOCK), 2 * CBLOCK * p};
   return ADMMQ_OK;
 }
 
@@ -59,7 +59,7 @@ admmq_status view_plan(const admmq_cache_plan* p, const CacheView& c, PlanView* 
   if (!p || p->struct_size != sizeof(admmq_cache_plan)) return ADMMQ_ERR_INVALID_ARG;
   if (p->n_requests < 1 || p->max_pages < 1 || p->group < 1 || p->n_rows < 0 || p->n_blocks < 0 || p->n_small < 0 || p->n_big < 0)
     return ADMMQ_ERR_SHAPE;
-  const long long capacity = (long long)p->max_pages << c.page_shift;
+  const long long capacity = (long long)p->max_pages * c.bpp * CBLOCK;
   if (capacity > MAX_POSITIONS || p->n_rows > MAX_POSITIONS) return ADMMQ_ERR_SHAPE;
   if (!aligned(p->d_tables, 4) || !aligned(p->d_held, 4) || !aligned(p->d_index, 16)) return ADMMQ_ERR_INVALID_ARG;
   const int* at = p->d_index + round4(p->n_requests + 1);
@@ -95,7 +95,7 @@ admmq_status store(bool write, const admmq_cache* cache, const admmq_cache_plan*
 
 // Workspace of one kind of tiles: for every CTA what is to be joined, and two partial results.
 size_t part_bytes(const CacheView& c, bool many, int sms) {
-  const size_t ctas = (size_t)sms * (many ? 1 : FEW_CTAS), rows = many ? many_rows(c.p) : FEW_ROWS;
+  const size_t ctas = (size_t)sms * (many ? 1 : few_ctas(c.p)), rows = many ? many_rows(c.p) : FEW_ROWS;
   return ctas * (sizeof(int4) + 2 * rows * (c.p * sizeof(float) + sizeof(float2)));
 }
 size_t workspace_of(const CacheView& c, const PlanView& p, int sms) {
@@ -208,7 +208,7 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
   char* at = (char*)d_workspace;
   for (int many = 0; many < 2; ++many) {
     if (!(many ? a.pl.n_big : a.pl.n_small)) continue;
-    const size_t ctas = (size_t)sms * (many ? 1 : FEW_CTAS), rows = many ? many_rows(a.c.p) : FEW_ROWS;
+    const size_t ctas = (size_t)sms * (many ? 1 : few_ctas(a.c.p)), rows = many ? many_rows(a.c.p) : FEW_ROWS;
     a.joins = (int4*)at;
     a.part = (float*)(a.joins + ctas);
     a.part_ml = (float2*)(a.part + ctas * 2 * rows * a.c.p);

@@ -1,23 +1,27 @@
 // Attention of a few rows over the 8-bit cache: one new token of a request, or a few drafted ones.
 //   z_j = scale q . k_j,  out = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m)
 //
-// Bound: reading the cache, once.  A warp takes 32 positions (two blocks) at a time: their codes come straight from memory
-// into registers, in the order of the second operand of m16n8k16 products (16 bytes a lane, 512 a warp and load), and the
-// next 32 positions' are under way while these are worked on.  The 16 rows of the product are the query heads of one key
+// Bound: reading the cache, once.  A warp takes 32 positions (two blocks) at a time.  Their codes come as two bulk copies into
+// a ring of its own in shared memory, in the order of the second operand of m16n8k16 products (16 bytes a lane, 512 a warp
+// and load); two further steps are under way meanwhile, 128 KB an SM (memory's latency times its rate asks for some 45).
+// The 16 rows of the product are the query heads of one key
 // head, of one token or of several; where fewer are in use the product's other rows cost nothing that the memory would not.
 // Codes become fp16 by placing them in the mantissa of 1024 + (code + 128) and subtracting 1152: exact, two instructions
 // for two.  Scales stay out of the products: the key scale multiplies the finished score, and the value scale s_b of a block
-// enters the exponent, w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m'), with m' the running maximum of that
-// exponent: w_j <= 1 whatever the scales are, so that fp16 holds it with 11 bits, and the sum of weights takes w_j / s_b.
+// enters the exponent, w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m'), with m' near the running maximum of that
+// exponent, so that fp16 holds w_j with 11 bits whatever the scales are, and the sum of weights takes w_j / s_b.
 //
 // Work is shared out in equal parts (cache_schedule.cuh); four warps of a CTA take turns through its units, each with a
 // maximum, a sum and an accumulator of its own, joined in shared memory at the end of a piece.
+#include "../../include/admmq_testing.h"
 #include "cache_schedule.cuh"
+#include "linear_tc.cuh"
 
 namespace admmq {
 namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 4;
+constexpr float LIMIT = 12.0f;                       // weights stay below 2^LIMIT: fp16
 constexpr float LN2 = 0.693147180559945309f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
@@ -27,27 +31,50 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 template <int P>
-struct FewShared {
-  Schedule<THREADS> schedule;
-  uint4 q[P / 16][32];                               // first operand: [64 h + 4 s .. of every 16][lane]
-  float row_scale[FEW_ROWS];
-  float m[WARPS][FEW_ROWS], l[WARPS][FEW_ROWS];
-  __align__(16) float o[WARPS][FEW_ROWS][P + 4];
+struct Few {
+  static constexpr int UNIT_BYTES = UNIT * 2 * P;    // codes of a step
+  static constexpr int STAGES = P == 64 ? 4 : P == 256 ? 3 : 2;
+  static constexpr int RING_BYTES = WARPS * STAGES * UNIT_BYTES;
+  struct Shared {
+    uint4 q[P / 16][32];                             // first operand: [64 h + 4 s .. of every 16][lane]
+    Schedule<THREADS> schedule;
+    float row_scale[FEW_ROWS];
+    float m[WARPS][FEW_ROWS], l[WARPS][FEW_ROWS];
+    int abort;
+    uint64_t full[WARPS][STAGES];                    // a step's codes are there
+  };
+  static constexpr int O_ROW = P + 4;                // the warps' sums, [warp][row], over the rings once they are done
+  static_assert(WARPS * FEW_ROWS * O_ROW * 4 <= RING_BYTES, "the sums lie over the rings");
+  static constexpr int SMEM = RING_BYTES + (int)sizeof(Shared);
+  static_assert((SMEM + 1024) * few_ctas(P) <= 228 * 1024, "shared memory");
 };
 
-// 32 positions from `first`: two blocks' codes, and their scales.
-template <int P>
-struct Fetched {
-  uint4 k[2][P / 32], v[2][P / 32];
-  float2 s[2];
+struct FewArgs {
+  AttendArgs a;
+  long long wait_limit;
+  int hold_loads;
 };
 
 template <int P>
-__global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const __grid_constant__ FewArgs A) {
+  using F = Few<P>;
+  const AttendArgs& a = A.a;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  FewShared<P>& sh = *reinterpret_cast<FewShared<P>*>(smem_raw);
+  typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(smem_raw + F::RING_BYTES);
+  float* const sums = reinterpret_cast<float*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int group = a.pl.group, heads = a.c.heads, d = a.c.d;
+  uint8_t* const ring = smem_raw + warp * F::STAGES * F::UNIT_BYTES;
+  const uint32_t ring_at = smem_u32(ring), full = smem_u32(&sh.full[warp][0]);
+  if (lane == 0) {
+    for (int i = 0; i < F::STAGES; ++i) mbar_init(full + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  if (tid == 0) sh.abort = 0;                        // (before the barriers of the schedule)
+  const WarpWait wait = {&sh.abort, a.status, A.wait_limit};
+  bool dead = false;                                 // a wait of this warp has run out: it does no more
+  uint32_t issued = 0, taken = 0;                    // steps of this warp so far
   pdl_launch();
   pdl_wait();
 
@@ -111,48 +138,73 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
     float o[P / 8][4];
 #pragma unroll
     for (int i = 0; i < P / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+    float m0 = 0.0f, m1 = 0.0f, l0 = 0.0f, l1 = 0.0f;
+    int empty = 3;                                   // bits: rows g, g + 8 have seen nothing so far
 
     const int unit0 = (int)(u - pc.begin) + pc.span.lo / UNIT, unit1 = (int)(stop - pc.begin) + pc.span.lo / UNIT;
     const int n_blocks = (pc.span.hi + CBLOCK - 1) / CBLOCK;
-    // places of a unit's two blocks; -1: none there
-    auto places = [&](int unit, long long (&at)[2]) {
+    // pages of a step's two blocks; -1: none there
+    struct Pages {
+      int p[2];
+    };
+    auto look = [&](int unit) {
+      Pages n = {{-1, -1}};
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int blk = 2 * unit + b;
-        at[b] = -1;
-        if (unit < unit1 && blk < n_blocks) {
-          const long long i = block_index(a.c, a.pl, pc.job.x, blk, a.status);
-          if (i >= 0) at[b] = i + (long long)pc.head * a.c.bpp;
+        if (unit < unit1 && blk < n_blocks) n.p[b] = a.pl.tables[(long long)pc.job.x * a.pl.max_pages + (blk >> a.c.bpp_shift)];
+      }
+      return n;
+    };
+    // A step under way: its blocks' scales, and whether they exist.
+    struct Step {
+      float2 s[2];
+      bool exists[2];
+    };
+    auto fetch = [&](int unit, const Pages& n) {
+      Step f;
+      int at[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int blk = 2 * unit + b;
+        f.exists[b] = (unsigned)n.p[b] < (unsigned)a.c.n_pages;
+        if (!f.exists[b] && unit < unit1 && blk < n_blocks) raise_status(a.status, ADMMQ_ERR_SHAPE);
+        at[b] = f.exists[b] ? (n.p[b] * heads + pc.head) * a.c.bpp + (blk & a.c.bpp - 1) : 0;
+        f.s[b] = f.exists[b] ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
+      }
+      if (unit < unit1) {
+        if (lane == 0 && !A.hold_loads) {
+          const uint32_t stage = issued % F::STAGES, bar = full + 8 * stage, dst = ring_at + stage * F::UNIT_BYTES;
+          const int bytes = (f.exists[0] ? F::UNIT_BYTES / 2 : 0) + (f.exists[1] ? F::UNIT_BYTES / 2 : 0);
+          if (bytes) mbar_expect_tx(bar, bytes);
+          else mbar_arrive(bar);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            if (f.exists[b])
+              bulk_load(dst + b * (F::UNIT_BYTES / 2), a.c.codes + (size_t)(uint32_t)at[b] * (uint32_t)a.c.block_bytes, F::UNIT_BYTES / 2, bar);
         }
+        ++issued;
       }
-    };
-    auto fetch_k = [&](Fetched<P>& f, const long long (&at)[2]) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        f.s[b] = at[b] >= 0 ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
-        const uint8_t* p = a.c.codes + at[b] * a.c.block_bytes + lane * 16;
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) f.k[b][i] = at[b] >= 0 ? ldg_stream(p + i * 512) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    auto fetch_v = [&](Fetched<P>& f, const long long (&at)[2]) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint8_t* p = a.c.codes + at[b] * a.c.block_bytes + 16 * P + lane * 16;
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) f.v[b][i] = at[b] >= 0 ? ldg_stream(p + i * 512) : make_uint4(0, 0, 0, 0);
-      }
+      return f;
     };
 
-    Fetched<P> f;
-    long long at[2], next[2];
-    int unit = unit0 + warp;
-    places(unit, at);
-    fetch_k(f, at);
-    fetch_v(f, at);
-    places(unit + WARPS, next);
+    // the steps under way, in their order, and the pages of the one after
+    Step ahead[F::STAGES];
+    int unit = dead ? unit1 : unit0 + warp;
+    {
+      Pages n[F::STAGES];
+#pragma unroll
+      for (int i = 0; i < F::STAGES; ++i) n[i] = look(unit + i * WARPS);
+#pragma unroll
+      for (int i = 0; i < F::STAGES; ++i) ahead[i] = fetch(unit + i * WARPS, n[i]);
+    }
+    Pages next = look(unit + F::STAGES * WARPS);
     for (; unit < unit1; unit += WARPS) {
+      const uint32_t stage = taken % F::STAGES;
+      dead = !wait.all(full + 8 * stage, taken / F::STAGES & 1u);
+      if (dead) break;
+      ++taken;
+      const uint8_t* codes = ring + stage * F::UNIT_BYTES + lane * 16;
       // ---- scores of the 32 positions
       float z[2][2][4];
 #pragma unroll
@@ -160,7 +212,12 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
 #pragma unroll
         for (int j = 0; j < 2; ++j) z[b][j][0] = z[b][j][1] = z[b][j][2] = z[b][j][3] = 0.0f;
 #pragma unroll
-      for (int h = 0; h < P / 64; ++h)
+      for (int h = 0; h < P / 64; ++h) {
+        uint4 k[2][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) k[b][j] = *reinterpret_cast<const uint4*>(codes + b * (F::UNIT_BYTES / 2) + (2 * h + j) * 512);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const uint4 q = sh.q[h * 4 + s][lane];
@@ -168,30 +225,29 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
           for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const uint4& w = f.k[b][2 * h + j];
+              const uint4& w = k[b][j];
               const uint32_t c = s == 0 ? w.x : s == 1 ? w.y : s == 2 ? w.z : w.w;
               mma_f16(z[b][j], q, two_codes<false>(c), two_codes<true>(c));
             }
         }
-      const float2 sc[2] = {f.s[0], f.s[1]};
-      const bool exists[2] = {at[0] >= 0, at[1] >= 0};
-      at[0] = next[0];
-      at[1] = next[1];
-      fetch_k(f, at);
+      }
+      const float2 sc[2] = {ahead[0].s[0], ahead[0].s[1]};
+      const bool exists[2] = {ahead[0].exists[0], ahead[0].exists[1]};
       // ---- exponents, base 2
       const int pos = unit * UNIT;
       const bool whole = pos + UNIT - 1 <= first_here && (a.window <= 0 || pos > last_here - a.window) && exists[0] && exists[1];
-      float most0 = -INFINITY, most1 = -INFINITY, inv_s[2];
+      float most0 = -INFINITY, most1 = -INFINITY, inv_s[2];   // of this lane's four positions of a block
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const float vs = sc[b].y == 0.0f ? 1.0f : sc[b].y, lv = __log2f(vs), k0 = f0 * sc[b].x, k1 = f1 * sc[b].x;
-        inv_s[b] = __fdividef(1.0f, vs);
+        // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
+        inv_s[b] = vs == vs ? __fdividef(1.0f, vs) : 1.0f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            z[b][j][e] = fmaf(z[b][j][e], k0, lv);
-            z[b][j][2 + e] = fmaf(z[b][j][2 + e], k1, lv);
+            z[b][j][e] = fmaf(z[b][j][e], k0, lv - m0);
+            z[b][j][2 + e] = fmaf(z[b][j][2 + e], k1, lv - m1);
             if (!whole) {
               const int p = pos + 16 * b + 8 * j + 2 * t + e;
               if (!exists[b] || p > here0 || (a.window > 0 && p <= here0 - a.window)) z[b][j][e] = -INFINITY;
@@ -202,15 +258,22 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
           }
         }
       }
+      // The reference is the row's maximum over the first positions seen; it is raised only where a weight would pass
+      // 2^LIMIT, which is rare.
+      if (__any_sync(0xffffffffu, empty || fmaxf(most0, most1) > LIMIT)) {
 #pragma unroll
-      for (int x = 1; x < 4; x <<= 1) {
-        most0 = fmaxf(most0, __shfl_xor_sync(0xffffffffu, most0, x));
-        most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, x));
-      }
-      most0 = fmaxf(most0, m0);
-      most1 = fmaxf(most1, m1);
-      if (__any_sync(0xffffffffu, most0 > m0 || most1 > m1)) {
-        const float a0 = most0 > m0 ? exp2_fast(m0 - most0) : 1.0f, a1 = most1 > m1 ? exp2_fast(m1 - most1) : 1.0f;
+        for (int x = 1; x < 4; x <<= 1) {
+          most0 = fmaxf(most0, __shfl_xor_sync(0xffffffffu, most0, x));
+          most1 = fmaxf(most1, __shfl_xor_sync(0xffffffffu, most1, x));
+        }
+        const float by0 = (empty & 1 ? most0 > -INFINITY : most0 > LIMIT) ? most0 : 0.0f;
+        const float by1 = (empty & 2 ? most1 > -INFINITY : most1 > LIMIT) ? most1 : 0.0f;
+        // (where nothing was seen yet the sums are 0)
+        const float a0 = empty & 1 ? 0.0f : exp2_fast(-by0), a1 = empty & 2 ? 0.0f : exp2_fast(-by1);
+        if (most0 > -INFINITY) empty &= ~1;
+        if (most1 > -INFINITY) empty &= ~2;
+        m0 += by0;
+        m1 += by1;
         l0 *= a0;
         l1 *= a1;
 #pragma unroll
@@ -220,10 +283,16 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
           o[i][2] *= a1;
           o[i][3] *= a1;
         }
-        m0 = most0;
-        m1 = most1;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              z[b][j][e] -= by0;
+              z[b][j][2 + e] -= by1;
+            }
       }
-      const float r0 = m0 == -INFINITY ? 0.0f : m0, r1 = m1 == -INFINITY ? 0.0f : m1;
       uint4 w[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -232,15 +301,14 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            z[b][j][e] = exp2_fast(z[b][j][e] - r0);
-            z[b][j][2 + e] = exp2_fast(z[b][j][2 + e] - r1);
+            z[b][j][e] = exp2_fast(z[b][j][e]);
+            z[b][j][2 + e] = exp2_fast(z[b][j][2 + e]);
             s0 += z[b][j][e];
             s1 += z[b][j][2 + e];
           }
         }
-        // (a block that the row sees nothing of adds nothing, even with a scale of NaN)
-        l0 = s0 == 0.0f ? l0 : fmaf(s0, inv_s[b], l0);
-        l1 = s1 == 0.0f ? l1 : fmaf(s1, inv_s[b], l1);
+        l0 = fmaf(s0, inv_s[b], l0);
+        l1 = fmaf(s1, inv_s[b], l1);
         w[b] = make_uint4(pack_f16(z[b][0][0], z[b][0][1]), pack_f16(z[b][0][2], z[b][0][3]), pack_f16(z[b][1][0], z[b][1][1]),
                           pack_f16(z[b][1][2], z[b][1][3]));
       }
@@ -249,15 +317,21 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int c = 0; c < P / 32; ++c) {
-          const uint4& x = f.v[b][c];
+          const uint4 x = *reinterpret_cast<const uint4*>(codes + b * (F::UNIT_BYTES / 2) + 16 * P + c * 512);
           mma_f16(o[4 * c], w[b], two_codes<false>(x.x), two_codes<true>(x.x));
           mma_f16(o[4 * c + 1], w[b], two_codes<false>(x.y), two_codes<true>(x.y));
           mma_f16(o[4 * c + 2], w[b], two_codes<false>(x.z), two_codes<true>(x.z));
           mma_f16(o[4 * c + 3], w[b], two_codes<false>(x.w), two_codes<true>(x.w));
         }
-      fetch_v(f, at);
-      places(unit + 2 * WARPS, next);
+      __syncwarp();                                  // (every lane has read the stage)
+#pragma unroll
+      for (int i = 0; i + 1 < F::STAGES; ++i) ahead[i] = ahead[i + 1];
+      ahead[F::STAGES - 1] = fetch(unit + F::STAGES * WARPS, next);
+      next = look(unit + (F::STAGES + 1) * WARPS);
     }
+    if (dead && !A.hold_loads)                       // copies in flight land before the memory is used again
+      for (; taken != issued; ++taken) mbar_wait_quiet(full + 8 * (taken % F::STAGES), taken / F::STAGES & 1u);
+    __syncthreads();                                 // (the sums go over every warp's ring)
 
     // ---- the warps' sums into one
 #pragma unroll
@@ -266,8 +340,8 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
       l1 += __shfl_xor_sync(0xffffffffu, l1, x);
     }
     if (t == 0) {
-      sh.m[warp][g] = m0;
-      sh.m[warp][g + 8] = m1;
+      sh.m[warp][g] = empty & 1 ? -INFINITY : m0;
+      sh.m[warp][g + 8] = empty & 2 ? -INFINITY : m1;
       sh.l[warp][g] = l0;
       sh.l[warp][g + 8] = l1;
     }
@@ -277,7 +351,7 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
       for (int half = 0; half < 2; ++half)           // columns 32 c + 8 t + 4 half + i of rows g and g + 8
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-          *reinterpret_cast<float4*>(&sh.o[warp][g + 8 * r][32 * c + 8 * t + 4 * half]) =
+          *reinterpret_cast<float4*>(sums + (warp * FEW_ROWS + g + 8 * r) * F::O_ROW + 32 * c + 8 * t + 4 * half) =
               make_float4(o[4 * c][2 * r + half], o[4 * c + 1][2 * r + half], o[4 * c + 2][2 * r + half], o[4 * c + 3][2 * r + half]);
     __syncthreads();
     const bool complete = u == pc.begin && stop == pc.end;
@@ -294,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
         const float k = exp2_fast(sh.m[w][r] - ref);
-        const float4 x = *reinterpret_cast<const float4*>(&sh.o[w][r][at4]);
+        const float4 x = *reinterpret_cast<const float4*>(sums + (w * FEW_ROWS + r) * F::O_ROW + at4);
         acc.x = fmaf(x.x, k, acc.x);
         acc.y = fmaf(x.y, k, acc.y);
         acc.z = fmaf(x.z, k, acc.z);
@@ -313,6 +387,7 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
         if (at4 == 0) a.part_ml[slot * FEW_ROWS + r] = make_float2(m, l);
       }
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies go over the sums next)
     __syncthreads();
     u = stop;
   }
@@ -321,19 +396,20 @@ __global__ void __launch_bounds__(THREADS, P <= 128 ? FEW_CTAS : 1) attend_few_k
 
 template <int P>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
-  const cudaError_t e = ensure_dynamic_smem((const void*)attend_few_kernel<P>, (int)sizeof(FewShared<P>));
+  const cudaError_t e = ensure_dynamic_smem((const void*)attend_few_kernel<P>, Few<P>::SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms * FEW_CTAS);
+  cfg.gridDim = dim3(sms * few_ctas(P));
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = sizeof(FewShared<P>);
+  cfg.dynamicSmemBytes = Few<P>::SMEM;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_few_kernel<P>, a);
+  const FewArgs args = {a, g_linear_wait_limit.load(std::memory_order_relaxed), g_linear_hold_loads.load(std::memory_order_relaxed)};
+  return cudaLaunchKernelEx(&cfg, attend_few_kernel<P>, args);
 }
 
 }  // namespace

@@ -123,16 +123,6 @@ __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// Bounded wait of a whole warp with one answer for all its lanes.  (Inlined: setmaxnreg asks for a kernel without calls.)
-struct WarpWait {
-  volatile int* abort_flag;
-  int* status;
-  long long limit;
-  __device__ __forceinline__ bool all(uint32_t bar, uint32_t parity) const {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, limit)) != 0;
-  }
-};
-
 // Waits, within the limit, for the word with the tag.
 __device__ __forceinline__ bool poll_swap(uint32_t from, uint32_t tag, float& value, const WarpWait& wait) {
   uint32_t v, t;
@@ -615,8 +605,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       n.more = true;
       const int b = pc.pos / CBLOCK + lane;
       if (lane < BLOCKS && b < (pc.hi + CBLOCK - 1) / CBLOCK) {
-        n.page = a.pl.tables[(long long)pc.request * a.pl.max_pages + b / a.c.bpp];
-        n.block = b % a.c.bpp;
+        n.page = a.pl.tables[(long long)pc.request * a.pl.max_pages + (b >> a.c.bpp_shift)];
+        n.block = b & a.c.bpp - 1;
         if (n.page < 0) n.page = 0x7fffffff;         // (-1 is "none", not a page that does not exist)
       }
       n.heads_before = pc.head * a.c.bpp;
@@ -812,6 +802,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         }
         __syncwarp();
         if (p.steps == 0) break;
+        // its queries into the L2 cache: fetched when the piece before ends, they would keep the softmax waiting for memory
+        for (int i = lane; n > 0 && i < TILE && p.row0 + i < p.packed; i += 32) {
+          const int pr = p.row0 + i, g = a.pl.group;
+          const bf16* src = a.q + (long long)(p.first_row + pr / g) * a.q_row + (p.head * g + pr % g) * a.q_head;
+          for (int c = 0; c < a.c.d; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + c));
+        }
       }
       if (lane == 0) a.joins[cta] = join;
     }

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Atten
 cudaError_t launch_cache_join(const AttendArgs& a, bool many, int sms, cudaStream_t stream) {
   const int rows = many ? many_rows(a.c.p) : FEW_ROWS, per = many ? MANY_ROWS / rows : 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms * (many ? 1 : FEW_CTAS) - 1, rows / 4);
+  cfg.gridDim = dim3(sms * (many ? 1 : few_ctas(a.c.p)) - 1, rows / 4);
   cfg.blockDim = dim3(128);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];

@@ -9,8 +9,19 @@
 // (tile, head), slot 0 where it goes on with one), and the join kernel adds them up in the order of the CTAs.
 #pragma once
 #include "cache.h"
+#include "tc_ptx.cuh"
 
 namespace admmq {
+
+// Bounded wait of a whole warp with one answer for all its lanes.  (Inlined: setmaxnreg asks for a kernel without calls.)
+struct WarpWait {
+  volatile int* abort_flag;
+  int* status;
+  long long limit;
+  __device__ __forceinline__ bool all(uint32_t bar, uint32_t parity) const {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, limit)) != 0;
+  }
+};
 
 // Positions that the rows of a tile see: [lo, hi); hi = 0 where the request takes no part.
 struct Span {

@@ -53,8 +53,8 @@ size_t admmq_cache_scale_bytes(int n_pages, int kv_heads, int head_dim, int page
 typedef struct {
   size_t struct_size;      /* sizeof(admmq_cache_plan) */
   int n_requests, max_pages, group;
-  int n_blocks;            /* admmq_cache_plan_fill sets these four */
-  int n_small, n_big;
+  int n_blocks;            /* admmq_cache_plan_fill sets these five */
+  int n_small, n_big, small_rows;
   long long n_rows;
   const int* d_tables;     /* [n_requests][max_pages] */
   const int* d_held;       /* [n_requests] */

@@ -33,6 +33,7 @@ struct PlanView {
   const int4* small;                 // tiles of packed rows: (request, first packed row, first row, rows of the request)
   const int4* big;
   int n, max_pages, group, n_blocks, n_small, n_big;
+  int small_rows;                    // most packed rows that a small tile holds
   long long capacity;                // positions of a table
 };
 constexpr int FEW_ROWS = 16, MANY_ROWS = 256;   // packed rows (token, query head) of a tile
@@ -97,11 +98,17 @@ struct AttendArgs {
   // workspace of one kind of tiles: for every CTA two partial results, and what is to be joined
   float* part;                       // [ctas][2][rows][p]
   float2* part_ml;                   // [ctas][2][rows]: maximum (base 2) and sum
-  int4* joins;                       // [ctas]: (tile, head, last CTA, -), tile -1: nothing
+  int4* joins;                       // (tile, head, first CTA, last CTA), the same CTA twice: nothing to join
+  int by_piece;                      // joins go by (tile, head), which are no more than CTAs; or by the first CTA
 };
 // CTAs of an SM that run attention of a few rows
 __host__ __device__ constexpr int few_ctas(int p) { return p <= 128 ? 3 : p <= 192 ? 2 : 1; }
 __host__ __device__ constexpr int many_rows(int p) { return p <= 128 ? MANY_ROWS : MANY_ROWS / 2; }
+// CTAs of either kernel, and (tile, head)s.
+inline int attend_ctas(int p, bool many, int sms) { return sms * (many ? 1 : few_ctas(p)); }
+inline long long pieces_of(const AttendArgs& a, bool many) {
+  return (long long)(many ? a.pl.n_big * (MANY_ROWS / many_rows(a.c.p)) : a.pl.n_small) * a.c.heads;
+}
 cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_cache_attend_many(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_cache_join(const AttendArgs& a, bool many, int sms, cudaStream_t stream);

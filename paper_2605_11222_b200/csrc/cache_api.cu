@@ -1,4 +1,6 @@
 // C entry points of admmq_cache.h: argument checks, the index of a call's rows, kernel selection.
+#include <algorithm>
+
 #include "cache.h"
 
 namespace admmq {
@@ -39,7 +41,7 @@ long long tiles_of(long long packed, int rows) { return (packed + rows - 1) / ro
 bool is_few(long long packed) { return packed <= MOST_FEW; }
 long long round4(long long n) { return (n + 3) & ~3LL; }
 struct IndexSizes {
-  long long rows, blocks, small, big;
+  long long rows, blocks, small, big, small_rows;   // small_rows: most packed rows that a small tile holds
   long long ints(int n) const { return round4(n + 1) + round4(2 * blocks) + 4 * (small + big); }
 };
 bool index_sizes(const long long* lengths, int n, int group, IndexSizes* s) {
@@ -51,13 +53,15 @@ bool index_sizes(const long long* lengths, int n, int group, IndexSizes* s) {
     if (s->rows * group > MAX_POSITIONS) return false;
     s->blocks += blocks_of(lengths[i]);
     const long long packed = lengths[i] * group;
+    if (is_few(packed)) s->small_rows = std::max(s->small_rows, std::min(packed, (long long)FEW_ROWS));
     (is_few(packed) ? s->small : s->big) += tiles_of(packed, is_few(packed) ? FEW_ROWS : MANY_ROWS);
   }
   return s->ints(n) <= 0x7fffffffLL;
 }
 admmq_status view_plan(const admmq_cache_plan* p, const CacheView& c, PlanView* v) {
   if (!p || p->struct_size != sizeof(admmq_cache_plan)) return ADMMQ_ERR_INVALID_ARG;
-  if (p->n_requests < 1 || p->max_pages < 1 || p->group < 1 || p->n_rows < 0 || p->n_blocks < 0 || p->n_small < 0 || p->n_big < 0)
+  if (p->n_requests < 1 || p->max_pages < 1 || p->group < 1 || p->n_rows < 0 || p->n_blocks < 0 || p->n_small < 0 || p->n_big < 0 ||
+      p->small_rows < 0 || p->small_rows > FEW_ROWS)
     return ADMMQ_ERR_SHAPE;
   const long long capacity = (long long)p->max_pages * c.bpp * CBLOCK;
   if (capacity > MAX_POSITIONS || p->n_rows > MAX_POSITIONS) return ADMMQ_ERR_SHAPE;
@@ -65,7 +69,7 @@ admmq_status view_plan(const admmq_cache_plan* p, const CacheView& c, PlanView* 
   const int* at = p->d_index + round4(p->n_requests + 1);
   const int* tiles = at + round4(2LL * p->n_blocks);
   *v = {p->d_tables, p->d_held, p->d_index, (const int2*)at, (const int4*)tiles, (const int4*)tiles + p->n_small,
-        p->n_requests, p->max_pages, p->group, p->n_blocks, p->n_small, p->n_big, capacity};
+        p->n_requests, p->max_pages, p->group, p->n_blocks, p->n_small, p->n_big, p->small_rows, capacity};
   return ADMMQ_OK;
 }
 
@@ -95,7 +99,7 @@ admmq_status store(bool write, const admmq_cache* cache, const admmq_cache_plan*
 
 // Workspace of one kind of tiles: for every CTA what is to be joined, and two partial results.
 size_t part_bytes(const CacheView& c, bool many, int sms) {
-  const size_t ctas = (size_t)sms * (many ? 1 : few_ctas(c.p)), rows = many ? many_rows(c.p) : FEW_ROWS;
+  const size_t ctas = attend_ctas(c.p, many, sms), rows = many ? many_rows(c.p) : FEW_ROWS;
   return ctas * (sizeof(int4) + 2 * rows * (c.p * sizeof(float) + sizeof(float2)));
 }
 size_t workspace_of(const CacheView& c, const PlanView& p, int sms) {
@@ -156,6 +160,7 @@ admmq_status admmq_cache_plan_fill(const long long* lengths, int n_requests, int
   plan->n_blocks = (int)s.blocks;
   plan->n_small = (int)s.small;
   plan->n_big = (int)s.big;
+  plan->small_rows = (int)s.small_rows;
   return ADMMQ_OK;
 }
 
@@ -208,7 +213,8 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
   char* at = (char*)d_workspace;
   for (int many = 0; many < 2; ++many) {
     if (!(many ? a.pl.n_big : a.pl.n_small)) continue;
-    const size_t ctas = (size_t)sms * (many ? 1 : few_ctas(a.c.p)), rows = many ? many_rows(a.c.p) : FEW_ROWS;
+    const size_t ctas = attend_ctas(a.c.p, many, sms), rows = many ? many_rows(a.c.p) : FEW_ROWS;
+    a.by_piece = pieces_of(a, many) <= (long long)ctas;
     a.joins = (int4*)at;
     a.part = (float*)(a.joins + ctas);
     a.part_ml = (float2*)(a.part + ctas * 2 * rows * a.c.p);

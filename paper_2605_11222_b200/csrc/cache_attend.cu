@@ -83,11 +83,11 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
   const long long total = units * heads;
   const int ctas = active_ctas(total, LEAST_UNITS), cta = blockIdx.x;
   if (cta >= ctas) {
-    if (tid == 0) a.joins[cta] = make_int4(-1, 0, 0, 0);
+    if (tid == 0) tell_none(a, cta);
     return;
   }
   const long long line_end = line_at(total, cta + 1, ctas);
-  int4 join = make_int4(-1, 0, 0, 0);
+  bool told = false;                                 // of a (tile, head) that others end
 
   for (long long u = line_at(total, cta, ctas); u < line_end;) {
     const Piece pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
@@ -95,7 +95,10 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
     u = max(u, pc.begin);
     if (u >= stop) break;
     const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
-    if (u == pc.begin && stop < pc.end) join = make_int4(pc.tile, pc.head, cta_of(pc.end - 1, total, ctas), 0);
+    if (u == pc.begin) {
+      told = stop < pc.end;
+      if (tid == 0) tell_join(a, pc.tile, pc.head, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
+    }
 
     // ---- queries: each row times a power of two that brings its largest value to [2^13, 2^14), as fp16
     {
@@ -391,7 +394,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
     __syncthreads();
     u = stop;
   }
-  if (tid == 0) a.joins[cta] = join;
+  if (tid == 0 && !told) tell_none(a, cta);
 }
 
 template <int P>

@@ -773,7 +773,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       const int ctas = active_ctas(total, 1), cta = blockIdx.x;
       long long u = cta < ctas ? line_at(total, cta, ctas) : 0;
       const long long line_end = cta < ctas ? line_at(total, cta + 1, ctas) : 0;
-      int4 join = make_int4(-1, 0, 0, 0);
+      bool told = false;                             // of a (tile, head) that others end
       for (uint32_t n = 0;; ++n) {
         PieceJob p = {};
         if (u < line_end) {
@@ -791,7 +791,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             p.at = f.span.at;
             p.hi = f.span.hi;
             p.part = u == f.begin && stop == f.end ? -1 : 2 * cta + (u == f.begin ? 1 : 0);
-            if (u == f.begin && stop < f.end) join = make_int4(f.tile, f.head, cta_of(f.end - 1, total, ctas), 0);
+            if (u == f.begin) {
+              told = stop < f.end;
+              if (lane == 0) tell_join(a, f.tile, f.head, cta, told ? cta_of(f.end - 1, total, ctas) : cta);
+            }
             u = stop;
           }
         }
@@ -809,7 +812,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           for (int c = 0; c < a.c.d; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + c));
         }
       }
-      if (lane == 0) a.joins[cta] = join;
+      if (lane == 0 && !told) tell_none(a, cta);
     }
   }
   __syncthreads();

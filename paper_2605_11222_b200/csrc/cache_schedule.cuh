@@ -124,6 +124,15 @@ __device__ __forceinline__ int active_ctas(long long total, int least) {
   return (int)(most < (long long)gridDim.x ? most : (long long)gridDim.x);
 }
 __device__ __forceinline__ long long line_at(long long total, int c, int ctas) { return total * c / ctas; }
+// What is to be joined of a (tile, head), told by the CTA that begins it.
+__device__ __forceinline__ void tell_join(const AttendArgs& a, int tile, int head, int first, int last) {
+  if (a.by_piece) a.joins[tile * a.c.heads + head] = make_int4(tile, head, first, last);
+  else if (last > first) a.joins[first] = make_int4(tile, head, first, last);
+}
+// And, where joins go by CTA, by one that begins none which others end.
+__device__ __forceinline__ void tell_none(const AttendArgs& a, int cta) {
+  if (!a.by_piece) a.joins[cta] = make_int4(0, 0, cta, cta);
+}
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
   return (int)(((u + 1) * ctas + total - 1) / total) - 1;
 }

@@ -35,7 +35,7 @@ class _Cache(C.Structure):
 
 class _Plan(C.Structure):
     _fields_ = [("struct_size", C.c_size_t), ("n_requests", C.c_int), ("max_pages", C.c_int), ("group", C.c_int),
-                ("n_blocks", C.c_int), ("n_small", C.c_int), ("n_big", C.c_int), ("n_rows", C.c_longlong),
+                ("n_blocks", C.c_int), ("n_small", C.c_int), ("n_big", C.c_int), ("small_rows", C.c_int), ("n_rows", C.c_longlong),
                 ("d_tables", C.c_void_p), ("d_held", C.c_void_p), ("d_index", C.c_void_p)]
 
 

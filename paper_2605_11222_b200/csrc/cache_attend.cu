@@ -21,6 +21,8 @@ namespace admmq {
 namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 4;
+constexpr int MOST_RANKS = 16;                       // CTAs of a cluster
+constexpr long long CLUSTER_POSITIONS = 1 << 14;     // positions of a table up to which clusters share a (tile, head)
 constexpr float LIMIT = 12.0f;                       // weights stay below 2^LIMIT: fp16
 constexpr float LN2 = 0.693147180559945309f;
 
@@ -30,6 +32,12 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+
 template <int P>
 struct Few {
   static constexpr int UNIT_BYTES = UNIT * 2 * P;    // codes of a step
@@ -44,7 +52,7 @@ struct Few {
     uint64_t full[WARPS][STAGES];                    // a step's codes are there
   };
   static constexpr int O_ROW = P + 4;                // the warps' sums, [warp][row], over the rings once they are done
-  static_assert(WARPS * FEW_ROWS * O_ROW * 4 <= RING_BYTES, "the sums lie over the rings");
+  static_assert(WARPS * FEW_ROWS * O_ROW * 4 + FEW_ROWS * (P * 4 + 8) <= RING_BYTES, "the sums lie over the rings");
   static constexpr int SMEM = RING_BYTES + (int)sizeof(Shared);
   static_assert((SMEM + 1024) * few_ctas(P) <= 228 * 1024, "shared memory");
 };
@@ -55,7 +63,9 @@ struct FewArgs {
   int hold_loads;
 };
 
-template <int P>
+// CLUSTER: the CTAs of a cluster share one (tile, head) and add up over distributed shared memory, so that there is nothing
+// to find first and nothing to join after; for so few (tile, head)s that all their clusters run at once.
+template <int P, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const __grid_constant__ FewArgs A) {
   using F = Few<P>;
   const AttendArgs& a = A.a;
@@ -79,26 +89,49 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
   pdl_wait();
 
   const auto job = [&](int tile) { return __ldg(a.pl.small + tile); };
-  const long long units = make_schedule<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule);
-  const long long total = units * heads;
-  const int ctas = active_ctas(total, LEAST_UNITS), cta = blockIdx.x;
-  if (cta >= ctas) {
-    if (tid == 0) tell_none(a, cta);
-    return;
+  const int cta = blockIdx.x;
+  int ctas = 0, rank = 0, ranks = 1;
+  long long total = 0, u = 0, line_end = 1;
+  if (CLUSTER) {
+    rank = (int)cluster_ctarank();
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    __syncthreads();                                 // (the abort flag)
+  } else {
+    total = make_schedule<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule) * heads;
+    ctas = active_ctas(total, LEAST_UNITS);
+    if (cta >= ctas) {
+      if (tid == 0) tell_none(a, cta);
+      return;
+    }
+    u = line_at(total, cta, ctas);
+    line_end = line_at(total, cta + 1, ctas);
   }
-  const long long line_end = line_at(total, cta + 1, ctas);
   bool told = false;                                 // of a (tile, head) that others end
 
-  for (long long u = line_at(total, cta, ctas); u < line_end;) {
-    const Piece pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
-    const long long stop = min(line_end, pc.end);
-    u = max(u, pc.begin);
-    if (u >= stop) break;
-    const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
-    if (u == pc.begin) {
-      told = stop < pc.end;
-      if (tid == 0) tell_join(a, pc.tile, pc.head, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
+  while (u < line_end) {
+    Piece pc;
+    long long stop;
+    if (CLUSTER) {
+      const int at = cta / ranks;
+      pc.tile = at / heads;
+      pc.head = at - pc.tile * heads;
+      pc.job = job(pc.tile);
+      pc.span = span_of(a, pc.job, FEW_ROWS);
+      pc.begin = 0;
+      pc.end = units_of<UNIT>(pc.span, pc.job, group);
+      u = pc.end * rank / ranks;
+      stop = pc.end * (rank + 1) / ranks;            // (perhaps none)
+    } else {
+      pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
+      stop = min(line_end, pc.end);
+      u = max(u, pc.begin);
+      if (u >= stop) break;
+      if (u == pc.begin) {
+        told = stop < pc.end;
+        if (tid == 0) tell_join(a, pc.tile, pc.head, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
+      }
     }
+    const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
 
     // ---- queries: each row times a power of two that brings its largest value to [2^13, 2^14), as fp16
     {
@@ -357,8 +390,18 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
           *reinterpret_cast<float4*>(sums + (warp * FEW_ROWS + g + 8 * r) * F::O_ROW + 32 * c + 8 * t + 4 * half) =
               make_float4(o[4 * c][2 * r + half], o[4 * c + 1][2 * r + half], o[4 * c + 2][2 * r + half], o[4 * c + 3][2 * r + half]);
     __syncthreads();
-    const bool complete = u == pc.begin && stop == pc.end;
+    const bool complete = !CLUSTER && u == pc.begin && stop == pc.end;
+    float* const shared_o = sums + WARPS * FEW_ROWS * F::O_ROW;              // of a cluster's CTA: its sums, then its maxima
+    float2* const shared_ml = reinterpret_cast<float2*>(shared_o + FEW_ROWS * P);
     const int slot = 2 * cta + (u == pc.begin ? 1 : 0);
+    auto put = [&](int r, int at4, const float4& acc, float m, float l) {    // four values of a finished row
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      const int pr = row0 + r, head = pc.head * group + pr % group;
+      const long long row = pc.job.z + pr / group;
+      *reinterpret_cast<uint2*>(a.out + row * a.out_row + head * a.out_head + at4) =
+          make_uint2(float2_to_bf16x2(acc.x * inv, acc.y * inv), float2_to_bf16x2(acc.z * inv, acc.w * inv));
+      if (at4 == 0 && a.lse) a.lse[row * (heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
+    };
     for (int i = tid; i < FEW_ROWS * P / 4; i += THREADS) {
       const int r = i / (P / 4), at4 = 4 * (i % (P / 4));
       if (r >= nr || at4 >= d) continue;
@@ -378,17 +421,41 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
         acc.w = fmaf(x.w, k, acc.w);
         l = fmaf(sh.l[w][r], k, l);
       }
-      if (complete) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int pr = row0 + r, head = pc.head * group + pr % group;
-        const long long row = pc.job.z + pr / group;
-        *reinterpret_cast<uint2*>(a.out + row * a.out_row + head * a.out_head + at4) =
-            make_uint2(float2_to_bf16x2(acc.x * inv, acc.y * inv), float2_to_bf16x2(acc.z * inv, acc.w * inv));
-        if (at4 == 0 && a.lse) a.lse[row * (heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
+      if (CLUSTER) {
+        *reinterpret_cast<float4*>(shared_o + r * P + at4) = acc;
+        if (at4 == 0) shared_ml[r] = make_float2(m, l);
+      } else if (complete) {
+        put(r, at4, acc, m, l);
       } else {
         *reinterpret_cast<float4*>(a.part + ((long long)slot * FEW_ROWS + r) * P + at4) = acc;
         if (at4 == 0) a.part_ml[slot * FEW_ROWS + r] = make_float2(m, l);
       }
+    }
+    if (CLUSTER) {
+      cluster_sync_all();
+      const uint32_t o_at = smem_u32(shared_o), ml_at = smem_u32(shared_ml);
+      for (int i = rank * THREADS + tid; i < nr * (P / 4); i += ranks * THREADS) {
+        const int r = i / (P / 4), at4 = 4 * (i % (P / 4));
+        if (at4 >= d) continue;
+        float m = -INFINITY, l = 0.0f;
+        for (int k = 0; k < ranks; ++k) m = fmaxf(m, ld_cluster_f2(map_to_cta(ml_at + 8 * r, k)).x);
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < ranks; ++k) {
+          const float2 ml = ld_cluster_f2(map_to_cta(ml_at + 8 * r, k));
+          const float4 x = ld_cluster_f4(map_to_cta(o_at + (r * P + at4) * 4, k));
+          const float f = exp2_fast(ml.x - ref);
+          acc.x = fmaf(x.x, f, acc.x);
+          acc.y = fmaf(x.y, f, acc.y);
+          acc.z = fmaf(x.z, f, acc.z);
+          acc.w = fmaf(x.w, f, acc.w);
+          l = fmaf(ml.y, f, l);
+        }
+        put(r, at4, acc, m, l);
+      }
+      cluster_sync_all();                            // (a CTA's memory is read until here)
+      return;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies go over the sums next)
     __syncthreads();
@@ -397,22 +464,64 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
   if (tid == 0 && !told) tell_none(a, cta);
 }
 
+// Clusters of `ranks` CTAs that run at once on the current device; 0 on error.
+template <int P>
+int clusters_at_once(int ranks) {
+  constexpr int MAX_DEVICES = 64;
+  static std::atomic<int> known[MAX_DEVICES][2];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
+  std::atomic<int>& slot = known[dev][ranks == MOST_RANKS];
+  int n = slot.load(std::memory_order_relaxed);
+  if (n == 0) {
+    const void* kernel = (const void*)attend_few_kernel<P, true>;
+    if (ensure_dynamic_smem(kernel, Few<P>::SMEM) != cudaSuccess) return 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ranks);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Few<P>::SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, (const void*)attend_few_kernel<P, true>, &cfg) != cudaSuccess) return 0;
+    if (n < 1) n = -1;
+    slot.store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 template <int P>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
-  const cudaError_t e = ensure_dynamic_smem((const void*)attend_few_kernel<P>, Few<P>::SMEM);
+  const long long pieces = pieces_of(a, false);
+  int ranks = 1;
+  if (a.pl.capacity <= CLUSTER_POSITIONS)
+    ranks = pieces <= clusters_at_once<P>(MOST_RANKS) ? MOST_RANKS : pieces <= clusters_at_once<P>(MOST_RANKS / 2) ? MOST_RANKS / 2 : 1;
+  const void* kernel = ranks > 1 ? (const void*)attend_few_kernel<P, true> : (const void*)attend_few_kernel<P, false>;
+  const cudaError_t e = ensure_dynamic_smem(kernel, Few<P>::SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(sms * few_ctas(P));
+  cfg.gridDim = dim3(ranks > 1 ? (unsigned)(pieces * ranks) : attend_ctas(P, false, sms));
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = Few<P>::SMEM;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ranks;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = ranks > 1 ? 2 : 1;
   const FewArgs args = {a, g_linear_wait_limit.load(std::memory_order_relaxed), g_linear_hold_loads.load(std::memory_order_relaxed)};
-  return cudaLaunchKernelEx(&cfg, attend_few_kernel<P>, args);
+  if (ranks > 1) return cudaLaunchKernelEx(&cfg, attend_few_kernel<P, true>, args);
+  const cudaError_t f = cudaLaunchKernelEx(&cfg, attend_few_kernel<P, false>, args);
+  return f == cudaSuccess ? launch_cache_join(a, false, sms, stream) : f;
 }
 
 }  // namespace
@@ -420,14 +529,12 @@ cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
 cudaError_t launch_cache_attend_few(const AttendArgs& a, cudaStream_t stream) {
   const int sms = device_sms();
   if (sms <= 0) return cudaErrorInvalidDevice;
-  cudaError_t e;
   switch (a.c.p / 64) {
-    case 1: e = launch<64>(a, sms, stream); break;
-    case 2: e = launch<128>(a, sms, stream); break;
-    case 3: e = launch<192>(a, sms, stream); break;
-    default: e = launch<256>(a, sms, stream); break;
+    case 1: return launch<64>(a, sms, stream);
+    case 2: return launch<128>(a, sms, stream);
+    case 3: return launch<192>(a, sms, stream);
+    default: return launch<256>(a, sms, stream);
   }
-  return e == cudaSuccess ? launch_cache_join(a, false, sms, stream) : e;
 }
 
 }  // namespace admmq

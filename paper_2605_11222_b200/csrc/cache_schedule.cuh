@@ -23,6 +23,10 @@ struct WarpWait {
   }
 };
 
+// (Numbers below 2^32, which these nearly always are, divide in a fraction of the time.)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // Positions that the rows of a tile see: [lo, hi); hi = 0 where the request takes no part.
 struct Span {
   int at;                              // position of the request's first row, -1: none
@@ -108,7 +112,7 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job,
     p.span = span_of(a, p.job, ROWS);
     const long long cost = cost_of<UNIT, EXTRA>(units_of<UNIT>(p.span, p.job, a.pl.group));
     if (u < at + cost * heads) {
-      p.head = (int)((u - at) / cost);
+      p.head = (int)quotient(u - at, cost);
       p.begin = at + p.head * cost + EXTRA;
       p.end = at + (p.head + 1) * cost;
       break;
@@ -120,10 +124,14 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job,
 }
 // CTAs that get work: at least `least` units each.
 __device__ __forceinline__ int active_ctas(long long total, int least) {
-  const long long most = (total + least - 1) / least;
+  const long long most = quotient(total + least - 1, least);
   return (int)(most < (long long)gridDim.x ? most : (long long)gridDim.x);
 }
-__device__ __forceinline__ long long line_at(long long total, int c, int ctas) { return total * c / ctas; }
+// CTA c has [line_at(c), line_at(c + 1)): total / ctas units, and one more the first total % ctas.
+__device__ __forceinline__ long long line_at(long long total, int c, int ctas) {
+  const long long each = quotient(total, ctas), more = total - each * ctas;
+  return c * each + min((long long)c, more);
+}
 // What is to be joined of a (tile, head), told by the CTA that begins it.
 __device__ __forceinline__ void tell_join(const AttendArgs& a, int tile, int head, int first, int last) {
   if (a.by_piece) a.joins[tile * a.c.heads + head] = make_int4(tile, head, first, last);
@@ -133,8 +141,10 @@ __device__ __forceinline__ void tell_join(const AttendArgs& a, int tile, int hea
 __device__ __forceinline__ void tell_none(const AttendArgs& a, int cta) {
   if (!a.by_piece) a.joins[cta] = make_int4(0, 0, cta, cta);
 }
+// The CTA that has unit u.
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
-  return (int)(((u + 1) * ctas + total - 1) / total) - 1;
+  const long long each = quotient(total, ctas), more = total - each * ctas, long_ones = more * (each + 1);
+  return (int)(u < long_ones ? quotient(u, each + 1) : more + quotient(u - long_ones, each));
 }
 
 }  // namespace admmq

@@ -20,7 +20,7 @@
 namespace admmq {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 4;
+constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 12;
 constexpr int MOST_RANKS = 16;                       // CTAs of a cluster
 constexpr long long CLUSTER_POSITIONS = 1 << 14;     // positions of a table up to which clusters share a (tile, head)
 constexpr float LIMIT = 12.0f;                       // weights stay below 2^LIMIT: fp16
@@ -41,7 +41,7 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
 template <int P>
 struct Few {
   static constexpr int UNIT_BYTES = UNIT * 2 * P;    // codes of a step
-  static constexpr int STAGES = P == 64 ? 4 : P == 256 ? 3 : 2;
+  static constexpr int STAGES = P == 64 ? 3 : P == 256 ? 3 : 2;
   static constexpr int RING_BYTES = WARPS * STAGES * UNIT_BYTES;
   struct Shared {
     uint4 q[P / 16][32];                             // first operand: [64 h + 4 s .. of every 16][lane]

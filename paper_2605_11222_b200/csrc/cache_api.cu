@@ -207,14 +207,15 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
   a.out_row = out_row;
   a.out_head = out_head;
   a.scale_log2 = (float)(scale * 1.4426950408889634);
-  a.window = window;
+  a.window = window < MAX_POSITIONS ? window : 0;    // (positions end below)
   a.status = d_status;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
   char* at = (char*)d_workspace;
   for (int many = 0; many < 2; ++many) {
     if (!(many ? a.pl.n_big : a.pl.n_small)) continue;
     const size_t ctas = attend_ctas(a.c.p, many, sms), rows = many ? many_rows(a.c.p) : FEW_ROWS;
-    a.by_piece = pieces_of(a, many) <= (long long)ctas;
+    // (halves of the plan's tiles may be without rows: nobody begins those)
+    a.by_piece = !(many && rows < MANY_ROWS) && pieces_of(a, many) <= (long long)ctas;
     a.joins = (int4*)at;
     a.part = (float*)(a.joins + ctas);
     a.part_ml = (float2*)(a.part + ctas * 2 * rows * a.c.p);

@@ -184,6 +184,7 @@ class KVCache:
         name = "admmq_cache_attend"
         self._check(plan, name)
         _no_graph(name, q)
+        _need(0 <= window < 2 ** 31, name + ": a window of at least one position, or 0 for none")
         heads = self.kv_heads * plan.group
         sq = self._strides(q, heads, torch.bfloat16, plan, name + " q")
         if out is None:

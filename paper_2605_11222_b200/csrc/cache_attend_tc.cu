@@ -774,10 +774,29 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       long long u = cta < ctas ? line_at(total, cta, ctas) : 0;
       const long long line_end = cta < ctas ? line_at(total, cta + 1, ctas) : 0;
       bool told = false;                             // of a (tile, head) that others end
+      Piece f;
       for (uint32_t n = 0;; ++n) {
         PieceJob p = {};
         if (u < line_end) {
-          const Piece f = find_piece<THREADS, TN, TILE, EXTRA>(a, job, n_tiles, schedule, u);
+          // searched for once, then one after the other
+          if (n == 0) {
+            f = find_piece<THREADS, TN, TILE, EXTRA>(a, job, n_tiles, schedule, u);
+          } else if (f.head + 1 < a.c.heads) {
+            const long long cost = f.end - f.begin + EXTRA;
+            ++f.head;
+            f.begin += cost;
+            f.end += cost;
+          } else {
+            int units;
+            do {                                     // (there is one: the line goes on)
+              f.job = job(++f.tile);
+              f.span = span_of(a, f.job, TILE);
+              units = units_of<TN>(f.span, f.job, a.pl.group);
+            } while (units == 0);
+            f.head = 0;
+            f.begin = f.end + EXTRA;
+            f.end = f.begin + units;
+          }
           const long long stop = min(line_end, f.end);
           u = max(u, f.begin);
           if (u < stop) {

@@ -85,6 +85,11 @@ struct StoreArgs {
 cudaError_t launch_cache_write(const StoreArgs& a, bool is_bf16, cudaStream_t stream);
 cudaError_t launch_cache_read(const StoreArgs& a, bool is_bf16, cudaStream_t stream);
 
+// What is to be joined of a (tile, head): the CTAs first .. last have its parts; the same CTA twice: nothing.
+struct __align__(16) Join {
+  int first, last, head, row0;         // row0: packed row of the tile's first
+  int first_row, rows, pad[2];         // first row of the request; packed rows of the tile
+};
 struct AttendArgs {
   CacheView c;
   PlanView pl;
@@ -98,7 +103,7 @@ struct AttendArgs {
   // workspace of one kind of tiles: for every CTA two partial results, and what is to be joined
   float* part;                       // [ctas][2][rows][p]
   float2* part_ml;                   // [ctas][2][rows]: maximum (base 2) and sum
-  int4* joins;                       // (tile, head, first CTA, last CTA), the same CTA twice: nothing to join
+  Join* joins;
   int by_piece;                      // joins go by (tile, head), which are no more than CTAs; or by the first CTA
 };
 // CTAs of an SM that run attention of a few rows

@@ -106,7 +106,7 @@ admmq_status store(bool write, const admmq_cache* cache, const admmq_cache_plan*
 // Workspace of one kind of tiles: for every CTA what is to be joined, and two partial results.
 size_t part_bytes(const CacheView& c, bool many, int sms) {
   const size_t ctas = attend_ctas(c.p, many, sms), rows = many ? many_rows(c.p) : FEW_ROWS;
-  return ctas * (sizeof(int4) + 2 * rows * (c.p * sizeof(float) + sizeof(float2)));
+  return ctas * (sizeof(Join) + 2 * rows * (c.p * sizeof(float) + sizeof(float2)));
 }
 size_t workspace_of(const CacheView& c, const PlanView& p, int sms) {
   return (p.n_small ? part_bytes(c, false, sms) : 0) + (p.n_big ? part_bytes(c, true, sms) : 0);
@@ -222,7 +222,7 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
     const size_t ctas = attend_ctas(a.c.p, many, sms), rows = many ? many_rows(a.c.p) : FEW_ROWS;
     // (halves of the plan's tiles may be without rows: nobody begins those)
     a.by_piece = !(many && rows < MANY_ROWS) && pieces_of(a, many) <= (long long)ctas;
-    a.joins = (int4*)at;
+    a.joins = (Join*)at;
     a.part = (float*)(a.joins + ctas);
     a.part_ml = (float2*)(a.part + ctas * 2 * rows * a.c.p);
     at += part_bytes(a.c, many, sms);

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       if (u >= stop) break;
       if (u == pc.begin) {
         told = stop < pc.end;
-        if (tid == 0) tell_join(a, pc.tile, pc.head, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
+        if (tid == 0) tell_join(a, pc, FEW_ROWS, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
       }
     }
     const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);

@@ -812,7 +812,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             p.part = u == f.begin && stop == f.end ? -1 : 2 * cta + (u == f.begin ? 1 : 0);
             if (u == f.begin) {
               told = stop < f.end;
-              if (lane == 0) tell_join(a, f.tile, f.head, cta, told ? cta_of(f.end - 1, total, ctas) : cta);
+              if (lane == 0) tell_join(a, f, TILE, cta, told ? cta_of(f.end - 1, total, ctas) : cta);
             }
             u = stop;
           }

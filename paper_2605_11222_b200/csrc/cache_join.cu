@@ -1,116 +1,136 @@
 // The end of attention over the cache where a row's positions were shared out over several CTAs (cache_schedule.cuh):
 //   out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,  M = max_c m_c,  over the CTAs c in their order.
-// Bound: latency.  WPR warps take a row, every WPR-th part each with eight loads under way, and add up in shared memory (a
-// warp that took its 55 parts of one request of 32768 tokens one after the other needed 32 us).
+// Bound: latency.  Few rows are shared out over many CTAs: four warps take a row, every fourth part each with eight loads
+// under way, and add up in shared memory (a warp that took the 55 parts of a request of 32768 tokens one after the other
+// needed 32 us).  Many rows have few parts: a warp takes four rows at once, two parts of each under way.
 #include "cache.h"
 
 namespace admmq {
 namespace {
 
 constexpr float LN2 = 0.693147180559945309f;
-constexpr int ROWS_AT_ONCE = 4;
+constexpr int SLOTS = 4;             // groups of WPR warps of a block
 
-// tile_rows: rows of a tile, `per` of them to one of the plan's tiles.
-template <int WPR>
-__global__ void __launch_bounds__(32 * WPR * ROWS_AT_ONCE) join_kernel(const __grid_constant__ AttendArgs a, const int4* tiles, int tile_rows, int per) {
-  __shared__ __align__(16) float sums[WPR > 1 ? ROWS_AT_ONCE : 1][WPR][256];
-  __shared__ float totals[ROWS_AT_ONCE][WPR];
+// tile_rows: rows of a tile.  WPR warps to RPW rows, AT_ONCE parts of them at once.
+template <int WPR, int RPW, int AT_ONCE>
+__global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_constant__ AttendArgs a, int tile_rows) {
+  static_assert(WPR == 1 || RPW == 1, "one or the other");
+  __shared__ __align__(16) float sums[WPR > 1 ? SLOTS : 1][WPR][256];
+  __shared__ float totals[SLOTS][WPR];
   pdl_launch();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = warp / WPR, w = warp % WPR;
-  const int r = blockIdx.y * ROWS_AT_ONCE + slot, p = a.c.p, d = a.c.d;
-  const int4 join = a.joins[blockIdx.x];
-  const int first = join.z, parts = join.w - first + 1;
+  const int r0 = (blockIdx.y * SLOTS + slot) * RPW, p = a.c.p, d = a.c.d;
+  const Join join = a.joins[blockIdx.x];
+  const int first = join.first, parts = join.last - first + 1;
   if (parts == 1) return;                            // (the same for the whole block)
-  int4 job = __ldg(tiles + join.x / per);
-  job.y += join.x % per * tile_rows;
-  const int group = a.pl.group, nr = min(tile_rows, job.w * group - job.y);
-  if (blockIdx.y * ROWS_AT_ONCE >= nr) return;
-  // row of part i: slot 1 of its CTA where the (tile, head) begins, 0 after
-  auto row_of = [&](int i) { return (long long)(2 * (first + i) + (i == 0)) * tile_rows + r; };
-  float m = -INFINITY, l = 0.0f;
-  float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-  if (r < nr) {
-    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[row_of(i)].x);
-    m = warp_max(m);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    const bool on[2] = {4 * lane < d, 4 * lane + 128 < d};
-    constexpr int AT_ONCE = 8;
-    for (int i0 = w; i0 < parts; i0 += WPR * AT_ONCE) {
-      float4 x[AT_ONCE][2];
-      float2 ml[AT_ONCE];
+  const int group = a.pl.group, nr = join.rows;
+  if (blockIdx.y * SLOTS * RPW >= nr) return;
+  // row r of part i: slot 1 of its CTA where the (tile, head) begins, 0 after
+  auto row_of = [&](int i, int r) { return (long long)(2 * (first + i) + (i == 0)) * tile_rows + r; };
+  const bool on[2] = {4 * lane < d, 4 * lane + 128 < d};
+  float m[RPW], l[RPW];
+  float4 acc[RPW][2];
 #pragma unroll
-      for (int e = 0; e < AT_ONCE; ++e) {
-        const int i = i0 + e * WPR;
-        const long long row = row_of(min(i, parts - 1));
-        ml[e] = a.part_ml[row];
-        if (i >= parts) ml[e] = make_float2(-INFINITY, 0.0f);
-        const float* src = a.part + row * p + 4 * lane;
+  for (int q = 0; q < RPW; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.0f;
+    acc[q][0] = acc[q][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  if (r0 < nr) {
+    float4 x[AT_ONCE][RPW][2];
+    float2 ml[AT_ONCE][RPW];
+    auto fetch = [&](int i0) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) x[e][k] = on[k] && i < parts ? *reinterpret_cast<const float4*>(src + 128 * k) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
+      for (int e = 0; e < AT_ONCE; ++e)
 #pragma unroll
-      for (int e = 0; e < AT_ONCE; ++e) {
-        const float k = exp2_fast(ml[e].x - ref);
-        l = fmaf(ml[e].y, k, l);
+        for (int q = 0; q < RPW; ++q) {
+          const int i = i0 + e * WPR;
+          const long long row = row_of(min(i, parts - 1), min(r0 + q, nr - 1));
+          ml[e][q] = i < parts ? a.part_ml[row] : make_float2(-INFINITY, 0.0f);
+          const float* src = a.part + row * p + 4 * lane;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          acc[c].x = fmaf(x[e][c].x, k, acc[c].x);
-          acc[c].y = fmaf(x[e][c].y, k, acc[c].y);
-          acc[c].z = fmaf(x[e][c].z, k, acc[c].z);
-          acc[c].w = fmaf(x[e][c].w, k, acc[c].w);
+          for (int c = 0; c < 2; ++c)
+            x[e][q][c] = on[c] && i < parts ? *reinterpret_cast<const float4*>(src + 128 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-      }
+    };
+    float top[RPW];
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) top[q] = lane < parts ? a.part_ml[row_of(lane, min(r0 + q, nr - 1))].x : -INFINITY;
+    fetch(w);                                        // (under way with the maxima)
+    for (int i = lane + 32; i < parts; i += 32)
+#pragma unroll
+      for (int q = 0; q < RPW; ++q) top[q] = fmaxf(top[q], a.part_ml[row_of(i, min(r0 + q, nr - 1))].x);
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) m[q] = warp_max(top[q]);
+    for (int i0 = w; i0 < parts; i0 += WPR * AT_ONCE) {
+      if (i0 > w) fetch(i0);
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e)
+#pragma unroll
+        for (int q = 0; q < RPW; ++q) {
+          const float k = exp2_fast(ml[e][q].x - (m[q] == -INFINITY ? 0.0f : m[q]));
+          l[q] = fmaf(ml[e][q].y, k, l[q]);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            acc[q][c].x = fmaf(x[e][q][c].x, k, acc[q][c].x);
+            acc[q][c].y = fmaf(x[e][q][c].y, k, acc[q][c].y);
+            acc[q][c].z = fmaf(x[e][q][c].z, k, acc[q][c].z);
+            acc[q][c].w = fmaf(x[e][q][c].w, k, acc[q][c].w);
+          }
+        }
     }
   }
   if (WPR > 1) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) *reinterpret_cast<float4*>(&sums[slot][w][4 * lane + 128 * c]) = acc[c];
-    if (lane == 0) totals[slot][w] = l;
+    for (int c = 0; c < 2; ++c) *reinterpret_cast<float4*>(&sums[slot][w][4 * lane + 128 * c]) = acc[0][c];
+    if (lane == 0) totals[slot][w] = l[0];
     __syncthreads();
-    if (w > 0 || r >= nr) return;
-    l = 0.0f;
+    if (w > 0) return;
+    l[0] = 0.0f;
 #pragma unroll
-    for (int v = 0; v < WPR; ++v) l += totals[slot][v];
+    for (int v = 0; v < WPR; ++v) l[0] += totals[slot][v];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      acc[c] = *reinterpret_cast<const float4*>(&sums[slot][0][4 * lane + 128 * c]);
+      acc[0][c] = *reinterpret_cast<const float4*>(&sums[slot][0][4 * lane + 128 * c]);
 #pragma unroll
       for (int v = 1; v < WPR; ++v) {
         const float4 x = *reinterpret_cast<const float4*>(&sums[slot][v][4 * lane + 128 * c]);
-        acc[c].x += x.x;
-        acc[c].y += x.y;
-        acc[c].z += x.z;
-        acc[c].w += x.w;
+        acc[0][c].x += x.x;
+        acc[0][c].y += x.y;
+        acc[0][c].z += x.z;
+        acc[0][c].w += x.w;
       }
     }
-  } else if (r >= nr) {
-    return;
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int pr = job.y + r, head = join.y * group + pr % group;
-  const long long row = job.z + pr / group;
-  bf16* dst = a.out + row * a.out_row + head * a.out_head + 4 * lane;
 #pragma unroll
-  for (int c = 0; c < 2; ++c)
-    if (4 * lane + 128 * c < d)
-      *reinterpret_cast<uint2*>(dst + 128 * c) =
-          make_uint2(float2_to_bf16x2(acc[c].x * inv, acc[c].y * inv), float2_to_bf16x2(acc[c].z * inv, acc[c].w * inv));
-  if (lane == 0 && a.lse) a.lse[row * (a.c.heads * group) + head] = l == 0.0f ? -INFINITY : m * LN2 + logf(l);
+  for (int q = 0; q < RPW; ++q) {
+    if (r0 + q >= nr) return;
+    const float inv = l[q] == 0.0f ? 0.0f : 1.0f / l[q];
+    const int pr = join.row0 + r0 + q, head = join.head * group + pr % group;
+    const long long row = join.first_row + pr / group;
+    bf16* dst = a.out + row * a.out_row + head * a.out_head + 4 * lane;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (on[c])
+        *reinterpret_cast<uint2*>(dst + 128 * c) = make_uint2(float2_to_bf16x2(acc[q][c].x * inv, acc[q][c].y * inv),
+                                                              float2_to_bf16x2(acc[q][c].z * inv, acc[q][c].w * inv));
+    if (lane == 0 && a.lse) a.lse[row * (a.c.heads * group) + head] = l[q] == 0.0f ? -INFINITY : m[q] * LN2 + logf(l[q]);
+  }
 }
 
-template <int WPR>
-cudaError_t launch(const AttendArgs& a, int joins, const int4* tiles, int rows, int per, int max_rows, cudaStream_t stream) {
+template <int WPR, int RPW, int AT_ONCE>
+cudaError_t launch(const AttendArgs& a, int joins, int rows, int max_rows, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(joins, (max_rows + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE);
-  cfg.blockDim = dim3(32 * WPR * ROWS_AT_ONCE);
+  cfg.gridDim = dim3(joins, (max_rows + SLOTS * RPW - 1) / (SLOTS * RPW));
+  cfg.blockDim = dim3(32 * WPR * SLOTS);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join_kernel<WPR>, a, tiles, rows, per);
+  return cudaLaunchKernelEx(&cfg, join_kernel<WPR, RPW, AT_ONCE>, a, rows);
 }
 
 }  // namespace
@@ -118,8 +138,8 @@ cudaError_t launch(const AttendArgs& a, int joins, const int4* tiles, int rows, 
 cudaError_t launch_cache_join(const AttendArgs& a, bool many, int sms, cudaStream_t stream) {
   const int rows = many ? many_rows(a.c.p) : FEW_ROWS;
   const int joins = a.by_piece ? pieces_of(a, many) : attend_ctas(a.c.p, many, sms);
-  return many ? launch<1>(a, joins, a.pl.big, rows, MANY_ROWS / rows, rows, stream)
-              : launch<4>(a, joins, a.pl.small, rows, 1, a.pl.small_rows, stream);
+  return many ? launch<1, 4, 2>(a, joins, rows, rows, stream)
+              : launch<4, 1, 8>(a, joins, rows, a.pl.small_rows, stream);
 }
 
 }  // namespace admmq

@@ -133,13 +133,14 @@ __device__ __forceinline__ long long line_at(long long total, int c, int ctas) {
   return c * each + min((long long)c, more);
 }
 // What is to be joined of a (tile, head), told by the CTA that begins it.
-__device__ __forceinline__ void tell_join(const AttendArgs& a, int tile, int head, int first, int last) {
-  if (a.by_piece) a.joins[tile * a.c.heads + head] = make_int4(tile, head, first, last);
-  else if (last > first) a.joins[first] = make_int4(tile, head, first, last);
+__device__ __forceinline__ void tell_join(const AttendArgs& a, const Piece& p, int tile_rows, int first, int last) {
+  const Join j = {first, last, p.head, p.job.y, p.job.z, min(tile_rows, p.job.w * a.pl.group - p.job.y), {0, 0}};
+  if (a.by_piece) a.joins[p.tile * a.c.heads + p.head] = j;
+  else if (last > first) a.joins[first] = j;
 }
 // And, where joins go by CTA, by one that begins none which others end.
 __device__ __forceinline__ void tell_none(const AttendArgs& a, int cta) {
-  if (!a.by_piece) a.joins[cta] = make_int4(0, 0, cta, cta);
+  if (!a.by_piece) a.joins[cta] = {cta, cta, 0, 0, 0, 0, {0, 0}};
 }
 // The CTA that has unit u.
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {

@@ -1,4 +1,4 @@
-"""From a calibrated layer to adapters trained over its codes: the input side of one attention block.
+"""From a calibrated layer to adapters trained over its codes, and attention over an 8-bit cache: one attention block.
 
     python examples/adapt_attention_input.py [--hidden 1024] [--steps 30]
 
@@ -6,7 +6,8 @@ The q, k and v projections of a block are quantized (W3, groups of 128) by the s
 laid out for multiplication.  Two groups of requests then train an adapter each, so that the block's normed and rotated
 queries and keys, and its values, come back to those of the unquantized weights: forward through the codes and the
 adapters, inputs kept in 8 bits, backward through the rotation, the norm and the codes.  At the end one new token of every
-request runs through the trained adapters, beside one that has none.
+request runs through the trained adapters, beside one that has none: the prompts' keys and values, kept in 8 bits, are
+attended over by the prompts themselves and by the new tokens.
 """
 import argparse
 import math
@@ -16,9 +17,9 @@ import sys
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
-from paper_2605_11222_b200 import adapt, binding as B, workloads as wl  # noqa: E402
+from paper_2605_11222_b200 import adapt, binding as B, kvcache, workloads as wl  # noqa: E402
 
-HEAD, GROUP, BITS, EPS = 64, 128, 3, 1e-6
+HEAD, GROUP, BITS, EPS, PAGE = 64, 128, 3, 1e-6, 32
 
 
 def quantize(spec, W, X):
@@ -61,6 +62,25 @@ class AttentionInput:
             dx = dx + d
             grads.append(adapt.adapter_grads(bank, plan, kept, hh, dy, u))
         return dx, grads
+
+
+def prompts_and_a_token(block, x, x_new, lengths, plan, new, pos, dev):
+    """Attention of the prompts' rows, then of one token behind each, over keys and values in 8 bits."""
+    need = [-(-(n + 1) // PAGE) for n in lengths]
+    tables, at = [], 0
+    for n in need:
+        tables.append(list(range(at, at + n)) + [0] * (max(need) - n))
+        at += n
+    cache = kvcache.KVCache(at, block.kv_heads, HEAD, PAGE, dev)
+    step = kvcache.CachePlan([1] * len(lengths), lengths, tables, block.heads // block.kv_heads, dev)
+    prompt = kvcache.CachePlan(lengths, [0] * len(lengths), step.tables, step.group)
+    out = []
+    for rows, where, requests, positions in ((x, prompt, plan, pos), (x_new, step, new, step.held.clone())):
+        (q, k, v), _ = block.forward(rows, requests, positions)
+        cache.write(k, v.view_as(k), where)
+        out.append(cache.attend(q, where)[0])
+    adapt.check_device_status(dev)
+    return out
 
 
 def main(hidden=1024, steps=30, rank=16, rows=384, dev="cuda:0", quiet=False):
@@ -111,7 +131,9 @@ def main(hidden=1024, steps=30, rank=16, rows=384, dev="cuda:0", quiet=False):
     alone = layers[0].forward(X[rows + 2: rows + 3].contiguous())[0]
     again = layers[0].forward(X[rows: rows + 3].contiguous(), banks[0], new)[0]
     same = torch.equal(again[2], alone[0])
+    prompt_out, token_out = prompts_and_a_token(block, x, X[rows: rows + 3].contiguous(), lengths, plan, new, pos, dev)
     if not quiet:
+        print(f"attention of the prompts {tuple(prompt_out.shape)} and of the tokens {tuple(token_out.shape)} over the 8-bit cache")
         print(f"decoded 3 tokens, q {tuple(qr.shape)}, k {tuple(kr.shape)}; the one without an adapter is the layer's alone: {same}")
     return losses, dx, same
 

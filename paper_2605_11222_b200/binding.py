@@ -35,6 +35,9 @@ EXPORTS = [
     "admmq_linear_grad_input", "admmq_adapter_grad", "admmq_checkpoint_save", "admmq_checkpoint_restore",
     "admmq_qk_workspace_bytes", "admmq_qk_norm_rope", "admmq_qk_norm_rope_backward", "admmq_test_linear_set_wait",
     "admmq_test_pair_rings", "admmq_test_warp_wait",
+    # admmq_cache.h (argument types in kvcache.py)
+    "admmq_cache_code_bytes", "admmq_cache_scale_bytes", "admmq_cache_plan_ints", "admmq_cache_plan_fill", "admmq_cache_write",
+    "admmq_cache_read", "admmq_cache_attend_workspace", "admmq_cache_attend",
 ]
 T_HESSIAN_PRODUCT, T_TRANSPOSE, T_FACTOR, T_WUPDATE_PRODUCT1, T_TRIDIAG_SOLVE, T_WUPDATE_PRODUCT2, \
     T_GRADIENT_PRODUCT, T_LOCAL_SEARCH, T_ROW_SPLIT, T_WUPDATE_ONE_PLANE = range(10)

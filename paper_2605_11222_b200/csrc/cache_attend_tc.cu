@@ -259,11 +259,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       // since the other may be one exchange ahead.  false: the wait ran out.
       uint32_t swaps = 0;
       const uint32_t swap_at = smem_u32(swapped) + (x * ROWS + r) * 8;
-      auto swap = [&](float mine, float& other) {
+      auto post = [&](float mine) {
         ++swaps;
-        const uint32_t to = swap_at + ((swaps & 1u) * 2 + half) * (2 * ROWS * 8), from = swap_at + ((swaps & 1u) * 2 + (half ^ 1)) * (2 * ROWS * 8);
+        const uint32_t to = swap_at + ((swaps & 1u) * 2 + half) * (2 * ROWS * 8);
         asm volatile("st.volatile.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(__float_as_uint(mine)), "r"(swaps) : "memory");
-        return poll_swap(from, swaps, other, wait);
+      };
+      auto answer = [&](float& other) {
+        return poll_swap(swap_at + ((swaps & 1u) * 2 + (half ^ 1)) * (2 * ROWS * 8), swaps, other, wait);
+      };
+      auto swap = [&](float mine, float& other) {
+        post(mine);
+        return answer(other);
       };
       // Queries come and results go by warps, a row's 16-byte chunks in neighbouring lanes: a row a lane would touch 32 lines
       // at a time.  Half a row is QC chunks; instruction i takes rows RI i + lane / QL, QL lanes to a row.
@@ -479,9 +485,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             }
           }
           if (!ok) break;
+          post(peak);                                // (read when the stores are on their way)
           tc_st16(s_col + CW / 2 - 16, w);
           float other;
-          ok = swap(peak, other);
+          ok = answer(other);
           if (!ok) break;
           peak = fmaxf(peak, other);
           raise = peak > LIMIT ? peak : 0.0f;

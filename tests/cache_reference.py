@@ -88,7 +88,7 @@ def attend64(q, sequences, lengths, held, group, scale, window=0):
     q = q.double().cpu()
     row = 0
     for i, n in enumerate(lengths):
-        if held[i] >= 0:
+        if held[i] >= 0 and n > 0:
             k, v = sequences[i]
             for h in range(hq):
                 kk, vv = k[:, h // group], v[:, h // group]

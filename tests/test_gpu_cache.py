@@ -551,3 +551,51 @@ def test_given_scale_and_unrolled_decoding_agree_with_a_prompt():
         one.held, one.plan = [i], kvcache.CachePlan([1], [i], one.padded, 2, DEV)
         one.new_rows()
         one.check_attend(window=17)
+
+
+def test_a_block_runs_its_prompts_and_decodes():
+    """Projections from codes with adapters, norm and rotation, cache and attention together, as a served block calls them:
+    prompts of ragged requests, then tokens one by one, one request joined by another in between."""
+    from paper_2605_11222_b200 import adapt, kvcache
+    heads, kv, d, hidden, page = 8, 2, 64, 512, 16
+    g = _gen(5)
+    layers, banks = [], []
+    for p in (heads * d, kv * d, kv * d):
+        codes = torch.randint(0, 16, (p, hidden), generator=g, device=DEV).to(torch.uint8)
+        scale = torch.full((p, 4), 0.06 / 15, device=DEV) * (1 + torch.rand(p, 4, generator=g, device=DEV))
+        layers.append(adapt.QuantLinear(codes, scale, -7.5 * scale, 4, 128))
+        banks.append(adapt.AdapterBank((0.05 * torch.randn(2, 8, hidden, generator=g, device=DEV)).bfloat16(),
+                                       (0.05 * torch.randn(2, 8, p, generator=g, device=DEV)).bfloat16(), torch.ones(2, device=DEV)))
+    w = [(1 + 0.1 * torch.randn(d, generator=g, device=DEV)).bfloat16() for _ in "qk"]
+    ang = torch.arange(256, device=DEV)[:, None] * 1e4 ** (-torch.arange(0, d, 2, device=DEV) / d)
+    cos, sin = ang.cos(), ang.sin()
+    lengths, adapters = [70, 0, 3, 33], [0, -1, 1, -1]
+    total = [n + 6 for n in lengths]
+    pages, lists, padded = _tables(total, page, 3)
+    cache, ref = kvcache.KVCache(pages, kv, d, page, DEV), ReferenceCache(kv, d, page)
+    tables = torch.tensor(padded, dtype=torch.int32, device=DEV)
+    held = [0, 0, 0, 0]
+
+    def run(new):
+        requests = adapt.RequestPlan(new, adapters, 2, DEV)
+        x = torch.randn(requests.n_rows, hidden, generator=g, device=DEV).bfloat16()
+        q, k, v = [l.forward(x, b, requests)[0] for l, b in zip(layers, banks)]
+        pos = torch.cat([torch.arange(p, p + n, dtype=torch.int32) for p, n in zip(held, new)]).to(DEV)
+        q, k = adapt.qk_norm_rope(q.view(-1, heads, d), k.view(-1, kv, d), *w, cos, sin, pos)
+        plan = kvcache.CachePlan(new, held, tables, heads // kv)
+        v = v.view(-1, kv, d)
+        cache.write(k, v, plan)
+        out, lse = cache.attend(q, plan)
+        adapt.check_device_status(DEV)
+        ref.write(k, v, new, held, lists)
+        seqs = [tuple(ref.sequence(s, t, p + n) for s in "kv") for t, p, n in zip(lists, held, new)]
+        want = attend64(q, seqs, new, held, heads // kv, d ** -0.5)
+        _within(out, want[0], want[2])
+        _within(lse, want[1], want[3])
+        return [p + n for p, n in zip(held, new)]
+
+    held = run(lengths)
+    held = run([1, 0, 1, 1])
+    held = run([1, 5, 1, 1])                     # the empty request's prompt joins the decoding ones
+    for _ in range(3):
+        held = run([1, 1, 1, 1])

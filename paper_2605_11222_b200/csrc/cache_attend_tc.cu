@@ -384,7 +384,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
               for (int e = 0; e < 8; ++e) z2[8 * b + e] = __ffma2_rn(z2[8 * b + e], make_float2(k, k), make_float2(o, o));
             }
             if (!(32 * c + 31 <= all_to && 32 * c >= all_from)) {
-              // bits of the positions that are seen: first <= e <= last
+              // bits of the positions that are seen: first <= e <= last.  (A branch indeed: turned into selections it would
+              // cost every step half as much again.)
+              asm volatile("");
               const int last = here - 32 * c, first = a.window > 0 ? last - a.window + 1 : 0;
               const uint32_t to = last < 0 ? 0u : last >= 31 ? 0xffffffffu : (2u << last) - 1u;
               const uint32_t from = first <= 0 ? 0xffffffffu : first > 31 ? 0u : 0xffffffffu << first;

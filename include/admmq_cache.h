@@ -46,7 +46,7 @@ size_t admmq_cache_scale_bytes(int n_pages, int kv_heads, int head_dim, int page
  * Request i has lengths[i] adjacent rows, at its positions held[i] .. held[i] + lengths[i] - 1; its position p is token
  * p % page_size of page tables[i][p / page_size].  lengths are the host's, tables and held the device's (read when the
  * kernels run, so a captured call follows them).  A request with held < 0 takes no part: nothing of it is written, its
- * rows read as zero.  One that does not fit its table raises ADMMQ_ERR_SHAPE in d_status and takes no part either, and
+ * rows read as zero.  tables and held may not change while a call runs.  One that does not fit its table raises ADMMQ_ERR_SHAPE in d_status and takes no part either, and
  * so does a page outside [0, n_pages), which is not accessed.
  * d_index: int32 buffer of admmq_cache_plan_ints entries that admmq_cache_plan_fill fills on the host (no CUDA call is
  * made) and the caller copies to the device.  group: query heads a key head (for attend). */
@@ -65,8 +65,8 @@ admmq_status admmq_cache_plan_fill(const long long* lengths, int n_requests, int
 
 /* ---- Writing and reading --------------------------------------------------------------------------------
  * k, v: [n_rows][kv_heads][head_dim] fp32 or bf16 by row and head strides (elements, inner stride 1; 16-byte aligned).
- * write: the plan's rows into the cache.  Two requests of a call may not write to one page (the cache's contents of such
- * a page are unspecified); pages that requests only read may be shared.
+ * write: the plan's rows into the cache.  A page may be written through one entry of the tables only (else its contents are
+ * unspecified); pages that requests only read may be shared.
  * read: what the cache holds at the plan's rows, as scale * code rounded to the given type. */
 admmq_status admmq_cache_write(const admmq_cache* cache, const admmq_cache_plan* plan, admmq_dtype dtype, const void* d_k,
                                long long k_row, long long k_head, const void* d_v, long long v_row, long long v_head,

@@ -49,6 +49,7 @@ struct Few {
     float row_scale[FEW_ROWS];
     float m[WARPS][FEW_ROWS], l[WARPS][FEW_ROWS];
     int abort;
+    Piece piece;
     uint64_t full[WARPS][STAGES];                    // a step's codes are there
   };
   static constexpr int O_ROW = P + 4;                // the warps' sums, [warp][row], over the rings once they are done
@@ -122,7 +123,12 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       u = pc.end * rank / ranks;
       stop = pc.end * (rank + 1) / ranks;            // (perhaps none)
     } else {
-      pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
+      if (warp == 0) {                               // (found once: every thread goes by the same lengths)
+        pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
+        if (lane == 0) sh.piece = pc;
+      }
+      __syncthreads();
+      pc = sh.piece;
       stop = min(line_end, pc.end);
       u = max(u, pc.begin);
       if (u >= stop) break;

@@ -9,13 +9,13 @@
 // multiplies the finished score.  The sum of weights takes w_j / s_b.  The reference m' is a row's maximum over the first
 // step; it is raised only after a weight has passed 2^8, which is rare, so that the accumulator is hardly ever touched
 // between its products, and a row's weights need not wait for its maximum.
-//   warps 0-7    softmax, a row a thread: scores from tensor memory into registers, weights back over them (the first
+//   warps 0-15   softmax, two threads to a row: scores from tensor memory into registers, weights back over them (the first
 //                operand of the second product), the accumulator's occasional scaling, queries in and results out
-//   warps 8-11   codes: from memory into registers a tile ahead, expanded into the swizzled operand tiles.  The order of
+//   warps 16-19  codes: from memory into registers a tile ahead, expanded into the swizzled operand tiles.  The order of
 //                positions inside a product is free, so that values, which the cache keeps as words of four tokens, need no
 //                transposition: position 16 b + k of the operand is token (0 1 8 9 2 3 10 11 4 5 12 13 6 7 14 15)[k] of block b
-//   warp 12      issues the products; tensor memory
-//   warp 13      finds the CTA's pieces of the work, ahead of the others
+//   warp 20      issues the products; tensor memory
+//   warp 21      finds the CTA's pieces of the work, ahead of the others (22 and 23: none)
 // Work is shared out in equal parts (cache_schedule.cuh), a CTA an SM.
 // Bound: exponentials (16 a cycle and SM: 2048 cycles for 256 x 128) and the tensor cores (2048 as well), overlapped.
 // Waits are bounded as in the other tensor-core kernels.  Products of a CTA run in the order of their issue; scores of the
@@ -28,8 +28,8 @@ namespace admmq {
 namespace {
 
 constexpr int ROWS = 128, SOFT_WARPS = 16, CODE_WARPS = 4, WARPS = 24, THREADS = 32 * WARPS, MMA_WARP = SOFT_WARPS + CODE_WARPS, PLAN_WARP = MMA_WARP + 1;
-constexpr int SOFT_REGS = 88, CODE_REGS = 88, MMA_REGS = 40;      // of 80 each at launch
-static_assert(4 * SOFT_REGS + CODE_REGS + MMA_REGS <= 6 * 80, "registers");
+constexpr int LAUNCH_REGS = 80, SOFT_REGS = 88, CODE_REGS = 88, MMA_REGS = 40;   // of a thread
+static_assert(4 * SOFT_REGS + CODE_REGS + MMA_REGS <= 6 * LAUNCH_REGS, "registers");
 constexpr int STAGES = 2, SCALE_SLOTS = 4, PIECE_SLOTS = 4;
 constexpr int EXTRA = 3;                             // a piece's start and end, in steps
 // Weights above 2^LIMIT raise the reference for the steps that follow; fp16 holds them up to 2^HARD_LIMIT.
@@ -48,7 +48,7 @@ struct Cfg {
   // score buffers: one a track, or two of the only one
   static constexpr int S_COL = 0, O_COL = 2 * TN;
   static_assert(O_COL + TRACKS * P <= 512, "tensor memory");
-  static_assert(SMEM <= 227 * 1024 - 8192, "shared memory");
+  static_assert(SMEM <= (227 - 16) * 1024, "shared memory, beside what is declared in the kernel");
 };
 
 // D[128][n] fp32 = A fp16 (K-major or tensor memory) B fp16 (K-major)
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   };
 
   if (warp < SOFT_WARPS) {
-    if (SOFT_REGS > 80) more_registers<SOFT_REGS>();
+    more_registers<SOFT_REGS>();
     // Two threads to a row, of warps w and w + 4: each has half of a step's positions, of the query and of the result.
     const int x = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
     constexpr int CW = TN / 2;                       // positions of a thread
@@ -796,12 +796,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             f.begin += cost;
             f.end += cost;
           } else {
-            int units;
-            do {                                     // (there is one: the line goes on)
+            int units = 0;                           // (there is a tile with some: the line goes on)
+            while (units == 0 && f.tile + 1 < n_tiles) {
               f.job = job(++f.tile);
               f.span = span_of(a, f.job, TILE);
               units = units_of<TN>(f.span, f.job, a.pl.group);
-            } while (units == 0);
+            }
             f.head = 0;
             f.begin = f.end + EXTRA;
             f.end = f.begin + units;
@@ -852,11 +852,19 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
   if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
 }
 
+bool has_registers(const void* kernel) {
+  cudaFuncAttributes attr;
+  return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs == LAUNCH_REGS;
+}
+
 template <int P>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
   using C = Cfg<P>;
   const cudaError_t e = ensure_dynamic_smem((const void*)attend_many_kernel<P>, C::SMEM);
   if (e != cudaSuccess) return e;
+  // (with fewer registers at launch the warps would wait for more than there are)
+  static const bool registers = has_registers((const void*)attend_many_kernel<P>);
+  if (!registers) return cudaErrorInvalidConfiguration;
   const ManyArgs args = {a, g_linear_wait_limit.load(std::memory_order_relaxed), g_linear_hold_loads.load(std::memory_order_relaxed)};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(sms);

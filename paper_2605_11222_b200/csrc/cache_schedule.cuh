@@ -107,12 +107,13 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job,
   long long at = s.sums[lo] * heads;
   Piece p;
   int t = lo * s.per;
-  for (;; ++t) {                       // (ends within the segment: u is below the line's end)
+  for (;; ++t) {
     p.job = job(t);
     p.span = span_of(a, p.job, ROWS);
     const long long cost = cost_of<UNIT, EXTRA>(units_of<UNIT>(p.span, p.job, a.pl.group));
-    if (u < at + cost * heads) {
-      p.head = (int)quotient(u - at, cost);
+    // (It is found within the segment.  Should somebody write into `held` meanwhile, the last tile ends the search.)
+    if (u < at + cost * heads || t + 1 >= n) {
+      p.head = cost > 0 ? (int)min(quotient(u - at, cost), (long long)heads - 1) : 0;
       p.begin = at + p.head * cost + EXTRA;
       p.end = at + (p.head + 1) * cost;
       break;

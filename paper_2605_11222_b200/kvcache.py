@@ -9,8 +9,8 @@
 
 16 neighbouring tokens of a head share a scale, max |x| / 127, for keys and for values; where a later token of the 16 is
 larger, the codes that are there are rounded to the new scale.  Every step runs in the library's kernels, on the current
-stream of the cache's device, and can be captured; the device reads `held` and `tables` when it runs, so a captured step
-follows them.  Argument errors raise AdmmqError before anything is enqueued; a request that does not fit its table, or a
+stream of the cache's device, and can be captured after a first call outside a capture; the device reads `held` and `tables`
+when it runs, so a captured step follows them (keep the plan and the cache: a graph holds their pointers).  Argument errors raise AdmmqError before anything is enqueued; a request that does not fit its table, or a
 page that does not exist, raises it in adapt.check_device_status.  No call records an autograd graph: inputs that require
 grad are refused while grad mode is on.
 """
@@ -138,8 +138,8 @@ class KVCache:
         return (x.stride(0) if x.shape[0] > 1 else 0), (x.stride(1) if heads > 1 else 0)
 
     def write(self, k: torch.Tensor, v: torch.Tensor, plan: CachePlan) -> None:
-        """Rows k, v [rows, kv_heads, head_dim], bf16 or fp32, any row and head strides, to the plan's positions.  Two
-        requests of a call may not write to one page."""
+        """Rows k, v [rows, kv_heads, head_dim], bf16 or fp32, any row and head strides, to the plan's positions.  A
+        page may be written through one entry of the tables only."""
         if plan.__class__ is CachePlan:
             r = adapt._fast.cache_write(self._status, self._ref, plan._ref, self.codes, self.scale, plan.tables, plan.held, k, v)
             if r is None:

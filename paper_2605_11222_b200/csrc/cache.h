@@ -107,7 +107,7 @@ struct AttendArgs {
   int by_piece;                      // joins go by (tile, head), which are no more than CTAs; or by the first CTA
 };
 // CTAs of an SM that run attention of a few rows
-__host__ __device__ constexpr int few_ctas(int p) { return p <= 64 ? 4 : p <= 128 ? 3 : p <= 192 ? 2 : 1; }
+__host__ __device__ constexpr int few_ctas(int p) { return p <= 64 ? 4 : p <= 128 ? 3 : 2; }
 __host__ __device__ constexpr int many_rows(int p) { return p <= 128 ? MANY_ROWS : MANY_ROWS / 2; }
 // CTAs of either kernel, and (tile, head)s.
 inline int attend_ctas(int p, bool many, int sms) { return sms * (many ? 1 : few_ctas(p)); }

@@ -1,7 +1,8 @@
 // Attention of a few rows over the 8-bit cache: one new token of a request, or a few drafted ones.
 //   z_j = scale q . k_j,  out = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m)
 //
-// Bound: reading the cache, once.  A warp takes 32 positions (two blocks) at a time.  Their codes come as two bulk copies into
+// Bound: reading the cache, once.  A warp takes 32 positions (two blocks; one of heads of more than
+// 128) at a time.  Their codes come as a bulk copy a block into
 // a ring of its own in shared memory, in the order of the second operand of m16n8k16 products (16 bytes a lane, 512 a warp
 // and load); two further steps are under way meanwhile, 128 KB an SM (memory's latency times its rate asks for some 45).
 // The 16 rows of the product are the query heads of one key
@@ -20,7 +21,7 @@
 namespace admmq {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, UNIT = 32, LEAST_UNITS = WARPS, EXTRA = 12;
+constexpr int WARPS = 4, THREADS = 32 * WARPS, LEAST_UNITS = WARPS, EXTRA = 12;
 constexpr int MOST_RANKS = 16;                       // CTAs of a cluster
 constexpr long long CLUSTER_POSITIONS = 1 << 14;     // positions of a table up to which clusters share a (tile, head)
 constexpr float LIMIT = 12.0f;                       // weights stay below 2^LIMIT: fp16
@@ -40,8 +41,10 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
 
 template <int P>
 struct Few {
-  static constexpr int UNIT_BYTES = UNIT * 2 * P;    // codes of a step
-  static constexpr int STAGES = P == 64 ? 3 : P == 256 ? 3 : 2;
+  static constexpr int NB = P <= 128 ? 2 : 1;                  // blocks of a step
+  static constexpr int UNIT = NB * CBLOCK;
+  static constexpr int BLOCK_BYTES = 2 * CBLOCK * P, UNIT_BYTES = NB * BLOCK_BYTES;   // codes of a block, of a step
+  static constexpr int STAGES = P == 192 ? 4 : P == 256 || P == 64 ? 3 : 2;
   static constexpr int RING_BYTES = WARPS * STAGES * UNIT_BYTES;
   struct Shared {
     uint4 q[P / 16][32];                             // first operand: [64 h + 4 s .. of every 16][lane]
@@ -69,6 +72,7 @@ struct FewArgs {
 template <int P, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const __grid_constant__ FewArgs A) {
   using F = Few<P>;
+  constexpr int UNIT = F::UNIT, NB = F::NB;
   const AttendArgs& a = A.a;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(smem_raw + F::RING_BYTES);
@@ -185,45 +189,46 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
 
     const int unit0 = (int)(u - pc.begin) + pc.span.lo / UNIT, unit1 = (int)(stop - pc.begin) + pc.span.lo / UNIT;
     const int n_blocks = (pc.span.hi + CBLOCK - 1) / CBLOCK;
-    // pages of a step's two blocks; -1: none there
+    // pages of a step's blocks; -1: none there
     struct Pages {
-      int p[2];
+      int p[NB];
     };
     auto look = [&](int unit) {
-      Pages n = {{-1, -1}};
+      Pages n;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int blk = 2 * unit + b;
+      for (int b = 0; b < NB; ++b) {
+        const int blk = NB * unit + b;
+        n.p[b] = -1;
         if (unit < unit1 && blk < n_blocks) n.p[b] = a.pl.tables[(long long)pc.job.x * a.pl.max_pages + (blk >> a.c.bpp_shift)];
       }
       return n;
     };
     // A step under way: its blocks' scales, and whether they exist.
     struct Step {
-      float2 s[2];
-      bool exists[2];
+      float2 s[NB];
+      bool exists[NB];
     };
     auto fetch = [&](int unit, const Pages& n) {
       Step f;
-      int at[2];
+      int at[NB], bytes = 0;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int blk = 2 * unit + b;
+      for (int b = 0; b < NB; ++b) {
+        const int blk = NB * unit + b;
         f.exists[b] = (unsigned)n.p[b] < (unsigned)a.c.n_pages;
         if (!f.exists[b] && unit < unit1 && blk < n_blocks) raise_status(a.status, ADMMQ_ERR_SHAPE);
         at[b] = f.exists[b] ? (n.p[b] * heads + pc.head) * a.c.bpp + (blk & a.c.bpp - 1) : 0;
+        bytes += f.exists[b] ? F::BLOCK_BYTES : 0;
         f.s[b] = f.exists[b] ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
       }
       if (unit < unit1) {
         if (lane == 0 && !A.hold_loads) {
           const uint32_t stage = issued % F::STAGES, bar = full + 8 * stage, dst = ring_at + stage * F::UNIT_BYTES;
-          const int bytes = (f.exists[0] ? F::UNIT_BYTES / 2 : 0) + (f.exists[1] ? F::UNIT_BYTES / 2 : 0);
           if (bytes) mbar_expect_tx(bar, bytes);
           else mbar_arrive(bar);
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < NB; ++b)
             if (f.exists[b])
-              bulk_load(dst + b * (F::UNIT_BYTES / 2), a.c.codes + (size_t)(uint32_t)at[b] * (uint32_t)a.c.block_bytes, F::UNIT_BYTES / 2, bar);
+              bulk_load(dst + b * F::BLOCK_BYTES, a.c.codes + (size_t)(uint32_t)at[b] * (uint32_t)F::BLOCK_BYTES, F::BLOCK_BYTES, bar);
         }
         ++issued;
       }
@@ -247,24 +252,24 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       if (dead) break;
       ++taken;
       const uint8_t* codes = ring + stage * F::UNIT_BYTES + lane * 16;
-      // ---- scores of the 32 positions
-      float z[2][2][4];
+      // ---- scores of the step's positions
+      float z[NB][2][4];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 2; ++j) z[b][j][0] = z[b][j][1] = z[b][j][2] = z[b][j][3] = 0.0f;
 #pragma unroll
       for (int h = 0; h < P / 64; ++h) {
-        uint4 k[2][2];
+        uint4 k[NB][2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) k[b][j] = *reinterpret_cast<const uint4*>(codes + b * (F::UNIT_BYTES / 2) + (2 * h + j) * 512);
+          for (int j = 0; j < 2; ++j) k[b][j] = *reinterpret_cast<const uint4*>(codes + b * F::BLOCK_BYTES + (2 * h + j) * 512);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const uint4 q = sh.q[h * 4 + s][lane];
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const uint4& w = k[b][j];
@@ -273,14 +278,20 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
             }
         }
       }
-      const float2 sc[2] = {ahead[0].s[0], ahead[0].s[1]};
-      const bool exists[2] = {ahead[0].exists[0], ahead[0].exists[1]};
+      float2 sc[NB];
+      bool exists[NB], all = true;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        sc[b] = ahead[0].s[b];
+        exists[b] = ahead[0].exists[b];
+        all &= exists[b];
+      }
       // ---- exponents, base 2
       const int pos = unit * UNIT;
-      const bool whole = pos + UNIT - 1 <= first_here && (a.window <= 0 || pos > last_here - a.window) && exists[0] && exists[1];
-      float most0 = -INFINITY, most1 = -INFINITY, inv_s[2];   // of this lane's four positions of a block
+      const bool whole = pos + UNIT - 1 <= first_here && (a.window <= 0 || pos > last_here - a.window) && all;
+      float most0 = -INFINITY, most1 = -INFINITY, inv_s[NB];   // of this lane's four positions of a block
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < NB; ++b) {
         const float vs = sc[b].y == 0.0f ? 1.0f : sc[b].y, lv = __log2f(vs), k0 = f0 * sc[b].x, k1 = f1 * sc[b].x;
         // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
         inv_s[b] = vs == vs ? __fdividef(1.0f, vs) : 1.0f;
@@ -326,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
           o[i][3] *= a1;
         }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -335,9 +346,9 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
               z[b][j][2 + e] -= by1;
             }
       }
-      uint4 w[2];
+      uint4 w[NB];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < NB; ++b) {
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -356,10 +367,10 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       }
       // ---- values
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int c = 0; c < P / 32; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(codes + b * (F::UNIT_BYTES / 2) + 16 * P + c * 512);
+          const uint4 x = *reinterpret_cast<const uint4*>(codes + b * F::BLOCK_BYTES + 16 * P + c * 512);
           mma_f16(o[4 * c], w[b], two_codes<false>(x.x), two_codes<true>(x.x));
           mma_f16(o[4 * c + 1], w[b], two_codes<false>(x.y), two_codes<true>(x.y));
           mma_f16(o[4 * c + 2], w[b], two_codes<false>(x.z), two_codes<true>(x.z));

@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
   const int group = a.pl.group, nr = join.rows;
   if (blockIdx.y * SLOTS * RPW >= nr) return;
   // row r of part i: slot 1 of its CTA where the (tile, head) begins, 0 after
-  auto row_of = [&](int i, int r) { return (long long)(2 * (first + i) + (i == 0)) * tile_rows + r; };
+  // (numbers of 32 bits: a few hundred CTAs' rows of at most 256 values)
+  auto row_of = [&](int i, int r) { return (2 * (first + i) + (i == 0)) * tile_rows + r; };
   const bool on[2] = {4 * lane < d, 4 * lane + 128 < d};
   float m[RPW], l[RPW];
   float4 acc[RPW][2];
@@ -46,9 +47,9 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
 #pragma unroll
         for (int q = 0; q < RPW; ++q) {
           const int i = i0 + e * WPR;
-          const long long row = row_of(min(i, parts - 1), min(r0 + q, nr - 1));
+          const int row = row_of(i, min(r0 + q, nr - 1));
           ml[e][q] = i < parts ? a.part_ml[row] : make_float2(-INFINITY, 0.0f);
-          const float* src = a.part + row * p + 4 * lane;
+          const float* src = a.part + (unsigned)(row * p + 4 * lane);
 #pragma unroll
           for (int c = 0; c < 2; ++c)
             x[e][q][c] = on[c] && i < parts ? *reinterpret_cast<const float4*>(src + 128 * c) : make_float4(0.f, 0.f, 0.f, 0.f);

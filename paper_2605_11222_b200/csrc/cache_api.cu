@@ -46,7 +46,7 @@ bool is_few(long long packed, long long all) { return packed <= MOST_FEW || all 
 long long round4(long long n) { return (n + 3) & ~3LL; }
 struct IndexSizes {
   long long rows, blocks, small, big, small_rows;   // small_rows: most packed rows that a small tile holds
-  long long ints(int n) const { return round4(n + 1) + round4(2 * blocks) + 4 * (small + big); }
+  long long ints(int n) const { return round4(n + 1) + 4 * (blocks + small + big); }
 };
 bool index_sizes(const long long* lengths, int n, int group, IndexSizes* s) {
   *s = {};
@@ -73,8 +73,8 @@ admmq_status view_plan(const admmq_cache_plan* p, const CacheView& c, PlanView* 
   if (capacity > MAX_POSITIONS || p->n_rows > MAX_POSITIONS) return ADMMQ_ERR_SHAPE;
   if (!aligned(p->d_tables, 4) || !aligned(p->d_held, 4) || !aligned(p->d_index, 16)) return ADMMQ_ERR_INVALID_ARG;
   const int* at = p->d_index + round4(p->n_requests + 1);
-  const int* tiles = at + round4(2LL * p->n_blocks);
-  *v = {p->d_tables, p->d_held, p->d_index, (const int2*)at, (const int4*)tiles, (const int4*)tiles + p->n_small,
+  const int* tiles = at + 4LL * p->n_blocks;
+  *v = {p->d_tables, p->d_held, p->d_index, (const int4*)at, (const int4*)tiles, (const int4*)tiles + p->n_small,
         p->n_requests, p->max_pages, p->group, p->n_blocks, p->n_small, p->n_big, p->small_rows, capacity};
   return ADMMQ_OK;
 }
@@ -137,7 +137,7 @@ admmq_status admmq_cache_plan_fill(const long long* lengths, int n_requests, int
   if (!index || !plan || plan->struct_size != sizeof(admmq_cache_plan)) return ADMMQ_ERR_INVALID_ARG;
   if (!index_sizes(lengths, n_requests, group, &s)) return ADMMQ_ERR_SHAPE;
   int* blocks = index + round4(n_requests + 1);
-  int* small = blocks + round4(2 * s.blocks);
+  int* small = blocks + 4 * s.blocks;
   int* big = small + 4 * s.small;
   for (int* p = index; p < big + 4 * s.big; ++p) *p = 0;
   int row = 0;
@@ -147,6 +147,8 @@ admmq_status admmq_cache_plan_fill(const long long* lengths, int n_requests, int
     for (int b = 0; b < blocks_of(rows); ++b) {
       *blocks++ = i;
       *blocks++ = b;
+      *blocks++ = row;
+      *blocks++ = rows;
     }
     const bool few = is_few((long long)rows * group, s.rows * group);
     const int step = few ? FEW_ROWS : MANY_ROWS;

@@ -23,7 +23,10 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS, LEAST_UNITS = WARPS, EXTRA = 12;
 constexpr int MOST_RANKS = 16;                       // CTAs of a cluster
-constexpr long long CLUSTER_POSITIONS = 1 << 14;     // positions of a table up to which clusters share a (tile, head)
+// Positions of a table for each of them, at most: a cluster is as slow as its longest request.  Heads of 128, 8 heads of keys,
+// clusters / shared out: 27 requests of 2000 27 / 37 us, 50 of 1000 25 / 39, 6 of 8000 27 / 30, one of 16000 22 / 20; one of 2000
+// among 26 of 60 tokens 19 / 15.
+constexpr long long RANK_POSITIONS = 1024;
 constexpr float LIMIT = 12.0f;                       // weights stay below 2^LIMIT: fp16
 constexpr float LN2 = 0.693147180559945309f;
 
@@ -481,14 +484,14 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
   if (tid == 0 && !told) tell_none(a, cta);
 }
 
-// Clusters of `ranks` CTAs that run at once on the current device; 0 on error.
+// Clusters of `ranks` CTAs (a power of two) that run at once on the current device; 0 on error.
 template <int P>
 int clusters_at_once(int ranks) {
   constexpr int MAX_DEVICES = 64;
-  static std::atomic<int> known[MAX_DEVICES][2];
+  static std::atomic<int> known[MAX_DEVICES][MOST_RANKS + 1];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
-  std::atomic<int>& slot = known[dev][ranks == MOST_RANKS];
+  std::atomic<int>& slot = known[dev][ranks];
   int n = slot.load(std::memory_order_relaxed);
   if (n == 0) {
     const void* kernel = (const void*)attend_few_kernel<P, true>;
@@ -515,14 +518,14 @@ int clusters_at_once(int ranks) {
 template <int P>
 cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
   const long long pieces = pieces_of(a, false);
-  int ranks = 1;
-  if (a.pl.capacity <= CLUSTER_POSITIONS)
-    ranks = pieces <= clusters_at_once<P>(MOST_RANKS) ? MOST_RANKS : pieces <= clusters_at_once<P>(MOST_RANKS / 2) ? MOST_RANKS / 2 : 1;
-  const void* kernel = ranks > 1 ? (const void*)attend_few_kernel<P, true> : (const void*)attend_few_kernel<P, false>;
+  int ranks = MOST_RANKS;                            // as many as leave every cluster running at once
+  while (ranks > 0 && pieces > clusters_at_once<P>(ranks)) ranks /= 2;
+  if (a.pl.capacity > ranks * RANK_POSITIONS) ranks = 0;
+  const void* kernel = ranks > 0 ? (const void*)attend_few_kernel<P, true> : (const void*)attend_few_kernel<P, false>;
   const cudaError_t e = ensure_dynamic_smem(kernel, Few<P>::SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ranks > 1 ? (unsigned)(pieces * ranks) : attend_ctas(P, false, sms));
+  cfg.gridDim = dim3(ranks > 0 ? (unsigned)(pieces * ranks) : attend_ctas(P, false, sms));
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = Few<P>::SMEM;
   cfg.stream = stream;
@@ -534,9 +537,9 @@ cudaError_t launch(const AttendArgs& a, int sms, cudaStream_t stream) {
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = ranks > 1 ? 2 : 1;
+  cfg.numAttrs = ranks > 0 ? 2 : 1;
   const FewArgs args = {a, g_linear_wait_limit.load(std::memory_order_relaxed), g_linear_hold_loads.load(std::memory_order_relaxed)};
-  if (ranks > 1) return cudaLaunchKernelEx(&cfg, attend_few_kernel<P, true>, args);
+  if (ranks > 0) return cudaLaunchKernelEx(&cfg, attend_few_kernel<P, true>, args);
   const cudaError_t f = cudaLaunchKernelEx(&cfg, attend_few_kernel<P, false>, args);
   return f == cudaSuccess ? launch_cache_join(a, false, sms, stream) : f;
 }

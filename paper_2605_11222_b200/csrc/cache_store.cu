@@ -66,8 +66,8 @@ struct Unit {
   int first, n;
 };
 __device__ __forceinline__ bool find_unit(const StoreArgs& a, Unit& u) {
-  const int2 job = __ldg(a.pl.blocks + blockIdx.x);
-  const int row0 = __ldg(a.pl.row_start + job.x), rows = __ldg(a.pl.row_start + job.x + 1) - row0;
+  const int4 job = __ldg(a.pl.blocks + blockIdx.x);
+  const int row0 = job.z, rows = job.w;
   const long long at = first_position(a.pl, job.x, rows, a.status);
   if (at < 0) return false;
   const int b = (int)(at / CBLOCK) + job.y, begin = max((int)at, b * CBLOCK), end = min((int)at + rows, (b + 1) * CBLOCK);
@@ -155,6 +155,13 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const __grid_const
         }
       }
     }
+    // codes of earlier tokens, if the block goes on
+    uint4 old[2 * PC];
+    if (u.first > 0) {
+#pragma unroll
+      for (int o = 0; o < 2 * PC; ++o)
+        old[o] = *reinterpret_cast<const uint4*>(block + (values ? o * 512 + lane * 16 : (o >> 1) * 1024 + (o & 1) * 512 + lane * 16));
+    }
     // (the order of the bit patterns is that of the magnitudes, with infinity and NaN on top)
 #pragma unroll
     for (int o = 0; o < 2 * PC; ++o)
@@ -191,8 +198,7 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const __grid_const
           }
           *dst = make_uint4(w[0], w[1], w[2], w[3]);
         } else if (slot < u.first && again) {
-          const uint4 old = *dst;
-          uint32_t w[4] = {old.x, old.y, old.z, old.w};
+          uint32_t w[4] = {old[o].x, old[o].y, old[o].z, old[o].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             w[i] = pack4(rounded_again(w[i], 0, r), rounded_again(w[i], 1, r), rounded_again(w[i], 2, r), rounded_again(w[i], 3, r));
@@ -220,14 +226,13 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const __grid_const
             else if (slot < u.first + u.n) mine |= 0xffu << (8 * k);
           }
           if (!mine && !(before && again)) continue;
-          const uint4 had = *dst;
-          const uint32_t old[4] = {had.x, had.y, had.z, had.w};
+          const uint32_t had[4] = {old[o].x, old[o].y, old[o].z, old[o].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t kept = again ? pack4(rounded_again(old[i], 0, r), rounded_again(old[i], 1, r), rounded_again(old[i], 2, r),
-                                                rounded_again(old[i], 3, r))
-                                        : old[i];
-            w[i] = (w[i] & mine) | (kept & before) | (old[i] & ~(mine | before));
+            const uint32_t kept = again ? pack4(rounded_again(had[i], 0, r), rounded_again(had[i], 1, r), rounded_again(had[i], 2, r),
+                                                rounded_again(had[i], 3, r))
+                                        : had[i];
+            w[i] = (w[i] & mine) | (kept & before) | (had[i] & ~(mine | before));
           }
         }
         *dst = make_uint4(w[0], w[1], w[2], w[3]);
@@ -246,8 +251,8 @@ __global__ void __launch_bounds__(THREADS) cache_read_kernel(const __grid_consta
   for (int which = blockIdx.y * WARPS + (threadIdx.x >> 5); which < 2 * a.c.heads; which += gridDim.y * WARPS) {
     if (!found) {
       // rows of a request that takes no part, or of a page that does not exist, read as zero
-      const int2 job = __ldg(a.pl.blocks + blockIdx.x);
-      const int row0 = __ldg(a.pl.row_start + job.x), rows = __ldg(a.pl.row_start + job.x + 1) - row0;
+      const int4 job = __ldg(a.pl.blocks + blockIdx.x);
+      const int row0 = job.z, rows = job.w;
       const int at = a.pl.held[job.x];
       int begin = 0, end = 0;
       if (at < 0 || (long long)at + rows > a.pl.capacity) {

@@ -58,13 +58,14 @@ def test_the_index_of_the_rows(kv, lengths, group):
     assert p.n_requests == n and p.group == group and p.n_rows == sum(lengths)
     assert list(index[: n + 1]) == [sum(lengths[:i]) for i in range(n + 1)]
     at = pad(n + 1)
-    blocks = index[at: at + 2 * p.n_blocks].reshape(-1, 2)
+    blocks = index[at: at + 4 * p.n_blocks].reshape(-1, 4)
+    assert all(row == sum(lengths[:r]) and n_rows == lengths[r] for r, _, row, n_rows in blocks)
     for i, k in enumerate(lengths):
-        mine = sorted(b for r, b in blocks if r == i)
+        mine = sorted(b for r, b, _, _ in blocks if r == i)
         assert mine == list(range((k + 30) // 16 if k else 0))
         for first in range(16):                                      # enough for every place of the first row in its block
             assert k == 0 or (first + k + 15) // 16 <= len(mine)
-    at += pad(2 * p.n_blocks)
+    at += 4 * p.n_blocks
     small, big = index[at: at + 4 * p.n_small].reshape(-1, 4), index[at + 4 * p.n_small: at + 4 * (p.n_small + p.n_big)].reshape(-1, 4)
     assert len(index) == at + 4 * (p.n_small + p.n_big)
     seen = {i: [] for i in range(n)}

@@ -171,6 +171,19 @@ def test_work_shared_out_over_ragged_requests(lengths, held, heads, group, d, wi
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
+@pytest.mark.parametrize("lengths,held,heads,group,d,page,window", ATTEND + [
+    ([1] * 20, [(137 * i) % 1100 for i in range(20)], 4, 4, 128, 64, 0),
+    ([2] * 6, [400 * i for i in range(6)], 2, 8, 192, 32, 333)])
+def test_tables_far_longer_than_the_requests(lengths, held, heads, group, d, page, window):
+    from paper_2605_11222_b200 import kvcache
+    s = Setup(lengths, held, heads, d, page, seed=sum(held) + d, group=group)
+    s.new_rows()
+    q, out, lse = s.check_attend(window)
+    wide = [t + [2 ** 30] * (40000 // page) for t in s.padded]              # the call that may not count on short requests
+    s.plan = kvcache.CachePlan(lengths, held, wide, group, DEV)
+    s.check_attend(window, q=q)
+
+
 def test_one_long_request_is_split_and_joined():
     s = Setup([1], [20000], 2, 128, 128, group=8, seed=3)                   # (over the clusters' positions)
     s.new_rows()

@@ -52,10 +52,12 @@ struct Few {
   struct Shared {
     uint4 q[P / 16][32];                             // first operand: [64 h + 4 s .. of every 16][lane]
     Schedule<THREADS> schedule;
+    long long total, line_end;                       // of the line, and where this CTA's part ends
+    int ctas;                                        // that have a part
     float row_scale[FEW_ROWS];
     float m[WARPS][FEW_ROWS], l[WARPS][FEW_ROWS];
     int abort;
-    Piece piece;
+    Piece piece[2];                                  // the one at hand and the next, found once: all go by the same lengths
     uint64_t full[WARPS][STAGES];                    // a step's codes are there
   };
   static constexpr int O_ROW = P + 4;                // the warps' sums, [warp][row], over the rings once they are done
@@ -98,56 +100,64 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
 
   const auto job = [&](int tile) { return __ldg(a.pl.small + tile); };
   const int cta = blockIdx.x;
-  int ctas = 0, rank = 0, ranks = 1;
-  long long total = 0, u = 0, line_end = 1;
+  int rank = 0, ranks = 1;
+  long long u = 0;
   if (CLUSTER) {
     rank = (int)cluster_ctarank();
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-    __syncthreads();                                 // (the abort flag)
+    if (tid == 0) {
+      Piece& pc = sh.piece[0];
+      sh.line_end = 1;
+      pc.tile = cta / ranks / heads;
+      pc.head = cta / ranks - pc.tile * heads;
+      pc.job = job(pc.tile);
+      pc.span = span_of(a, pc.job, FEW_ROWS);
+      pc.begin = 0;
+      pc.end = units_of<UNIT>(pc.span, pc.job, group);
+    }
+    __syncthreads();
   } else {
-    total = make_schedule<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule) * heads;
-    ctas = active_ctas(total, LEAST_UNITS);
+    const long long total = make_schedule<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule) * heads;
+    const int ctas = active_ctas(total, LEAST_UNITS);
     if (cta >= ctas) {
       if (tid == 0) tell_none(a, cta);
       return;
     }
     u = line_at(total, cta, ctas);
-    line_end = line_at(total, cta + 1, ctas);
+    const long long line_end = line_at(total, cta + 1, ctas);
+    if (tid == 0) {
+      sh.total = total;
+      sh.ctas = ctas;
+      sh.line_end = line_end;
+    }
+    // (a thread looks into its own segment: a search by one warp took 1.5 us)
+    if (sh.schedule.sums[tid] * heads <= u && u < sh.schedule.sums[tid + 1] * heads)
+      sh.piece[0] = piece_of<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, tid, u);
+    __syncthreads();
   }
+  int pieces = 0;                                    // of this CTA so far
   bool told = false;                                 // of a (tile, head) that others end
 
-  while (u < line_end) {
-    Piece pc;
+  while (u < sh.line_end) {
+    const Piece& pc = sh.piece[pieces & 1];
     long long stop;
     if (CLUSTER) {
-      const int at = cta / ranks;
-      pc.tile = at / heads;
-      pc.head = at - pc.tile * heads;
-      pc.job = job(pc.tile);
-      pc.span = span_of(a, pc.job, FEW_ROWS);
-      pc.begin = 0;
-      pc.end = units_of<UNIT>(pc.span, pc.job, group);
       u = pc.end * rank / ranks;
       stop = pc.end * (rank + 1) / ranks;            // (perhaps none)
     } else {
-      if (warp == 0) {                               // (found once: every thread goes by the same lengths)
-        pc = find_piece<THREADS, UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.schedule, u);
-        if (lane == 0) sh.piece = pc;
-      }
-      __syncthreads();
-      pc = sh.piece;
-      stop = min(line_end, pc.end);
+      stop = min(sh.line_end, pc.end);
       u = max(u, pc.begin);
       if (u >= stop) break;
       if (u == pc.begin) {
         told = stop < pc.end;
-        if (tid == 0) tell_join(a, pc, FEW_ROWS, cta, told ? cta_of(pc.end - 1, total, ctas) : cta);
+        if (tid == 0) tell_join(a, pc, FEW_ROWS, cta, told ? cta_of(pc.end - 1, sh.total, sh.ctas) : cta);
       }
     }
-    const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
+    const int request = pc.job.x, key_head = pc.head;
 
     // ---- queries: each row times a power of two that brings its largest value to [2^13, 2^14), as fp16
     {
+      const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
       const int r = tid >> 3, sub = tid & 7, pr = row0 + r, token = pr / group, head = pc.head * group + pr % group;
       const bf16* src = a.q + (long long)(pc.job.z + token) * a.q_row + head * a.q_head;
       uint2 raw[P / 32];
@@ -181,8 +191,8 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
     __syncthreads();
     const float f0 = sh.row_scale[g], f1 = sh.row_scale[g + 8];
     // the last position that rows g and g + 8 see
-    const int here0 = pc.span.at + (row0 + g) / group, here1 = pc.span.at + (row0 + g + 8) / group;
-    const int first_here = pc.span.at + row0 / group, last_here = pc.span.hi - 1;
+    const int here0 = pc.span.at + (pc.job.y + g) / group, here1 = pc.span.at + (pc.job.y + g + 8) / group;
+    const int first_here = pc.span.at + pc.job.y / group, last_here = pc.span.hi - 1;
 
     float o[P / 8][4];
 #pragma unroll
@@ -202,7 +212,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       for (int b = 0; b < NB; ++b) {
         const int blk = NB * unit + b;
         n.p[b] = -1;
-        if (unit < unit1 && blk < n_blocks) n.p[b] = a.pl.tables[(long long)pc.job.x * a.pl.max_pages + (blk >> a.c.bpp_shift)];
+        if (unit < unit1 && blk < n_blocks) n.p[b] = a.pl.tables[(long long)request * a.pl.max_pages + (blk >> a.c.bpp_shift)];
       }
       return n;
     };
@@ -219,7 +229,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
         const int blk = NB * unit + b;
         f.exists[b] = (unsigned)n.p[b] < (unsigned)a.c.n_pages;
         if (!f.exists[b] && unit < unit1 && blk < n_blocks) raise_status(a.status, ADMMQ_ERR_SHAPE);
-        at[b] = f.exists[b] ? (n.p[b] * heads + pc.head) * a.c.bpp + (blk & a.c.bpp - 1) : 0;
+        at[b] = f.exists[b] ? (n.p[b] * heads + key_head) * a.c.bpp + (blk & a.c.bpp - 1) : 0;
         bytes += f.exists[b] ? F::BLOCK_BYTES : 0;
         f.s[b] = f.exists[b] ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
       }
@@ -249,6 +259,8 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       for (int i = 0; i < F::STAGES; ++i) ahead[i] = fetch(unit + i * WARPS, n[i]);
     }
     Pages next = look(unit + F::STAGES * WARPS);
+    if (!CLUSTER && tid == THREADS - 1 && stop < sh.line_end)
+      sh.piece[~pieces & 1] = piece_after<UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.piece[pieces & 1]);   // (while the copies are under way)
     for (; unit < unit1; unit += WARPS) {
       const uint32_t stage = taken % F::STAGES;
       dead = !wait.all(full + 8 * stage, taken / F::STAGES & 1u);
@@ -410,6 +422,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
           *reinterpret_cast<float4*>(sums + (warp * FEW_ROWS + g + 8 * r) * F::O_ROW + 32 * c + 8 * t + 4 * half) =
               make_float4(o[4 * c][2 * r + half], o[4 * c + 1][2 * r + half], o[4 * c + 2][2 * r + half], o[4 * c + 3][2 * r + half]);
     __syncthreads();
+    const int row0 = pc.job.y, nr = min(FEW_ROWS, pc.job.w * group - row0);
     const bool complete = !CLUSTER && u == pc.begin && stop == pc.end;
     float* const shared_o = sums + WARPS * FEW_ROWS * F::O_ROW;              // of a cluster's CTA: its sums, then its maxima
     float2* const shared_ml = reinterpret_cast<float2*>(shared_o + FEW_ROWS * P);
@@ -480,6 +493,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (copies go over the sums next)
     __syncthreads();
     u = stop;
+    ++pieces;
   }
   if (tid == 0 && !told) tell_none(a, cta);
 }

@@ -95,18 +95,13 @@ struct Piece {
   Span span;
   long long begin, end;                // the (tile, head)'s units in the line (u may be before: of the extra ones)
 };
+// .. of those in segment `seg`.
 template <int THREADS, int UNIT, int ROWS, int EXTRA, class Job>
-__device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job, int n, const Schedule<THREADS>& s, long long u) {
+__device__ __forceinline__ Piece piece_of(const AttendArgs& a, const Job& job, int n, const Schedule<THREADS>& s, int seg, long long u) {
   const int heads = a.c.heads;
-  int lo = 0, hi = THREADS;            // segment: the last one with sums * heads <= u
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (s.sums[mid] * heads <= u) lo = mid;
-    else hi = mid;
-  }
-  long long at = s.sums[lo] * heads;
+  long long at = s.sums[seg] * heads;
   Piece p;
-  int t = lo * s.per;
+  int t = seg * s.per;
   for (;; ++t) {
     p.job = job(t);
     p.span = span_of(a, p.job, ROWS);
@@ -121,6 +116,32 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job,
     at += cost * heads;
   }
   p.tile = t;
+  return p;
+}
+template <int THREADS, int UNIT, int ROWS, int EXTRA, class Job>
+__device__ __forceinline__ Piece find_piece(const AttendArgs& a, const Job& job, int n, const Schedule<THREADS>& s, long long u) {
+  int lo = 0, hi = THREADS;            // segment: the last one with sums * heads <= u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (s.sums[mid] * a.c.heads <= u) lo = mid;
+    else hi = mid;
+  }
+  return piece_of<THREADS, UNIT, ROWS, EXTRA>(a, job, n, s, lo, u);
+}
+// The piece after `p`; an empty one at its end where there is none.
+template <int UNIT, int ROWS, int EXTRA, class Job>
+__device__ __forceinline__ Piece piece_after(const AttendArgs& a, const Job& job, int n, Piece p) {
+  long long cost = p.end - p.begin + EXTRA;
+  if (++p.head == a.c.heads) {
+    p.head = 0;
+    for (cost = 0; cost == 0 && ++p.tile < n;) {
+      p.job = job(p.tile);
+      p.span = span_of(a, p.job, ROWS);
+      cost = cost_of<UNIT, EXTRA>(units_of<UNIT>(p.span, p.job, a.pl.group));
+    }
+  }
+  p.begin = cost > 0 ? p.end + EXTRA : p.end;
+  p.end += cost;
   return p;
 }
 // CTAs that get work: at least `least` units each.

@@ -1,21 +1,23 @@
 // The end of attention over the cache where a row's positions were shared out over several CTAs (cache_schedule.cuh):
 //   out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,  M = max_c m_c,  over the CTAs c in their order.
-// Bound: latency.  Few rows are shared out over many CTAs: four warps take a row, every fourth part each with eight loads
-// under way, and add up in shared memory (a warp that took the 55 parts of a request of 32768 tokens one after the other
-// needed 32 us).  Many rows have few parts: a warp takes four rows at once, two parts of each under way.
+// Bound: latency.  Few rows are shared out over many CTAs: a block of four warps takes a row, every fourth part each with four
+// loads under way, and adds up in shared memory (a warp that took the 55 parts of a request of 32768 tokens one after the
+// other needed 32 us).  Many rows have few parts: a warp takes two rows at once, two parts of each under way.  Small blocks of
+// few registers, so that all of them are there when the attention ends (64 ragged requests of 3000 tokens on average, the whole
+// call: 76.5 us; 80 with blocks of four rows, of which an SM holds one; 32 requests with 4 new rows each: 62 and 70).
 #include "cache.h"
 
 namespace admmq {
 namespace {
 
 constexpr float LN2 = 0.693147180559945309f;
-constexpr int SLOTS = 4;             // groups of WPR warps of a block
 
-// tile_rows: rows of a tile.  WPR warps to RPW rows, AT_ONCE parts of them at once.
-template <int WPR, int RPW, int AT_ONCE>
+// tile_rows: rows of a tile.  H: 128-value columns of a row.  SLOTS groups of WPR warps, each with RPW rows, AT_ONCE parts of them
+// at once.
+template <int H, int SLOTS, int WPR, int RPW, int AT_ONCE>
 __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_constant__ AttendArgs a, int tile_rows) {
   static_assert(WPR == 1 || RPW == 1, "one or the other");
-  __shared__ __align__(16) float sums[WPR > 1 ? SLOTS : 1][WPR][256];
+  __shared__ __align__(16) float sums[WPR > 1 ? SLOTS : 1][WPR][128 * H];
   __shared__ float totals[SLOTS][WPR];
   pdl_launch();
   pdl_wait();
@@ -29,17 +31,18 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
   // row r of part i: slot 1 of its CTA where the (tile, head) begins, 0 after
   // (numbers of 32 bits: a few hundred CTAs' rows of at most 256 values)
   auto row_of = [&](int i, int r) { return (2 * (first + i) + (i == 0)) * tile_rows + r; };
-  const bool on[2] = {4 * lane < d, 4 * lane + 128 < d};
+  auto on = [&](int c) { return 4 * lane + 128 * c < d; };
   float m[RPW], l[RPW];
-  float4 acc[RPW][2];
+  float4 acc[RPW][H];
 #pragma unroll
   for (int q = 0; q < RPW; ++q) {
     m[q] = -INFINITY;
     l[q] = 0.0f;
-    acc[q][0] = acc[q][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int c = 0; c < H; ++c) acc[q][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   if (r0 < nr) {
-    float4 x[AT_ONCE][RPW][2];
+    float4 x[AT_ONCE][RPW][H];
     float2 ml[AT_ONCE][RPW];
     auto fetch = [&](int i0) {
 #pragma unroll
@@ -51,8 +54,8 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
           ml[e][q] = i < parts ? a.part_ml[row] : make_float2(-INFINITY, 0.0f);
           const float* src = a.part + (unsigned)(row * p + 4 * lane);
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            x[e][q][c] = on[c] && i < parts ? *reinterpret_cast<const float4*>(src + 128 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c = 0; c < H; ++c)
+            x[e][q][c] = on(c) && i < parts ? *reinterpret_cast<const float4*>(src + 128 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     };
     float top[RPW];
@@ -73,7 +76,7 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
           const float k = exp2_fast(ml[e][q].x - (m[q] == -INFINITY ? 0.0f : m[q]));
           l[q] = fmaf(ml[e][q].y, k, l[q]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < H; ++c) {
             acc[q][c].x = fmaf(x[e][q][c].x, k, acc[q][c].x);
             acc[q][c].y = fmaf(x[e][q][c].y, k, acc[q][c].y);
             acc[q][c].z = fmaf(x[e][q][c].z, k, acc[q][c].z);
@@ -84,7 +87,7 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
   }
   if (WPR > 1) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) *reinterpret_cast<float4*>(&sums[slot][w][4 * lane + 128 * c]) = acc[0][c];
+    for (int c = 0; c < H; ++c) *reinterpret_cast<float4*>(&sums[slot][w][4 * lane + 128 * c]) = acc[0][c];
     if (lane == 0) totals[slot][w] = l[0];
     __syncthreads();
     if (w > 0) return;
@@ -92,7 +95,7 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
 #pragma unroll
     for (int v = 0; v < WPR; ++v) l[0] += totals[slot][v];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < H; ++c) {
       acc[0][c] = *reinterpret_cast<const float4*>(&sums[slot][0][4 * lane + 128 * c]);
 #pragma unroll
       for (int v = 1; v < WPR; ++v) {
@@ -112,15 +115,15 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
     const long long row = join.first_row + pr / group;
     bf16* dst = a.out + row * a.out_row + head * a.out_head + 4 * lane;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (on[c])
+    for (int c = 0; c < H; ++c)
+      if (on(c))
         *reinterpret_cast<uint2*>(dst + 128 * c) = make_uint2(float2_to_bf16x2(acc[q][c].x * inv, acc[q][c].y * inv),
                                                               float2_to_bf16x2(acc[q][c].z * inv, acc[q][c].w * inv));
     if (lane == 0 && a.lse) a.lse[row * (a.c.heads * group) + head] = l[q] == 0.0f ? -INFINITY : m[q] * LN2 + logf(l[q]);
   }
 }
 
-template <int WPR, int RPW, int AT_ONCE>
+template <int H, int SLOTS, int WPR, int RPW, int AT_ONCE>
 cudaError_t launch(const AttendArgs& a, int joins, int rows, int max_rows, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(joins, (max_rows + SLOTS * RPW - 1) / (SLOTS * RPW));
@@ -131,16 +134,19 @@ cudaError_t launch(const AttendArgs& a, int joins, int rows, int max_rows, cudaS
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, join_kernel<WPR, RPW, AT_ONCE>, a, rows);
+  return cudaLaunchKernelEx(&cfg, join_kernel<H, SLOTS, WPR, RPW, AT_ONCE>, a, rows);
+}
+template <int H>
+cudaError_t launch(const AttendArgs& a, bool many, int joins, cudaStream_t stream) {
+  return many ? launch<H, 4, 1, 2, 2>(a, joins, many_rows(a.c.p), many_rows(a.c.p), stream)
+              : launch<H, 1, 4, 1, 4>(a, joins, FEW_ROWS, a.pl.small_rows, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_join(const AttendArgs& a, bool many, int sms, cudaStream_t stream) {
-  const int rows = many ? many_rows(a.c.p) : FEW_ROWS;
   const int joins = a.by_piece ? pieces_of(a, many) : attend_ctas(a.c.p, many, sms);
-  return many ? launch<1, 4, 2>(a, joins, rows, rows, stream)
-              : launch<4, 1, 8>(a, joins, rows, a.pl.small_rows, stream);
+  return a.c.p <= 128 ? launch<1>(a, many, joins, stream) : launch<2>(a, many, joins, stream);
 }
 
 }  // namespace admmq

@@ -295,26 +295,22 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       // The rows' queries: each times a power of two, as fp16, into the operand tile; `factor` takes a row's scores to base-2
       // exponents.
       auto place_query = [&](long long place, float& factor) {
-        float top = 0.0f, other;                     // of this lane's row
+        uint32_t tops = 0;                           // of this lane's row: magnitudes are in the order of their bits
 #pragma unroll(AHEAD ? 8 : 2)
         for (int i = 0; i < QL; ++i) {
-          float t = 0.0f;
+          uint32_t t = 0;
 #pragma unroll
           for (int c = 0; c < QN; ++c) {
             const uint4 q = AHEAD ? raw[AHEAD ? i : 0]
                                   : chunk(__shfl_sync(0xffffffffu, place, RI * i + lane / QL), half * QC + c * QL + lane % QL);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = bf16x2_to_float2(w[e]);
-              t = fmaxf(t, isfinite(f.x) && isfinite(f.y) ? fmaxf(fabsf(f.x), fabsf(f.y)) : INFINITY);
-            }
+            t = __vmaxu2(__vmaxu2(t, __vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu)), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
           }
 #pragma unroll
-          for (int o = 1; o < QL; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+          for (int o = 1; o < QL; o <<= 1) t = __vmaxu2(t, __shfl_xor_sync(0xffffffffu, t, o));
           t = __shfl_sync(0xffffffffu, t, lane % RI * QL);
-          if (lane / RI == i) top = t;
+          if (lane / RI == i) tops = t;
         }
+        float top = __uint_as_float(min(max(tops << 16, tops & 0xffff0000u), 0x7f800000u)), other;   // (infinity for NaN)
         if (!swap(top, other)) return false;
         top = fmaxf(top, other);
         float inv;

@@ -161,21 +161,16 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       const int r = tid >> 3, sub = tid & 7, pr = row0 + r, token = pr / group, head = pc.head * group + pr % group;
       const bf16* src = a.q + (long long)(pc.job.z + token) * a.q_row + head * a.q_head;
       uint2 raw[P / 32];
-      float top = 0.0f;
-      bool finite = true;
+      uint32_t tops = 0;                             // magnitudes are in the order of their bits
 #pragma unroll
       for (int j = 0; j < P / 32; ++j) {
         const int at = 4 * (sub + 8 * j);
         raw[j] = r < nr && at < d ? __ldg(reinterpret_cast<const uint2*>(src + at)) : make_uint2(0, 0);
-        const float2 x = bf16x2_to_float2(raw[j].x), y = bf16x2_to_float2(raw[j].y);
-        top = fmaxf(top, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
-        finite &= isfinite(x.x) && isfinite(x.y) && isfinite(y.x) && isfinite(y.y);
+        tops = __vmaxu2(tops, __vmaxu2(raw[j].x & 0x7fff7fffu, raw[j].y & 0x7fff7fffu));
       }
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        finite &= __shfl_xor_sync(0xffffffffu, (int)finite, o) != 0;
-      }
+      for (int o = 1; o < 8; o <<= 1) tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+      const float top = __uint_as_float(min(max(tops << 16, tops & 0xffff0000u), 0x7f800000u));   // (infinity for NaN)
       float inv;
       const float up = pow2_scale_for(top, &inv);
 #pragma unroll
@@ -186,7 +181,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
         dst[0] = pack_f16(x.x * up, x.y * up);
         dst[2] = pack_f16(y.x * up, y.y * up);
       }
-      if (sub == 0) sh.row_scale[r] = finite ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
+      if (sub == 0) sh.row_scale[r] = top < INFINITY ? a.scale_log2 * inv : __int_as_float(0x7fc00000);
     }
     __syncthreads();
     const float f0 = sh.row_scale[g], f1 = sh.row_scale[g + 8];

@@ -46,8 +46,8 @@ size_t admmq_cache_scale_bytes(int n_pages, int kv_heads, int head_dim, int page
  * Request i has lengths[i] adjacent rows, at its positions held[i] .. held[i] + lengths[i] - 1; its position p is token
  * p % page_size of page tables[i][p / page_size].  lengths are the host's, tables and held the device's (read when the
  * kernels run, so a captured call follows them).  A request with held < 0 takes no part: nothing of it is written, its
- * rows read as zero.  tables and held may not change while a call runs.  One that does not fit its table raises ADMMQ_ERR_SHAPE in d_status and takes no part either, and
- * so does a page outside [0, n_pages), which is not accessed.
+ * rows read as zero.  One that does not fit its table raises ADMMQ_ERR_SHAPE in d_status and takes no part either, and so
+ * does a page outside [0, n_pages), which is not accessed.  tables and held may not change while a call runs.
  * d_index: int32 buffer of admmq_cache_plan_ints entries that admmq_cache_plan_fill fills on the host (no CUDA call is
  * made) and the caller copies to the device.  group: query heads a key head (for attend). */
 typedef struct {

@@ -184,6 +184,15 @@ def test_tables_far_longer_than_the_requests(lengths, held, heads, group, d, pag
     s.check_attend(window, q=q)
 
 
+@pytest.mark.parametrize("n,heads,d", [(1, 1, 128), (2, 8, 128), (5, 8, 64), (3, 9, 128), (9, 8, 128), (13, 8, 64), (27, 8, 128),
+                                       (50, 8, 128), (50, 8, 64), (7, 8, 192), (14, 8, 256), (25, 8, 256)])
+def test_numbers_of_requests(n, heads, d):
+    held = [(29 * i + 61) % 400 for i in range(n - 1)] + [970]              # a long one: CTAs together from 16 down to one
+    s = Setup([1] * n, held, heads, d, 64, seed=n, group=2)
+    s.new_rows()
+    s.check_attend()
+
+
 def test_one_long_request_is_split_and_joined():
     s = Setup([1], [20000], 2, 128, 128, group=8, seed=3)                   # (over the clusters' positions)
     s.new_rows()

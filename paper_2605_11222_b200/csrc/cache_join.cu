@@ -19,8 +19,9 @@ __global__ void __launch_bounds__(32 * WPR * SLOTS) join_kernel(const __grid_con
   static_assert(WPR == 1 || RPW == 1, "one or the other");
   __shared__ __align__(16) float sums[WPR > 1 ? SLOTS : 1][WPR][128 * H];
   __shared__ float totals[SLOTS][WPR];
-  pdl_launch();
   pdl_wait();
+  pdl_launch();                                      // (not before: the next call's CTAs would come while the attention still
+                                                     // has its places; two calls over 2 x 100001 tokens in turn 103 us each, 78 so)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = warp / WPR, w = warp % WPR;
   const int r0 = (blockIdx.y * SLOTS + slot) * RPW, p = a.c.p, d = a.c.d;
   const Join join = a.joins[blockIdx.x];

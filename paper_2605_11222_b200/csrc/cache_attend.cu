@@ -1,8 +1,8 @@
 // Attention of a few rows over the 8-bit cache: one new token of a request, or a few drafted ones.
 //   z_j = scale q . k_j,  out = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m)
 //
-// Bound: reading the cache, once (128 requests of 4300 tokens on average, 32 query and 8 key heads of 128: 254 us, 6.1 TB/s),
-// and issue, 45 % of the slots.  A warp takes 32 positions (two blocks; one of heads of more than 128) at a time.  Their codes
+// Bound: reading the cache, once (128 requests of 6000 tokens, 32 query and 8 key heads of 128: 250 us, 6.3 TB/s), and issue,
+// 47 % of the slots; short calls the 6 us before the first codes are there and the 5 us of the join.  A warp takes 32 positions (two blocks; one of heads of more than 128) at a time.  Their codes
 // come as a bulk copy a block into a ring of its own in shared memory, in the order of the second operand of m16n8k16 products
 // (16 bytes a lane, 512 a warp and load), while those before are worked on: 192 KB an SM.  (Codes loaded into registers a step
 // ahead instead left room for eight warps an SM, which ran at 4.2 TB/s.)  The 16 rows of the product are the query heads of one

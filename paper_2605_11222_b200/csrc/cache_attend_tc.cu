@@ -18,7 +18,7 @@
 //   warp 21      finds the CTA's pieces of the work, ahead of the others (22 and 23: none)
 // Work is shared out in equal parts (cache_schedule.cuh), a CTA an SM.
 // Bound: exponentials (16 a cycle and SM: 2048 cycles for 256 x 128) and the tensor cores (2048 as well), overlapped.  Measured, 32
-// query and 8 key heads of 128: 2048 rows over 30720 1067 us (998 TFLOP/s, 2.5 us or some 4700 cycles a step), a prompt of 8192
+// query and 8 key heads of 128: the last 2048 rows of 32768 1067 us (998 TFLOP/s, 2.5 us or some 4700 cycles a step), a prompt of 8192
 // 618 us (889).  Tensor and exponential pipes are busy 44 % of the time each, the schedulers 50 % (9850 warp instructions a
 // step): what is left is the chain scores, exponents, weights, product of a track, of which only two are under way.  A
 // polynomial in place of a quarter of the exponentials cost 14 %.  A CTA's first

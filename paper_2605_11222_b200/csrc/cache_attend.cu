@@ -1,12 +1,13 @@
 // Attention of a few rows over the 8-bit cache: one new token of a request, or a few drafted ones.
 //   z_j = scale q . k_j,  out = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m)
 //
-// Bound: reading the cache, once (128 requests of 6000 tokens, 32 query and 8 key heads of 128: 250 us, 6.3 TB/s), and issue,
-// 47 % of the slots; short calls the 6 us before the first codes are there and the 5 us of the join.  A warp takes 32 positions (two blocks; one of heads of more than 128) at a time.  Their codes
-// come as a bulk copy a block into a ring of its own in shared memory, in the order of the second operand of m16n8k16 products
-// (16 bytes a lane, 512 a warp and load), while those before are worked on: 192 KB an SM.  (Codes loaded into registers a step
-// ahead instead left room for eight warps an SM, which ran at 4.2 TB/s.)  The 16 rows of the product are the query heads of one
-// key head, of one token or of several; where fewer are in use the product's other rows cost nothing that memory would not.
+// Bound: reading the cache, once (128 requests of 6000 tokens, 32 query and 8 key heads of 128: 250 us, 6.3 TB/s), and
+// issue, 47 % of the slots; short calls the 6 us before the first codes are there and the 5 us of the join.  A warp takes
+// 32 positions (two blocks; one of heads of more than 128) at a time.  Their codes come as a bulk copy a block into a ring
+// of its own in shared memory, in the order of the second operand of m16n8k16 products (16 bytes a lane, 512 a warp and
+// load), while those before are worked on: 192 KB an SM.  (Codes loaded into registers a step ahead instead left room for
+// eight warps an SM, which ran at 4.2 TB/s.)  The 16 rows of the product are the query heads of one key head, of one token
+// or of several; where fewer are in use the product's other rows cost nothing that memory would not.
 // Codes become fp16 by placing them in the mantissa of 1024 + (code + 128) and subtracting 1152: exact, two instructions
 // for two.  Scales stay out of the products: the key scale multiplies the finished score, and the value scale s_b of a block
 // enters the exponent, w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m'), with m' near the running maximum of that
@@ -254,8 +255,8 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       for (int i = 0; i < F::STAGES; ++i) ahead[i] = fetch(unit + i * WARPS, n[i]);
     }
     Pages next = look(unit + F::STAGES * WARPS);
-    if (!CLUSTER && tid == THREADS - 1 && stop < sh.line_end)
-      sh.piece[~pieces & 1] = piece_after<UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.piece[pieces & 1]);   // (while the copies are under way)
+    if (!CLUSTER && tid == THREADS - 1 && stop < sh.line_end)   // (while the copies are under way)
+      sh.piece[~pieces & 1] = piece_after<UNIT, FEW_ROWS, EXTRA>(a, job, a.pl.n_small, sh.piece[pieces & 1]);
     for (; unit < unit1; unit += WARPS) {
       const uint32_t stage = taken % F::STAGES;
       dead = !wait.all(full + 8 * stage, taken / F::STAGES & 1u);

@@ -784,6 +784,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       long long u = cta < ctas ? line_at(total, cta, ctas) : 0;
       const long long line_end = cta < ctas ? line_at(total, cta + 1, ctas) : 0;
       bool told = false;                             // of a (tile, head) that others end
+      // Once a wait has run out nobody takes pieces any more; the line is walked to its end all the same, since the join
+      // that follows goes by what is told of every (tile, head).
+      bool heard = true;
       Piece f;
       for (uint32_t n = 0;; ++n) {
         PieceJob p = {};
@@ -827,13 +830,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             u = stop;
           }
         }
-        if (!wait.all(p_empty + 8 * (n % PIECE_SLOTS), (n / PIECE_SLOTS & 1u) ^ 1u)) break;
-        if (lane == 0) {
+        heard = heard && wait.all(p_empty + 8 * (n % PIECE_SLOTS), (n / PIECE_SLOTS & 1u) ^ 1u);
+        if (heard && lane == 0) {
           pieces[n % PIECE_SLOTS] = p;
           mbar_arrive(p_full + 8 * (n % PIECE_SLOTS));
         }
         __syncwarp();
         if (p.steps == 0) break;
+        if (!heard) continue;
         // its queries into the L2 cache: fetched when the piece before ends, they would keep the softmax waiting for memory
         for (int i = lane; n > 0 && i < TILE && p.row0 + i < p.packed; i += 32) {
           const int pr = p.row0 + i, g = a.pl.group;

@@ -1,0 +1,61 @@
+"""GPU tests of the 8-bit cache where attention over it meets the ends of its ranges: pieces of calls whose waits run out,
+blocks of zeros, weights far below a row's largest, pages behind a window, queries near zero."""
+import ctypes as C
+
+import pytest
+import torch
+
+from tests.test_gpu_cache import DEV, _gen
+
+pytestmark = pytest.mark.gpu
+
+
+def test_waits_that_run_out_leave_nothing_to_be_joined_untold():
+    """A call whose joins go by (tile, head), some CTAs with more of them than wait to be taken at once: when the waits
+    run out, all of them have been told to the join, which uses what it finds as indexes.  The workspace holds harmless entries
+    (nothing to be joined) with a mark where a told one has zeros."""
+    from paper_2605_11222_b200 import adapt, kvcache
+    from paper_2605_11222_b200.binding import ERR_TIMEOUT, AdmmqError
+    heads, group, d, page, short, at = 8, 4, 64, 64, 17, 60000
+    lengths, held = [40] * (short + 1), [at] + [0] * short
+    wide = -(-(at + 40) // page)
+    tables = [list(range(wide))] + [[wide + i] + [0] * (wide - 1) for i in range(short)]
+    cache = kvcache.KVCache(wide + short, heads, d, page, DEV)
+    cache.codes.random_(1, 256, generator=_gen(1))
+    cache.scale.fill_(0.01)
+    plan = kvcache.CachePlan(lengths, held, tables, group, DEV)
+    pieces = (short + 1) * heads                     # 160 packed rows: one tile of many rows a request
+    assert plan._c.n_small == 0 and plan._c.n_big == short + 1
+    ctas = torch.cuda.get_device_properties(DEV).multi_processor_count
+    assert pieces <= ctas
+    q = torch.randn(plan.n_rows, heads * group, d, generator=_gen(2), device=DEV).bfloat16()
+    want = cache.attend(q, plan)
+    adapt.check_device_status(DEV)
+
+    lib = kvcache._library()
+    nbytes = lib.admmq_cache_attend_workspace(cache._ref, plan._ref)
+    work = torch.zeros(nbytes // 4, dtype=torch.int32, device=DEV)
+    entries = work[: 8 * pieces].view(pieces, 8)     # first, last, head, row0, first row, rows, two of padding
+    entries[:, 6:] = 77
+    out, lse = torch.zeros_like(q), torch.zeros(plan.n_rows, heads * group, device=DEV)
+
+    def call():
+        adapt._call(lib.admmq_cache_attend, "admmq_cache_attend", 0, cache._ref, plan._ref, d ** -0.5, 0, q.data_ptr(), heads * group * d,
+                    d, out.data_ptr(), heads * group * d, d, lse.data_ptr(), work.data_ptr(), C.c_size_t(nbytes), cache._status)
+
+    assert lib.admmq_test_linear_set_wait(2_000_000, 1) == 0
+    try:
+        call()
+        with pytest.raises(AdmmqError) as e:
+            adapt.check_device_status(DEV)
+        assert e.value.status == ERR_TIMEOUT
+    finally:
+        assert lib.admmq_test_linear_set_wait(2_000_000_000, 0) == 0
+    told = entries.cpu()
+    assert (told[:, 6:] == 0).all()
+    assert (told[:, 0] >= 0).all() and (told[:, 1] >= told[:, 0]).all() and (told[:, 1] < ctas).all()
+    assert told[:, 2].tolist() == [i % heads for i in range(pieces)] and (told[:, 3] == 0).all()
+    assert told[:, 4].tolist() == [40 * (i // heads) for i in range(pieces)] and (told[:, 5] == 160).all()
+    call()                                           # and the same workspace serves the next call
+    adapt.check_device_status(DEV)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

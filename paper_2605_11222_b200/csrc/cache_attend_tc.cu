@@ -128,12 +128,17 @@ __device__ __forceinline__ void fewer_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
+// A value with a tag beside it, as one access of 64 bits: the elements of a vector access have no order, so that the tag could
+// be seen before its value.
+__device__ __forceinline__ void post_swap(uint32_t to, uint32_t tag, float value) {
+  asm volatile("st.volatile.shared.b64 [%0], %1;" ::"r"(to), "l"((uint64_t)tag << 32 | __float_as_uint(value)) : "memory");
+}
 // Waits, within the limit, for the word with the tag.
 __device__ __forceinline__ bool poll_swap(uint32_t from, uint32_t tag, float& value, const WarpWait& wait) {
-  uint32_t v, t;
+  uint64_t v;
   auto look = [&] {
-    asm volatile("ld.volatile.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v), "=r"(t) : "r"(from) : "memory");
-    return __all_sync(0xffffffffu, t == tag) != 0;
+    asm volatile("ld.volatile.shared.b64 %0, [%1];" : "=l"(v) : "r"(from) : "memory");
+    return __all_sync(0xffffffffu, (uint32_t)(v >> 32) == tag) != 0;
   };
   bool ok = look();
   if (!ok) {
@@ -147,7 +152,7 @@ __device__ __forceinline__ bool poll_swap(uint32_t from, uint32_t tag, float& va
       }
     }
   }
-  value = __uint_as_float(v);
+  value = __uint_as_float((uint32_t)v);
   return ok;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -266,8 +271,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
       const uint32_t swap_at = smem_u32(swapped) + (x * ROWS + r) * 8;
       auto post = [&](float mine) {
         ++swaps;
-        const uint32_t to = swap_at + ((swaps & 1u) * 2 + half) * (2 * ROWS * 8);
-        asm volatile("st.volatile.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(__float_as_uint(mine)), "r"(swaps) : "memory");
+        post_swap(swap_at + ((swaps & 1u) * 2 + half) * (2 * ROWS * 8), swaps, mine);
       };
       auto answer = [&](float& other) {
         return poll_swap(swap_at + ((swaps & 1u) * 2 + (half ^ 1)) * (2 * ROWS * 8), swaps, other, wait);

@@ -59,3 +59,28 @@ def test_waits_that_run_out_leave_nothing_to_be_joined_untold():
     call()                                           # and the same workspace serves the next call
     adapt.check_device_status(DEV)
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("d", [64, 128, 192])
+def test_references_that_rise_at_every_step_give_the_same_bits(d):
+    """Scores that go on growing make the two threads of a row agree on a new reference again and again: fifty calls of three
+    requests at once, one result."""
+    from paper_2605_11222_b200 import adapt, kvcache
+    lengths, held, page = [150, 70, 200], [3000, 1000, 0], 64
+    total = [n + p for n, p in zip(lengths, held)]
+    need = [-(-n // page) for n in total]
+    tables = [[sum(need[:i]) + j if j < need[i] else 0 for j in range(max(need))] for i in range(3)]
+    cache, g = kvcache.KVCache(sum(need), 4, d, page, DEV), _gen(d)
+    direction = torch.randn(4, d, generator=g, device=DEV)
+    at = torch.cat([torch.arange(n, device=DEV) for n in total])[:, None, None]
+    k = 0.1 * torch.randn(sum(total), 4, d, generator=g, device=DEV) + direction * (at / 40.0)
+    cache.write(k.bfloat16(), torch.randn(sum(total), 4, d, generator=g, device=DEV).bfloat16(),
+                kvcache.CachePlan(total, [0] * 3, tables, device=DEV))
+    plan = kvcache.CachePlan(lengths, held, tables, 2, DEV)
+    q = direction.repeat_interleave(2, 0) + 0.3 * torch.randn(plan.n_rows, 8, d, generator=g, device=DEV)
+    q = q.bfloat16()
+    want = cache.attend(q, plan)
+    got = [cache.attend(q, plan) for _ in range(50)]
+    adapt.check_device_status(DEV)
+    assert torch.isfinite(want[0].float()).all()
+    assert all(torch.equal(o, want[0]) and torch.equal(l, want[1]) for o, l in got)

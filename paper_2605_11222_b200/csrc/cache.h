@@ -75,6 +75,19 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Exponents of weights take log2 of the block's value scale, the sum of weights its reciprocal.  A block whose values are all zero
+// (scale 0) adds nothing to the result, so it counts with a scale below any that a block can have (2^-40 / 127): its weights
+// are in the sum as they should be, and never set a reference at which those of other blocks would have no bits left.
+constexpr float LOG2_SCALE_OF_ZEROS = -47.0f, INV_SCALE_OF_ZEROS = 140737488355328.0f;   // 2^47
+struct ValueScale {
+  float log2, inv;
+};
+__device__ __forceinline__ ValueScale value_scale(float s) {
+  if (s == 0.0f) return {LOG2_SCALE_OF_ZEROS, INV_SCALE_OF_ZEROS};
+  // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
+  return {__log2f(s), s == s ? __fdividef(1.0f, s) : 1.0f};
+}
+
 struct StoreArgs {
   CacheView c;
   PlanView pl;

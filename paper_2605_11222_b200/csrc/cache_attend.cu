@@ -304,9 +304,9 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       float most0 = -INFINITY, most1 = -INFINITY, inv_s[NB];   // of this lane's four positions of a block
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const float vs = sc[b].y == 0.0f ? 1.0f : sc[b].y, lv = __log2f(vs), k0 = f0 * sc[b].x, k1 = f1 * sc[b].x;
-        // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
-        inv_s[b] = vs == vs ? __fdividef(1.0f, vs) : 1.0f;
+        const ValueScale vs = value_scale(sc[b].y);
+        const float lv = vs.log2, k0 = f0 * sc[b].x, k1 = f1 * sc[b].x;
+        inv_s[b] = vs.inv;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll

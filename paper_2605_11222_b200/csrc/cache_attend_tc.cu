@@ -688,10 +688,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 make_uint4(two_codes<false>(c.z), two_codes<true>(c.z), two_codes<false>(c.w), two_codes<true>(c.w));
           }
         if (w == 0 && lane < BLOCKS) {
-          const float vs = now.scale.y == 0.0f ? 1.0f : now.scale.y;
-          // (no NaN for the sum of weights: a weight of NaN brings it by itself, and one that is not seen does not)
-          scales[it % SCALE_SLOTS][lane] = now.at >= 0 ? make_float4(now.scale.x, __log2f(vs), vs == vs ? __fdividef(1.0f, vs) : 1.0f, 0.f)
-                                                       : make_float4(0.f, -INFINITY, 0.f, 0.f);
+          const ValueScale vs = value_scale(now.scale.y);
+          scales[it % SCALE_SLOTS][lane] = now.at >= 0 ? make_float4(now.scale.x, vs.log2, vs.inv, 0.f) : make_float4(0.f, -INFINITY, 0.f, 0.f);
         }
         fence_async();
         __syncwarp();

@@ -5,7 +5,8 @@ import ctypes as C
 import pytest
 import torch
 
-from tests.test_gpu_cache import DEV, _gen
+from tests.cache_reference import ReferenceCache, attend64
+from tests.test_gpu_cache import DEV, Setup, _gen, _rows, _tables, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +85,42 @@ def test_references_that_rise_at_every_step_give_the_same_bits(d):
     adapt.check_device_status(DEV)
     assert torch.isfinite(want[0].float()).all()
     assert all(torch.equal(o, want[0]) and torch.equal(l, want[1]) for o, l in got)
+
+
+# packed rows of few and of many, heads of one track and of two, requests in clusters and shared out
+FORMS = [([1], 128, 300), ([1, 3], 256, 300), ([2] * 40, 64, 200), ([130], 64, 300), ([150, 70], 128, 200), ([90, 40], 192, 300)]
+
+
+@pytest.mark.parametrize("lengths,d,held", FORMS)
+@pytest.mark.parametrize("size", [1e-3, 1e-5, 1e-9])
+@pytest.mark.parametrize("zeros", [(0, 16), (32, 48), (160, 176), (0, 64), (200, 201)])
+def test_a_block_of_zero_values_leaves_its_neighbours_their_digits(lengths, d, held, size, zeros):
+    """Values of one size, and a block of them zero or below 2^-40 (its scale is 0): it has weight in the sum and none in the
+    result, and what scale the kernels take it to have must not push the others' weights out of their 16 bits."""
+    s = Setup(lengths, [0] * len(lengths), 2, d, 64, seed=d, group=2)
+    total = [n + held for n in lengths]
+    from paper_2605_11222_b200 import kvcache
+    pages, s.lists, s.padded = _tables(total, 64, 5)
+    s.cache, s.ref = kvcache.KVCache(pages, 2, d, 64, DEV), ReferenceCache(2, d, 64)
+    k, v = [_rows(s.g, sum(total), 2, d).float() for _ in "kv"]
+    at = torch.cat([torch.arange(n, device=DEV) for n in total])[:, None, None]
+    gone = (at >= zeros[0]) & (at < zeros[1])
+    v = torch.where(gone, 1e-14 * v if zeros[0] == 32 else 0.0 * v, size * v)
+    s.write(total, [0] * len(lengths), k.bfloat16(), v.bfloat16())
+    s.held = [held] * len(lengths)
+    s.plan = kvcache.CachePlan(lengths, s.held, s.padded, 2, DEV)
+    q = (0.3 * torch.randn(sum(lengths), 4, d, generator=s.g, device=DEV)).bfloat16()
+    out, lse = s.cache.attend(q, s.plan)
+    want = attend64(q, s.sequences(), lengths, s.held, 2, d ** -0.5)
+    _within(out, want[0], want[2])
+    _within(lse, want[1], want[3])
+
+
+@pytest.mark.parametrize("lengths,d", [([1], 128), ([1, 3], 256), ([130], 64), ([90], 192)])
+def test_values_that_are_all_zero(lengths, d):
+    s = Setup(lengths, [100] * len(lengths), 2, d, 64, group=2)
+    total = [n + 100 for n in lengths]
+    k, v = _rows(s.g, sum(total), 2, d), torch.zeros(sum(total), 2, d, device=DEV).bfloat16()
+    s.write(total, [0] * len(lengths), k, v)
+    q, out, lse = s.check_attend()
+    assert (out == 0).all() and torch.isfinite(lse).all()

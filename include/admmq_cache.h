@@ -78,7 +78,8 @@ admmq_status admmq_cache_read(const admmq_cache* cache, const admmq_cache_plan* 
 /* ---- Attention ------------------------------------------------------------------------------------------
  * q, out: [n_rows][kv_heads * group][head_dim] bf16 by row and head strides; query head h goes with key head h / group.
  * A row at position p sees the positions j <= p of its request that the cache holds (its own among them: write first),
- * with window > 0 those with j > p - window:
+ * with window > 0 those with j > p - window (pages with none of the positions that a request's rows see are not asked for,
+ * so those that a window has left may be gone from the tables):
  *   out = sum_j w_j v_j,  w = softmax_j(scale q . k_j),  lse [n_rows][heads] fp32 = log sum_j exp(scale q . k_j)
  * in fp32 sums; weights enter the second product as fp16, queries as fp16 after a shift by a power of two of each row
  * (exact for values within 2^-27 of the row's largest; a query with an infinity or a NaN gives a row of NaN).  Requests

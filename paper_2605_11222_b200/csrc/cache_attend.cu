@@ -209,7 +209,10 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       for (int b = 0; b < NB; ++b) {
         const int blk = NB * unit + b;
         n.p[b] = -1;
-        if (unit < unit1 && blk < n_blocks) n.p[b] = a.pl.tables[(long long)request * a.pl.max_pages + (blk >> a.c.bpp_shift)];
+        if (unit < unit1 && blk < n_blocks) {
+          n.p[b] = a.pl.tables[(long long)request * a.pl.max_pages + (blk >> a.c.bpp_shift)];
+          if (n.p[b] < 0) n.p[b] = 0x7fffffff;       // (-1 is "none", not a page that does not exist)
+        }
       }
       return n;
     };
@@ -225,7 +228,7 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       for (int b = 0; b < NB; ++b) {
         const int blk = NB * unit + b;
         f.exists[b] = (unsigned)n.p[b] < (unsigned)a.c.n_pages;
-        if (!f.exists[b] && unit < unit1 && blk < n_blocks) raise_status(a.status, ADMMQ_ERR_SHAPE);
+        if (n.p[b] >= a.c.n_pages) raise_status(a.status, ADMMQ_ERR_SHAPE);
         at[b] = f.exists[b] ? (n.p[b] * heads + key_head) * a.c.bpp + (blk & a.c.bpp - 1) : 0;
         bytes += f.exists[b] ? F::BLOCK_BYTES : 0;
         f.s[b] = f.exists[b] ? __ldg(a.c.scale + at[b]) : make_float2(0.f, 0.f);
@@ -252,6 +255,10 @@ __global__ void __launch_bounds__(THREADS, few_ctas(P)) attend_few_kernel(const 
       Pages n[F::STAGES];
 #pragma unroll
       for (int i = 0; i < F::STAGES; ++i) n[i] = look(unit + i * WARPS);
+      // (of the first step, blocks behind the window are not asked for: their pages may be gone)
+#pragma unroll
+      for (int b = 0; b + 1 < NB; ++b)
+        if (NB * unit + b < pc.span.lo / CBLOCK) n[0].p[b] = -1;
 #pragma unroll
       for (int i = 0; i < F::STAGES; ++i) ahead[i] = fetch(unit + i * WARPS, n[i]);
     }

@@ -176,11 +176,14 @@ __device__ __forceinline__ int4 job_of(const AttendArgs& a, int tile) {
   return job;
 }
 // A piece as the roles take it from shared memory.
+constexpr int SKIP_BIT = 27;                         // (positions end at 2^30, a step has at most eight blocks)
 struct PieceJob {
   int steps;                                         // 0: there are no more
   int pos;                                           // position of its first step
   int head, request, row0, first_row, packed;        // row0: packed row of the tile's first; packed: of the request in all
-  int at, hi;                                        // position of the request's first row; end of what the tile sees
+  int at;                                            // position of the request's first row
+  int blocks;                                        // end of what the tile sees, in blocks; from SKIP_BIT on: how many of the first
+                                                     // step's blocks lie behind its window
   int part;                                          // where its partial result goes; -1: it is whole
 };
 
@@ -611,14 +614,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     bool ended = false;                              // no more pieces, or a wait ran out
     auto look = [&]() {
       Look n = {-1, 0, 0, false};
+      int skip = 0;
       if (left == 0) {
         ended = ended || !take(n_piece++, pc) || pc.steps == 0;
         if (ended) return n;
         left = pc.steps;
+        skip = pc.blocks >> SKIP_BIT;                // (blocks behind the window are not asked for: their pages may be gone)
+        pc.blocks &= (1 << SKIP_BIT) - 1;
       }
       n.more = true;
       const int b = pc.pos / CBLOCK + lane;
-      if (lane < BLOCKS && b < (pc.hi + CBLOCK - 1) / CBLOCK) {
+      if (lane < BLOCKS && lane >= skip && b < pc.blocks) {
         n.page = a.pl.tables[(long long)pc.request * a.pl.max_pages + (b >> a.c.bpp_shift)];
         n.block = b & a.c.bpp - 1;
         if (n.page < 0) n.page = 0x7fffffff;         // (-1 is "none", not a page that does not exist)
@@ -823,7 +829,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             p.first_row = f.job.z;
             p.packed = f.job.w * a.pl.group;
             p.at = f.span.at;
-            p.hi = f.span.hi;
+            p.blocks = (f.span.hi + CBLOCK - 1) / CBLOCK | max(0, f.span.lo / CBLOCK - p.pos / CBLOCK) << SKIP_BIT;
             p.part = u == f.begin && stop == f.end ? -1 : 2 * cta + (u == f.begin ? 1 : 0);
             if (u == f.begin) {
               told = stop < f.end;

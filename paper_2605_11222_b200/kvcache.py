@@ -173,8 +173,8 @@ class KVCache:
     def attend(self, q: torch.Tensor, plan: CachePlan, scale: Optional[float] = None, window: int = 0,
                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(out, lse): softmax attention of q [rows, kv_heads * group, head_dim] bf16 over what each row's request holds up
-        to the row itself (written before), with window > 0 the last `window` positions of that; scale 1 / sqrt(head_dim)
-        if not given.  out like q, lse [rows, heads] fp32 the logarithm of the sum of the weights' exponentials.  Rows of
+        to the row itself (written before), with window > 0 the last `window` positions of that (pages that no row sees may be gone
+        from the tables); scale 1 / sqrt(head_dim) if not given.  out like q, lse [rows, heads] fp32 the logarithm of the sum of the weights' exponentials.  Rows of
         a request that takes no part get 0 and -inf."""
         if out is None and lse is None and plan.__class__ is CachePlan:
             r = adapt._fast.cache_attend(self._status, self._ref, plan._ref, self.codes, self.scale, plan.tables, plan.held, q,

@@ -124,3 +124,28 @@ def test_values_that_are_all_zero(lengths, d):
     s.write(total, [0] * len(lengths), k, v)
     q, out, lse = s.check_attend()
     assert (out == 0).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("lengths", [[1], [1] * 90, [3, 1], [70], [300, 1]])
+@pytest.mark.parametrize("d,window", [(64, 40), (128, 200), (256, 100)])
+@pytest.mark.parametrize("held", [500, 511, 512, 520, 543, 600])
+def test_pages_behind_the_window_may_be_gone(lengths, d, window, held):
+    """A server that frees the pages that a sliding window has left marks them as absent: nothing of a page that no row sees
+    is asked for, wherever it lies in a step of the kernels."""
+    from paper_2605_11222_b200 import adapt, kvcache
+    s = Setup(lengths, [held] * len(lengths), 1, d, 16, seed=held, group=2)
+    s.new_rows()
+    q = torch.randn(sum(lengths), 2, d, generator=s.g, device=DEV).bfloat16()
+    want = s.cache.attend(q, s.plan, window=window)
+    adapt.check_device_status(DEV)
+    first = (held - window + 1) // 16                        # the page of the first position that is seen
+    for absent in (-1, 2 ** 30):
+        gone = [[absent] * first + row[first:] for row in s.padded]
+        out, lse = s.cache.attend(q, kvcache.CachePlan(lengths, s.held, gone, 2, DEV), window=window)
+        adapt.check_device_status(DEV)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    # one page more is one that is seen
+    gone = [[-1] * (first + 1) + row[first + 1:] for row in s.padded]
+    s.cache.attend(q, kvcache.CachePlan(lengths, s.held, gone, 2, DEV), window=window)
+    with pytest.raises(adapt.AdmmqError):
+        adapt.check_device_status(DEV)

@@ -6,8 +6,8 @@
 // Both products take fp16 operands: queries times a power of two of their row, codes as they are, and weights
 //   w_j = s_b exp(z_j - m') = 2^(z_j log2 e + log2 s_b - m')
 // with the value scale s_b of the block in the exponent, so that they fit fp16 whatever the scales are; the key scale
-// multiplies the finished score.  The sum of weights takes w_j / s_b.  The reference m' is a row's maximum over the first
-// step; it is raised only after a weight has passed 2^8, which is rare, so that the accumulator is hardly ever touched
+// multiplies the finished score.  The sum of weights takes w_j / s_b in fp32.  The reference m' lies 6 below a row's maximum over
+// the first positions; it is raised only after a weight has passed 2^14, which is rare, so that the accumulator is hardly ever touched
 // between its products, and a row's weights need not wait for its maximum.
 //   warps 0-15   softmax, two threads to a row: scores from tensor memory into registers, weights back over them (the first
 //                operand of the second product), the accumulator's occasional scaling, queries in and results out
@@ -37,8 +37,12 @@ constexpr int LAUNCH_REGS = 80, SOFT_REGS = 88, CODE_REGS = 88, MMA_REGS = 40;  
 static_assert(4 * SOFT_REGS + CODE_REGS + MMA_REGS <= 6 * LAUNCH_REGS, "registers");
 constexpr int STAGES = 2, SCALE_SLOTS = 4, PIECE_SLOTS = 4;
 constexpr int EXTRA = 3;                             // a piece's start and end, in steps
-// Weights above 2^LIMIT raise the reference for the steps that follow; fp16 holds them up to 2^HARD_LIMIT.
-constexpr float LIMIT = 8.0f, HARD_LIMIT = 15.0f;
+// Weights are fp16.  The first largest of a row is 2^TOP; one above 2^LIMIT raises the reference for the steps that follow, so that
+// it is 2^TOP again, and one above 2^HARD_LIMIT at once, by a whole number, so that the step's other weights are scaled exactly.
+// So weights down to 2^-20 of the largest have 11 bits, and those down to 2^-31 some (with TOP 0 the positions behind a token with
+// nearly all the weight lost theirs).
+constexpr float TOP = 6.0f, LIMIT = 14.0f, HARD_LIMIT = 15.0f;
+__device__ __forceinline__ float whole_raise(float top) { return rintf(top - TOP); }
 constexpr float LN2 = 0.693147180559945309f;
 
 template <int P>
@@ -464,15 +468,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
               const float most = fmaxf(top, other);
               if (empty && most > -INFINITY) {
                 empty = false;
-                ref = most;
-                top -= most;
+                ref = most - TOP;
+                top -= ref;
 #pragma unroll
-                for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - most);
+                for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) - ref);
               }
             }
             peak = fmaxf(peak, top + up);
             if (__any_sync(0xffffffffu, top > HARD_LIMIT)) {
-              const float by = top > HARD_LIMIT ? top : 0.0f, f = exp2_fast(-by);
+              const float by = top > HARD_LIMIT ? whole_raise(top) : 0.0f, f = exp2_fast(-by);
               scale_weights(s_col, 16 * c, f);
               add *= f;
               up += by;
@@ -501,9 +505,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
           ok = answer(other);
           if (!ok) break;
           peak = fmaxf(peak, other);
-          raise = peak > LIMIT ? peak : 0.0f;
+          raise = peak > LIMIT ? peak - TOP : 0.0f;
           if (__any_sync(0xffffffffu, peak > HARD_LIMIT)) {   // it cannot wait for the next step
-            const float by = peak > HARD_LIMIT ? peak : 0.0f, f = exp2_fast(-by), f_step = exp2_fast(up - by);
+            const float by = peak > HARD_LIMIT ? whole_raise(peak) : 0.0f, f = exp2_fast(-by), f_step = exp2_fast(up - by);
             scale_weights(s_col, CW / 2, f_step);
             add *= f_step;
             if (it > begin) {

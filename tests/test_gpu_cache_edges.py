@@ -1,6 +1,7 @@
 """GPU tests of the 8-bit cache where attention over it meets the ends of its ranges: pieces of calls whose waits run out,
 blocks of zeros, weights far below a row's largest, pages behind a window, queries near zero."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -149,3 +150,45 @@ def test_pages_behind_the_window_may_be_gone(lengths, d, window, held):
     s.cache.attend(q, kvcache.CachePlan(lengths, s.held, gone, 2, DEV), window=window)
     with pytest.raises(adapt.AdmmqError):
         adapt.check_device_status(DEV)
+
+
+@pytest.mark.parametrize("sink", [0])
+@pytest.mark.parametrize("requests,rows,d", [(64, 1, 64), (64, 1, 128), (20, 70, 64), (20, 70, 128), (20, 70, 192)])
+def test_weights_far_below_the_largest_of_their_row_are_kept(requests, rows, d, sink):
+    """A token with nearly all of a row's weight and values of zero, in a block whose scale is that of the others: the
+    result is what the others' weights make of it, 2^-25 to 2^-27 of the largest each, 2000 of them.  More (tile, head)s
+    than CTAs, so that a CTA sees most of a row.
+
+    Tolerance, beside the rounding of the result (2^-8 of it): a weight is rounded to fp16 with its row's largest at
+    least 2^6 in the kernels' unit, so by 2^-12 of itself at most while it is above 2^-14, and below by half a step of 2^-24:
+    2^-31 of the largest, at random: six standard deviations are 6 / sqrt(3) 2^-31 sqrt(sum v^2); the exponent of a weight (some 30) has
+    2^-19 of error after a few roundings, the sums 2^-18: together 2^-17 sum w |v|."""
+    from paper_2605_11222_b200 import adapt, kvcache
+    heads, n, page = 8, 2000, 64
+    g = _gen(d + rows)
+    pages = -(-(n + rows) // page)
+    cache = kvcache.KVCache(pages, heads, d, page, DEV)
+    total = n + rows
+    # one channel carries the score: that token's is 26 powers of two above the others', give or take one
+    k, v = torch.zeros(total, heads, d, device=DEV), 0.5 + torch.rand(total, heads, d, generator=g, device=DEV)
+    k[:, :, 0] = torch.rand(total, heads, generator=g, device=DEV)
+    k[sink, :, 0] = 27.0
+    v[sink] = 0.0
+    cache.write(k.bfloat16(), v.bfloat16(), kvcache.CachePlan([total], [0], [list(range(pages))], device=DEV))
+    q = torch.zeros(requests * rows, heads, d, device=DEV)
+    q[..., 0] = 1.0
+    plan = kvcache.CachePlan([rows] * requests, [n] * requests, [list(range(pages))] * requests, 1, DEV)   # all read the same pages
+    out, lse = cache.attend(q.bfloat16(), plan, math.log(2.0))
+    adapt.check_device_status(DEV)
+    kk, vv = [x.double() for x in cache.read(kvcache.CachePlan([total], [0], [list(range(pages))], device=DEV), torch.float32)]
+    z = kk[:, :, 0].T * math.log(2.0)                                                  # [heads, positions], of any row
+    seen = torch.arange(total, device=DEV)[None] <= n + torch.arange(rows, device=DEV)[:, None]
+    w = torch.softmax(z[:, None].masked_fill(~seen, -math.inf), -1)                    # [heads, rows, positions]
+    assert (w[:, :, sink] > 0.99).all() and ((w < 2.0 ** -24).sum(-1) >= n - 1).all()
+    want = torch.einsum("hrp,phd->rhd", w, vv)
+    tiny = 6 / math.sqrt(3) * 2.0 ** -31 * (vv ** 2).sum(0).sqrt()                     # [heads, d]
+    tol = 2.0 ** -8 * want.abs() + tiny + 2.0 ** -17 * torch.einsum("hrp,phd->rhd", w, vv.abs())
+    lw = torch.logsumexp(z[:, None].masked_fill(~seen, -math.inf), -1).T
+    for i in range(requests):
+        _within(out[i * rows: (i + 1) * rows], want.cpu(), tol.cpu())
+        _within(lse[i * rows: (i + 1) * rows], lw.cpu(), torch.full_like(lw, 2.0 ** -18 * 27).cpu())

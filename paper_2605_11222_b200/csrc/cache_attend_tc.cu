@@ -413,7 +413,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             return fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]);
           };
           auto scale_weights = [&](uint32_t col, int n, float f) {   // those of this step that are there, n columns of them
-            const __half2 f2 = __float2half2_rn(f);
             tc_st_wait();
 #pragma unroll 1
             for (int c = 0; c < n; c += 8) {
@@ -422,8 +421,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
               tc_ld8_wait(o);
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&o[e]), f2);
-                o[e] = *reinterpret_cast<const uint32_t*>(&v);
+                // (in fp32: the factor itself may be below what fp16 holds, where the products are not)
+                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&o[e]));
+                o[e] = pack_f16(v.x * f, v.y * f);
               }
               tc_st8(col + c, o);
             }

@@ -152,7 +152,7 @@ def test_pages_behind_the_window_may_be_gone(lengths, d, window, held):
         adapt.check_device_status(DEV)
 
 
-@pytest.mark.parametrize("sink", [0])
+@pytest.mark.parametrize("sink", [0, 40, 100, 255, 1990])
 @pytest.mark.parametrize("requests,rows,d", [(64, 1, 64), (64, 1, 128), (20, 70, 64), (20, 70, 128), (20, 70, 192)])
 def test_weights_far_below_the_largest_of_their_row_are_kept(requests, rows, d, sink):
     """A token with nearly all of a row's weight and values of zero, in a block whose scale is that of the others: the

@@ -28,7 +28,8 @@ __device__ __forceinline__ void split_f16(float a, __half& hi, __half& lo) {
   hi = __float2half_rn(a);
   lo = __float2half_rn(a - __half2float(hi));
 }
-// Power of two S with maxabs * S in [2^13, 2^14); 1 for a zero or non-finite maximum.  *inv = 1 / S.
+// Power of two S with maxabs * S in [2^13, 2^14), or 2^126 for maxima below 2^-113; 1 for a zero or non-finite maximum.
+// *inv = 1 / S.
 __device__ __forceinline__ float pow2_scale_for(float maxabs, float* inv) {
   if (!(maxabs > 0.0f) || !isfinite(maxabs)) {
     *inv = 1.0f;
@@ -36,6 +37,7 @@ __device__ __forceinline__ float pow2_scale_for(float maxabs, float* inv) {
   }
   int e;
   frexpf(maxabs, &e);
+  e = max(e, -112);                                  // (both powers are normal numbers: no row of tiny values times infinity)
   *inv = ldexpf(1.0f, e - 14);
   return ldexpf(1.0f, 14 - e);
 }

@@ -192,3 +192,16 @@ def test_weights_far_below_the_largest_of_their_row_are_kept(requests, rows, d, 
     for i in range(requests):
         _within(out[i * rows: (i + 1) * rows], want.cpu(), tol.cpu())
         _within(lse[i * rows: (i + 1) * rows], lw.cpu(), torch.full_like(lw, 2.0 ** -18 * 27).cpu())
+
+
+@pytest.mark.parametrize("n", [1, 40, 100])
+@pytest.mark.parametrize("size", [2.0 ** -133, 2.0 ** -126, 2.0 ** -115, 2.0 ** -110, 0.0])
+def test_queries_near_zero(n, size):
+    """A row of queries down to bf16's smallest numbers: its scores are zero as far as they matter, its weights equal."""
+    s = Setup([n], [100], 2, 128, 64, group=2)
+    s.new_rows()
+    q = torch.randn(n, 4, 128, generator=s.g, device=DEV).bfloat16()
+    q[0, 1] = size
+    q[0, 2] = 0.0
+    q[0, 2, 5] = -size
+    s.check_attend(q=q)

@@ -28,11 +28,10 @@ struct CacheView {
 struct PlanView {
   const int* tables;
   const int* held;
-  const int* row_start;              // [n + 1]
   const int4* blocks;                // (request, i, first row, rows): the i-th block that its rows touch, if they touch so many
   const int4* small;                 // tiles of packed rows: (request, first packed row, first row, rows of the request)
   const int4* big;
-  int n, max_pages, group, n_blocks, n_small, n_big;
+  int max_pages, group, n_blocks, n_small, n_big;
   int small_rows;                    // most packed rows that a small tile holds
   long long capacity;                // positions of a table
 };

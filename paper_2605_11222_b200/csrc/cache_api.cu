@@ -44,6 +44,8 @@ long long blocks_of(long long rows) { return rows > 0 ? (rows + 2 * CBLOCK - 2) 
 long long tiles_of(long long packed, int rows) { return (packed + rows - 1) / rows; }
 bool is_few(long long packed, long long all) { return packed <= MOST_FEW || all <= MOST_FEW_ALONE; }
 long long round4(long long n) { return (n + 3) & ~3LL; }
+// The index of a call's rows: the first row of every request and their number (for the caller; the kernels find it in the
+// entries below), then an entry of four for every block that rows may touch and for every tile.
 struct IndexSizes {
   long long rows, blocks, small, big, small_rows;   // small_rows: most packed rows that a small tile holds
   long long ints(int n) const { return round4(n + 1) + 4 * (blocks + small + big); }
@@ -74,8 +76,8 @@ admmq_status view_plan(const admmq_cache_plan* p, const CacheView& c, PlanView* 
   if (!aligned(p->d_tables, 4) || !aligned(p->d_held, 4) || !aligned(p->d_index, 16)) return ADMMQ_ERR_INVALID_ARG;
   const int* at = p->d_index + round4(p->n_requests + 1);
   const int* tiles = at + 4LL * p->n_blocks;
-  *v = {p->d_tables, p->d_held, p->d_index, (const int4*)at, (const int4*)tiles, (const int4*)tiles + p->n_small,
-        p->n_requests, p->max_pages, p->group, p->n_blocks, p->n_small, p->n_big, p->small_rows, capacity};
+  *v = {p->d_tables, p->d_held, (const int4*)at, (const int4*)tiles, (const int4*)tiles + p->n_small,
+        p->max_pages, p->group, p->n_blocks, p->n_small, p->n_big, p->small_rows, capacity};
   return ADMMQ_OK;
 }
 

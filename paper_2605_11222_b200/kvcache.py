@@ -59,10 +59,21 @@ def _library():
     return _lib
 
 
+def _host(x, dtype, name):
+    """A sequence as an array of whole numbers; what does not fit, or lists of different lengths, is refused."""
+    try:
+        a = np.ascontiguousarray(np.asarray(x, dtype=dtype))
+        fits = x.__class__ is list or bool((a == np.asarray(x)).all())   # (of a list's numbers numpy refuses those that do not,
+    except (TypeError, ValueError, OverflowError):                       # an array's it wraps around)
+        fits = False
+    _need(fits, f"CachePlan: {name}: whole numbers of {8 * np.dtype(dtype).itemsize} bits", B.ERR_SHAPE)
+    return a
+
+
 def _ints(x, shape, device, name):
-    """An int32 tensor on the device, used in place; a sequence is copied there."""
+    """An int32 tensor on the device, used in place; an array is copied there."""
     if not torch.is_tensor(x):
-        x = torch.from_numpy(np.ascontiguousarray(np.asarray(x, dtype=np.int32))).to(device)
+        x = torch.from_numpy(x).to(device)
     _need(x.dtype is torch.int32 and x.is_cuda and x.is_contiguous(), f"CachePlan: contiguous int32 {name} on a GPU")
     _need(x.dim() == len(shape) and all(s is None or s == n for s, n in zip(shape, x.shape)), f"CachePlan: {name} {shape}",
           B.ERR_SHAPE)
@@ -79,7 +90,7 @@ class CachePlan:
 
     def __init__(self, lengths: Sequence[int], held: Union[torch.Tensor, Sequence[int]],
                  tables: Union[torch.Tensor, Sequence[Sequence[int]]], group: int = 1, device="cuda"):
-        lengths = np.ascontiguousarray(np.asarray(lengths, dtype=np.int64).reshape(-1))
+        lengths = _host(lengths, np.int64, "lengths").reshape(-1)
         lib, n = _library(), len(lengths)
         size = lib.admmq_cache_plan_ints(lengths.ctypes.data, n, group) if 0 < n < 2 ** 31 and 0 < group < 2 ** 31 else -1
         _need(size >= 0, "CachePlan: at least one request, no negative length, at most 2^30 rows, group 1 to 1024", B.ERR_SHAPE)
@@ -87,6 +98,10 @@ class CachePlan:
         host = np.empty(size, dtype=np.int32)
         st = lib.admmq_cache_plan_fill(lengths.ctypes.data, n, group, host.ctypes.data, C.addressof(self._c))
         _need(st == B.OK, "admmq_cache_plan_fill", st)
+        if not torch.is_tensor(tables):
+            tables = _host(tables, np.int32, "tables")
+        if not torch.is_tensor(held):
+            held = _host(held, np.int32, "held")
         device = tables.device if torch.is_tensor(tables) else held.device if torch.is_tensor(held) else device
         self.tables, self.held = _ints(tables, (n, None), device, "tables"), _ints(held, (n,), device, "held")
         self.device, self.index = self.tables.device, self.tables.get_device()

@@ -139,3 +139,22 @@ def test_calls_refuse_bad_arguments(kv, name):
     else:
         assert call(a0=2) == B.ERR_INVALID_ARG
     assert call(plan=_plan(kv, lengths=(0, 0))) == B.OK                     # no rows: nothing to do
+
+
+def test_numbers_of_a_plan_that_are_refused(kv):
+    """Held positions and pages are whole numbers of 32 bits: nothing is wrapped around."""
+    from paper_2605_11222_b200.binding import AdmmqError
+    for good in ([], [[], []], [3, -1], np.array([5, 7], np.uint8), np.array([2 ** 31 - 1, -2 ** 31]), [[1, 2], [3, 4]], range(3)):
+        a = kv._host(good, np.int32, "held")
+        assert (a == np.asarray(good)).all() and a.dtype == np.int32
+    for bad in (np.array([2 ** 32 + 5]), [np.int64(2 ** 32 + 5)], [2 ** 31], [-2 ** 31 - 1], [2 ** 70], [float("nan")], [float("inf")],
+                [[1, 2], [3]], ["one"], [None], np.array([1.5])):
+        with pytest.raises(AdmmqError):
+            kv._host(bad, np.int32, "held")
+    for bad in ([2 ** 70], [np.int64(2 ** 32 + 5)], np.array([2 ** 63 + 1], np.uint64), [[1, 2], [3]], ["one"], [None], [float("nan")]):
+        with pytest.raises(AdmmqError):
+            kv.CachePlan(bad, [0] * len(bad), [[0]] * len(bad))
+    with pytest.raises(AdmmqError):
+        kv.CachePlan([1], np.array([2 ** 32 + 5]), [[0]])
+    with pytest.raises(AdmmqError):
+        kv.CachePlan([1, 1], [0, 0], [[0, 1], [2]])

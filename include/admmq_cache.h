@@ -67,7 +67,7 @@ admmq_status admmq_cache_plan_fill(const long long* lengths, int n_requests, int
  * k, v: [n_rows][kv_heads][head_dim] fp32 or bf16 by row and head strides (elements, inner stride 1; 16-byte aligned).
  * write: the plan's rows into the cache.  A page may be written through one entry of the tables only (else its contents are
  * unspecified); pages that requests only read may be shared.
- * read: what the cache holds at the plan's rows, as scale * code rounded to the given type. */
+ * read: what the cache holds at the plan's rows, as scale * code rounded to the given type; rows and heads may not overlap. */
 admmq_status admmq_cache_write(const admmq_cache* cache, const admmq_cache_plan* plan, admmq_dtype dtype, const void* d_k,
                                long long k_row, long long k_head, const void* d_v, long long v_row, long long v_head,
                                int* d_status, void* cuda_stream);
@@ -76,7 +76,8 @@ admmq_status admmq_cache_read(const admmq_cache* cache, const admmq_cache_plan* 
                               void* cuda_stream);
 
 /* ---- Attention ------------------------------------------------------------------------------------------
- * q, out: [n_rows][kv_heads * group][head_dim] bf16 by row and head strides; query head h goes with key head h / group.
+ * q, out: [n_rows][kv_heads * group][head_dim] bf16 by row and head strides (at most 65536 heads; those of out may not overlap, nor
+ * out and q); query head h goes with key head h / group.
  * A row at position p sees the positions j <= p of its request that the cache holds (its own among them: write first),
  * with window > 0 those with j > p - window (pages with none of the positions that a request's rows see are not asked for,
  * so those that a window has left may be gone from the tables):

@@ -21,6 +21,12 @@ int log2_of(int n) {
   while ((1 << s) < n) ++s;
   return s;
 }
+// Whether the rows and heads of an output lie apart (the stride of a single one does not matter).
+bool apart(long long rows, long long row, int heads, long long head, int d) {
+  if (rows < 2) return heads < 2 || head >= d;
+  if (heads < 2) return row >= d;
+  return row >= head ? head >= d && row >= (heads - 1) * head + d : row >= d && head >= (rows - 1) * row + d;
+}
 admmq_status check_sizes(int n_pages, int kv_heads, int head_dim, int page_size) {
   if (n_pages < 1 || kv_heads < 1 || kv_heads > MAX_HEADS) return ADMMQ_ERR_SHAPE;
   if (head_dim < 16 || head_dim > ADMMQ_CACHE_MAX_HEAD || head_dim % 16) return ADMMQ_ERR_SHAPE;
@@ -91,6 +97,8 @@ admmq_status store(bool write, const admmq_cache* cache, const admmq_cache_plan*
   if (dtype != ADMMQ_F32 && dtype != ADMMQ_BF16) return ADMMQ_ERR_INVALID_ARG;
   const int e = dtype == ADMMQ_BF16 ? 8 : 4;
   if (k_row % e || k_head % e || v_row % e || v_head % e) return ADMMQ_ERR_SHAPE;
+  if (!write && !(apart(plan->n_rows, k_row, a.c.heads, k_head, a.c.d) && apart(plan->n_rows, v_row, a.c.heads, v_head, a.c.d)))
+    return ADMMQ_ERR_SHAPE;
   if (!aligned(d_status, 4)) return ADMMQ_ERR_INVALID_ARG;
   if (plan->n_rows == 0) return ADMMQ_OK;
   if (!aligned(k, 16) || !aligned(v, 16)) return ADMMQ_ERR_INVALID_ARG;
@@ -203,6 +211,7 @@ admmq_status admmq_cache_attend(const admmq_cache* cache, const admmq_cache_plan
   if (!(scale > 0.0) || scale > 1e30 || window < 0) return ADMMQ_ERR_INVALID_ARG;
   if ((long long)a.c.heads * a.pl.group > 65536) return ADMMQ_ERR_SHAPE;
   if (q_row % 8 || q_head % 8 || out_row % 8 || out_head % 8) return ADMMQ_ERR_SHAPE;
+  if (!apart(plan->n_rows, out_row, a.c.heads * a.pl.group, out_head, a.c.d)) return ADMMQ_ERR_SHAPE;
   if (!aligned(d_status, 4)) return ADMMQ_ERR_INVALID_ARG;
   if (plan->n_rows == 0) return ADMMQ_OK;
   if (!aligned(d_q, 16) || !aligned(d_out, 16) || (d_lse && !aligned(d_lse, 4)) || !aligned(d_workspace, 16)) return ADMMQ_ERR_INVALID_ARG;

@@ -158,3 +158,25 @@ def test_numbers_of_a_plan_that_are_refused(kv):
         kv.CachePlan([1], np.array([2 ** 32 + 5]), [[0]])
     with pytest.raises(AdmmqError):
         kv.CachePlan([1, 1], [0, 0], [[0, 1], [2]])
+
+
+def test_outputs_whose_rows_or_heads_overlap_are_refused(kv):
+    from paper_2605_11222_b200 import binding as B
+    lib = kv._library()
+    cache, plan = _cache(kv), _plan(kv)
+
+    def read(k_row, k_head, v_row=128, v_head=64):
+        return lib.admmq_cache_read(C.addressof(cache), C.addressof(plan), 1, None, k_row, k_head, FAKE, v_row, v_head, FAKE, None)
+
+    def attend(row, head):
+        return lib.admmq_cache_attend(C.addressof(cache), C.addressof(plan), 0.125, 0, None, 0, 0, FAKE, row, head, FAKE, FAKE, 0, FAKE, None)
+
+    # six rows, two key heads, four query heads of 64; what fits is refused for its null pointer only
+    for row, head in ((128, 64), (256, 64), (64, 384), (72, 432), (136, 72)):
+        assert read(row, head) == B.ERR_INVALID_ARG
+    for row, head in ((0, 64), (128, 0), (128, 72), (120, 64), (64, 64), (128, 56), (64, 376), (-128, 64)):
+        assert read(row, head) == read(128, 64, row, head) == B.ERR_SHAPE
+    for row, head in ((256, 64), (320, 72), (64, 384)):
+        assert attend(row, head) == B.ERR_INVALID_ARG
+    for row, head in ((0, 64), (256, 0), (248, 64), (256, 56), (64, 376)):
+        assert attend(row, head) == B.ERR_SHAPE

@@ -205,3 +205,23 @@ def test_queries_near_zero(n, size):
     q[0, 2] = 0.0
     q[0, 2, 5] = -size
     s.check_attend(q=q)
+
+
+def test_outputs_that_overlap_are_refused():
+    from paper_2605_11222_b200 import adapt
+    s = Setup([3, 2], [20, 0], 2, 64, 32, group=2)
+    s.new_rows()
+    q = torch.randn(5, 4, 64, generator=s.g, device=DEV).bfloat16()
+    row = torch.zeros(5, 4, 64, dtype=torch.bfloat16, device=DEV)
+    for bad in (row[:1].expand(5, 4, 64), row[:, :1].expand(5, 4, 64), row.as_strided((5, 4, 64), (64, 64, 1))):
+        with pytest.raises(adapt.AdmmqError):
+            s.cache.attend(q, s.plan, out=bad)
+        with pytest.raises(adapt.AdmmqError):
+            s.cache.read(s.plan, k=bad[:, :2])
+        with pytest.raises(adapt.AdmmqError):
+            s.cache.read(s.plan, v=bad[:, :2])
+    want = s.cache.attend(q, s.plan)
+    head_major = torch.zeros(4, 5, 64, dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    got = s.cache.attend(q, s.plan, out=head_major)
+    assert got[0] is head_major and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    adapt.check_device_status(DEV)

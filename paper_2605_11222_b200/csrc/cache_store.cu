@@ -12,7 +12,7 @@
 namespace admmq {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, ENOUGH_CTAS = 2368;
+constexpr int WARPS = 4, THREADS = 32 * WARPS, ENOUGH_CTAS = 16;   // CTAs an SM that keep it busy
 constexpr float LEAST = 9.094947017729282e-13f;     // 2^-40: magnitudes of a block that is held as zeros stay below
 constexpr uint32_t MOST_BITS = 0x53800000u;         // 2^40
 
@@ -312,14 +312,17 @@ __global__ void __launch_bounds__(THREADS, read_ctas(PC)) cache_read_kernel(cons
           store_values<BF16>(x + (slot - u.first) * row_bytes + at * E, v);
         }
       }
-    }  }
+    }
+  }
 }
 
 template <bool WRITE, bool BF16, int PC>
 cudaError_t launch(const StoreArgs& a, cudaStream_t stream) {
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
   cudaLaunchConfig_t cfg = {};
   // Few blocks: a warp for each head's keys and values.  Many: as many CTAs as keep the device busy.
-  const int most = (2 * a.c.heads + WARPS - 1) / WARPS, enough = (ENOUGH_CTAS + a.pl.n_blocks - 1) / a.pl.n_blocks;
+  const int most = (2 * a.c.heads + WARPS - 1) / WARPS, enough = (ENOUGH_CTAS * sms + a.pl.n_blocks - 1) / a.pl.n_blocks;
   cfg.gridDim = dim3((unsigned)a.pl.n_blocks, (unsigned)(most < enough ? most : enough));
   cfg.blockDim = dim3(THREADS);
   cfg.stream = stream;

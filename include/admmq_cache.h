@@ -83,7 +83,7 @@ admmq_status admmq_cache_read(const admmq_cache* cache, const admmq_cache_plan* 
  * so those that a window has left may be gone from the tables):
  *   out = sum_j w_j v_j,  w = softmax_j(scale q . k_j),  lse [n_rows][heads] fp32 = log sum_j exp(scale q . k_j)
  * in fp32 sums; weights (times their value scale) enter the second product as fp16, with 11 bits down to 2^-20 of the row's
- * largest, fewer down to 2^-31 and none below; queries as fp16 after a shift by a power of two of each row (exact for values
+ * largest at least, fewer down to 2^-31 and perhaps none below; queries as fp16 after a shift by a power of two of each row (exact for values
  * within 2^-27 of the row's largest; a query with an infinity or a NaN gives a row of NaN).  Requests
  * that take no part get out = 0 and lse = -inf.  d_lse may be NULL.  A block with scale NaN gives NaN to the rows that see
  * any of its tokens.

@@ -39,8 +39,9 @@ constexpr int STAGES = 2, SCALE_SLOTS = 4, PIECE_SLOTS = 4;
 constexpr int EXTRA = 3;                             // a piece's start and end, in steps
 // Weights are fp16.  The first largest of a row is 2^TOP; one above 2^LIMIT raises the reference for the steps that follow, so that
 // it is 2^TOP again, and one above 2^HARD_LIMIT at once, by a whole number, so that the step's other weights are scaled exactly.
-// So weights down to 2^-20 of the largest have 11 bits, and those down to 2^-31 some (with TOP 0 the positions behind a token with
-// nearly all the weight lost theirs).
+// So weights down to 2^-20 of the largest have 11 bits, and those down to 2^-31 some.  (Behind a token with 99 % of the weight, 131072 and
+// a million positions of one size: the result is off by 9 and 42 % with TOP 0, by 0.2 and 1.1 % with 6.  With 8 references rise more
+// often: a prompt of 8192 takes 642 us in place of 626, with 10 715.)
 constexpr float TOP = 6.0f, LIMIT = 14.0f, HARD_LIMIT = 15.0f;
 __device__ __forceinline__ float whole_raise(float top) { return rintf(top - TOP); }
 constexpr float LN2 = 0.693147180559945309f;

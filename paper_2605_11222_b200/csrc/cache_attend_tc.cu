@@ -18,11 +18,13 @@
 //   warp 21      finds the CTA's pieces of the work, ahead of the others (22 and 23: none)
 // Work is shared out in equal parts (cache_schedule.cuh), a CTA an SM.
 // Bound: exponentials (16 a cycle and SM: 2048 cycles for 256 x 128) and the tensor cores (2048 as well), overlapped.  Measured, 32
-// query and 8 key heads of 128: the last 2048 rows of 32768 1067 us (998 TFLOP/s, 2.5 us or some 4700 cycles a step), a prompt of 8192
-// 618 us (889).  Tensor and exponential pipes are busy 44 % of the time each, the schedulers 50 % (9850 warp instructions a
-// step): what is left is the chain scores, exponents, weights, product of a track, of which only two are under way.  A
-// polynomial in place of a quarter of the exponentials cost 14 %.  A CTA's first
+// query and 8 key heads of 128: the last 2048 rows of 32768 1086 us (981 TFLOP/s, 2.5 us or some 4700 cycles a step), a prompt of 8192
+// 626 us (878); heads of 64 534 us, of 192 (one track) 1623, of 256 2127.  Tensor and exponential pipes are busy 44 % of the time
+// each, the schedulers 50 % (9850 warp instructions a step): what is left is the chain scores, exponents, weights, second
+// product of a track.  Weights lie over their scores, so that a track's next scores wait for its own second product, and for
+// what the other track has before them.  A polynomial in place of a quarter of the exponentials cost 14 %.  A CTA's first
 // scores are there 11 us after its start: schedule and piece 3, queries 5, first codes and product 1.
+// Registers: 88 a thread where the softmax and the codes run, 40 elsewhere; the compiler spills 76 to 178 bytes of a thread.
 // Waits are bounded as in the other tensor-core kernels.  Products of a CTA run in the order of their issue; scores of the
 // next positions overwrite weights on that ground.
 #include "../../include/admmq_testing.h"

@@ -4,9 +4,10 @@
 // registers when their largest magnitude is known, and the codes leave in the order in which the cache keeps them, 16
 // bytes a lane.  Where the block is held in part, the bytes of the earlier tokens are read, rounded to the new scale if it
 // has grown, and written back.
-// Bound: memory for many rows (a bf16 value is read as 2 bytes and written as 1; 16384 rows, 8 heads of 128: written in 20.8 us,
-// 4.8 TB/s, read back in 18.6 us, 5.4 TB/s), a chain of latencies for one: position, page, row with held codes, maximum, store
-// (a token of each of 77 requests, 4.4 us).
+// Bound: memory for many rows (a bf16 value is read as 2 bytes and written as 1; 65536 rows, 8 heads of 128: written in 76 us,
+// 5.3 TB/s, read back in 73 us, 5.5 TB/s; in fp32 115 us, 5.8 TB/s, and 142, 4.7; 16384 rows, from and to cold memory, 29 and 25 us,
+// where the ends count: a warp loads, works, then stores, with nothing under way meanwhile), a chain of latencies for
+// one: position, page, row with held codes, maximum, store (a token of each of 77 requests, 4.4 us).
 #include "cache.h"
 
 namespace admmq {
@@ -101,8 +102,9 @@ __device__ __forceinline__ Item item_of(const StoreArgs& a, const Unit& u, int w
   return i;
 }
 
-// CTAs of an SM that registers are limited for: more would spill, fewer leave the memory waiting (16384 rows, 8 heads of 128, bf16:
-// 20.8 us with 6, 22.8 with 5 or 7, 24.5 without a limit; read back 18.6 with 8, 20.7 without).
+// CTAs of an SM that registers are limited for: more would spill, fewer leave the memory waiting (16384 rows, 8 heads of 128, bf16,
+// again and again, in part from the L2 cache: 20.8 us with 6, 22.8 with 5 or 7, 24.5 without a limit; read back 18.6 with 8, 20.7
+// without).
 constexpr int write_ctas(bool bf16, int pc) { return bf16 ? (pc <= 2 ? 6 : 4) : pc == 1 ? 6 : pc == 2 ? 4 : 2; }
 constexpr int read_ctas(int pc) { return pc <= 2 ? 8 : 5; }
 

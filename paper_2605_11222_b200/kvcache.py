@@ -10,9 +10,9 @@
 16 neighbouring tokens of a head share a scale, max |x| / 127, for keys and for values; where a later token of the 16 is
 larger, the codes that are there are rounded to the new scale.  Every step runs in the library's kernels, on the current
 stream of the cache's device, and can be captured after a first call outside a capture; the device reads `held` and `tables`
-when it runs, so a captured step follows them (keep the plan and the cache: a graph holds their pointers).  Argument errors raise AdmmqError before anything is enqueued; a request that does not fit its table, or a
-page that does not exist, raises it in adapt.check_device_status.  No call records an autograd graph: inputs that require
-grad are refused while grad mode is on.
+when it runs, so a captured step follows them (keep the plan and the cache: a graph holds their pointers).  Argument errors
+raise AdmmqError before anything is enqueued; a request that does not fit its table, or a page that does not exist, raises it
+in adapt.check_device_status.  No call records an autograd graph: inputs that require grad are refused while grad mode is on.
 """
 from __future__ import annotations
 
